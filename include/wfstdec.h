@@ -340,6 +340,106 @@ wd_status wd_stream_advance(wd_stream* s, const int32_t* n_frames);
 wd_status wd_stream_end(wd_stream* s, wd_result** out);
 void      wd_stream_free(wd_stream* s);
 
+/* ---- log-likelihoods from a model's last hidden layer ------------------ */
+
+/* Three operators between an acoustic model's last hidden layer and the
+ * decoder, for many requests (utterances, live streams) that share one model
+ * and one graph.  They enqueue kernels on `stream` and return; nothing is
+ * copied to the host and nothing is kept from one call for the next.
+ * Index arrays live on the device and are not checked on the host: an entry
+ * outside its range is left out as each call says, never followed.  Host
+ * arguments are checked before any device work (WD_EINVAL).  N = 0 is a call
+ * without work.  Row strides (ld) count elements. */
+typedef enum { WD_F32 = 0, WD_F16 = 1, WD_BF16 = 2 } wd_dtype;
+
+/* The output layer W x + b that every row shares, and low-rank adapters
+ * beside it: adapter g adds scale[g] B_g (A_g x).  Device memory, row-major. */
+#define WD_MAX_RANK 128
+typedef struct {
+  int32_t D, P;            /* inputs and outputs, >= 1; 1 <= P < 2^24 */
+  int32_t type;            /* wd_dtype of weight, a, b and the rows: WD_F16 or WD_BF16 */
+  int32_t n_adapters;      /* G >= 0 */
+  int32_t rank;            /* R, 1..WD_MAX_RANK where G > 0 */
+  int64_t weight_ld;       /* >= D */
+  const void* weight;      /* [P][D] */
+  const float* bias;       /* [P]; NULL: none */
+  const void* a;           /* [G][R][D] contiguous */
+  const void* b;           /* [G][P][R] contiguous */
+  const float* scale;      /* [G]; NULL: 1 */
+} wd_head;
+
+/* out[n] = W x[n] + b + scale[g] B_g (A_g x[n]) with g = adapter[n] (any order
+ * of rows; outside 0..G-1, or adapter NULL: the shared layer alone), n < N.
+ * x: N rows of h->type, x_ld >= D.  out: N rows of out_type (WD_F32 or
+ * h->type), out_ld >= P, no overlap with the inputs.  Products are exact, sums
+ * are kept in 32 bits, A_g x in 16 bits of mantissa or more; one rounding to
+ * out_type at the end.  A row never sees another row's adapter (its infinities
+ * and NaNs included).  ws: device, ws_bytes >= wd_project_workspace_bytes(h, N),
+ * 256-byte aligned, in use until the enqueued work has run. */
+wd_status wd_project_workspace_bytes(const wd_head* h, int64_t N, size_t* bytes);
+wd_status wd_project(const wd_head* h, const void* x, int64_t x_ld, int64_t N, const int32_t* adapter, void* out,
+                     int64_t out_ld, int32_t out_type, void* ws, size_t ws_bytes, void* stream);
+
+/* Log-likelihoods of N rows of V logits, in the fp32 the decoder reads.  For
+ * row n with q = request[n] and value z of label v, in this order:
+ *   c = how often v stands in the request's history (hist_off, hist); if c > 0:
+ *     z = (z > 0 ? z / repetition[q] : z * repetition[q])
+ *         - (presence[q] + frequency[q] * c)
+ *   z += the request's bias of v (bias_off, bias_id, bias_val; where v stands
+ *     more than once, the last entry holds)
+ *   z = -inf if the bit of v is clear in the row's mask (whatever z was)
+ *   y = scale * (z - log(sum over the row of exp(z)) - log_prior[v]); with
+ *     normalize = 0 without the log of the sum; y = -inf where z = -inf
+ * so a row that is left empty is -inf throughout, and a NaN or +inf that is
+ * not masked makes the rest of its row NaN (with normalize = 0 only itself as
+ * the formula has it). */
+typedef struct {
+  int64_t N;
+  int32_t V;                 /* 1 <= V < 2^24 */
+  int32_t type;              /* wd_dtype of logits */
+  const void* logits;        /* [N][ld], ld >= V */
+  int64_t ld;
+  int32_t normalize;
+  float scale;               /* finite, > 0 */
+  const float* log_prior;    /* [V], finite; NULL: 0 */
+  int32_t n_requests;        /* Q; 0: no row has a request */
+  const int32_t* request;    /* [N]; NULL: row n is request n; outside 0..Q-1: no history, no biases */
+  const int64_t* hist_off;   /* [Q+1] into hist; NULL: no histories.  Clamped to 0..n_hist */
+  const int32_t* hist;       /* labels; those outside 0..V-1 are left out */
+  int64_t n_hist;
+  const float* repetition;   /* [Q], > 0; NULL: 1 */
+  const float* presence;     /* [Q]; NULL: 0 */
+  const float* frequency;    /* [Q]; NULL: 0 */
+  const int64_t* bias_off;   /* [Q+1] into bias_id, bias_val; NULL: no biases.  Clamped to 0..n_bias */
+  const int32_t* bias_id;    /* labels; those outside 0..V-1 are left out */
+  const float* bias_val;
+  int64_t n_bias;            /* < 2^32 - 1 */
+  const uint32_t* mask;      /* n_masks rows of mask_ld >= ceil(V/32) words, bit v % 32 of word v / 32; NULL: none */
+  int64_t n_masks;
+  int64_t mask_ld;
+  const int32_t* mask_of;    /* [N]; NULL: row n has mask n; outside 0..n_masks-1: no mask */
+  float* out;                /* out_rows rows, out_ld >= V; may be the logits themselves (WD_F32, out_ld = ld,
+                                out_row NULL), else no overlap */
+  int64_t out_ld;
+  int64_t out_rows;
+  const int32_t* out_row;    /* [N] different rows, e.g. of streams' frame stores; NULL: row n (out_rows >= N);
+                                outside 0..out_rows-1: the row is not written */
+} wd_loglikes_args;
+wd_status wd_loglikes_workspace_bytes(const wd_loglikes_args* a, size_t* bytes);
+wd_status wd_loglikes(const wd_loglikes_args* a, void* ws, size_t ws_bytes, void* stream);
+
+/* Label masks for wd_loglikes from the decoding graph: bit k-1 of row n is set
+ * if an arc with input label k >= 1 leaves one of the states
+ * states[off[n]] .. states[off[n+1] - 1] (graph states; others are left out;
+ * repeats and any order allowed).  Epsilon arcs are not followed: states
+ * behind them are in the list, as they are among a frame's lattice nodes
+ * (wd_result_nodes): the masks of frame t come from the nodes of frame t-1.
+ * off: [N+1], clamped to 0..n_states.  mask: N rows of mask_ld >=
+ * ceil(num_pdfs/32) words; those words are written (bits past num_pdfs 0), the
+ * others left as they are. */
+wd_status wd_label_masks(const wd_graph* g, int64_t N, const int64_t* off, const int32_t* states, int64_t n_states,
+                         uint32_t* mask, int64_t mask_ld, void* stream);
+
 /* ---- lattice determinisation (host) ----------------------------------- */
 
 /* The compact "exact lattice" (Sec. 3.4, after Povey et al. 2012) of a pruned

@@ -5,4 +5,4 @@ include/wfstdec.h); `wfstdec` is its ctypes binding.  Importing the package
 does not load the library; the first call does, and raises if it is missing.
 """
 from . import wfstdec  # noqa: F401
-from .wfstdec import Graph, WdError, decode, decode_batch  # noqa: F401
+from .wfstdec import Graph, Head, WdError, decode, decode_batch, loglikes  # noqa: F401

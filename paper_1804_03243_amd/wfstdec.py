@@ -12,6 +12,7 @@ is missing this module raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 from types import SimpleNamespace
@@ -88,9 +89,34 @@ class wd_stats(ctypes.Structure):
                 ("lattice_ms", ctypes.c_float), ("needed", wd_caps)]
 
 
+WD_F32, WD_F16, WD_BF16 = range(3)
+WD_MAX_RANK = 128
+
+
+class wd_head(ctypes.Structure):
+    _fields_ = [("D", ctypes.c_int32), ("P", ctypes.c_int32), ("type", ctypes.c_int32),
+                ("n_adapters", ctypes.c_int32), ("rank", ctypes.c_int32), ("weight_ld", ctypes.c_int64),
+                ("weight", ctypes.c_void_p), ("bias", ctypes.c_void_p), ("a", ctypes.c_void_p),
+                ("b", ctypes.c_void_p), ("scale", ctypes.c_void_p)]
+
+
+class wd_loglikes_args(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int64), ("V", ctypes.c_int32), ("type", ctypes.c_int32),
+                ("logits", ctypes.c_void_p), ("ld", ctypes.c_int64), ("normalize", ctypes.c_int32),
+                ("scale", ctypes.c_float), ("log_prior", ctypes.c_void_p), ("n_requests", ctypes.c_int32),
+                ("request", ctypes.c_void_p), ("hist_off", ctypes.c_void_p), ("hist", ctypes.c_void_p),
+                ("n_hist", ctypes.c_int64), ("repetition", ctypes.c_void_p), ("presence", ctypes.c_void_p),
+                ("frequency", ctypes.c_void_p), ("bias_off", ctypes.c_void_p), ("bias_id", ctypes.c_void_p),
+                ("bias_val", ctypes.c_void_p), ("n_bias", ctypes.c_int64), ("mask", ctypes.c_void_p),
+                ("n_masks", ctypes.c_int64), ("mask_ld", ctypes.c_int64), ("mask_of", ctypes.c_void_p),
+                ("out", ctypes.c_void_p), ("out_ld", ctypes.c_int64), ("out_rows", ctypes.c_int64),
+                ("out_row", ctypes.c_void_p)]
+
+
 EXPORTS = ["wd_graph_bytes", "wd_graph_load", "wd_graph_free", "wd_graph_eps_levels", "wd_graph_eps_paths",
            "wd_workspace_bytes", "wd_decode", "wd_decode_batch", "wd_decode_noalloc", "wd_stream_begin",
-           "wd_stream_advance", "wd_stream_end", "wd_stream_free", "wd_lattice_determinize",
+           "wd_stream_advance", "wd_stream_end", "wd_stream_free", "wd_project_workspace_bytes", "wd_project",
+           "wd_loglikes_workspace_bytes", "wd_loglikes", "wd_label_masks", "wd_lattice_determinize",
            "wd_clat_states", "wd_clat_arcs", "wd_clat_finals", "wd_clat_alignment", "wd_clat_free",
            "wd_result_status",
            "wd_result_cost", "wd_result_words", "wd_result_lattice", "wd_result_nodes",
@@ -131,6 +157,12 @@ def lib():
             "wd_stream_advance": ([VP, P(ctypes.c_int32)], ctypes.c_int),
             "wd_stream_end": ([VP, P(VP)], ctypes.c_int),
             "wd_stream_free": ([VP], None),
+            "wd_project_workspace_bytes": ([VP, ctypes.c_int64, P(ctypes.c_size_t)], ctypes.c_int),
+            "wd_project": ([VP, VP, ctypes.c_int64, ctypes.c_int64, VP, VP, ctypes.c_int64, ctypes.c_int32, VP,
+                            ctypes.c_size_t, VP], ctypes.c_int),
+            "wd_loglikes_workspace_bytes": ([VP, P(ctypes.c_size_t)], ctypes.c_int),
+            "wd_loglikes": ([VP, VP, ctypes.c_size_t, VP], ctypes.c_int),
+            "wd_label_masks": ([VP, ctypes.c_int64, VP, VP, ctypes.c_int64, VP, ctypes.c_int64, VP], ctypes.c_int),
             "wd_lattice_determinize": ([VP, ctypes.c_int64, VP, ctypes.c_int64, ctypes.c_int32, VP,
                                         ctypes.c_double, ctypes.c_int64, P(VP)], ctypes.c_int),
             "wd_clat_states": ([VP], ctypes.c_int32),
@@ -272,6 +304,32 @@ def wd_stream_end(sh: int, B: int) -> tuple[int, list[int]]:
 
 def wd_stream_free(sh: int) -> None:
     lib().wd_stream_free(sh)
+
+
+def wd_project_workspace_bytes(head: wd_head, N: int) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().wd_project_workspace_bytes(ctypes.byref(head), N, ctypes.byref(n)))
+    return n.value
+
+
+def wd_project(head: wd_head, x: int, x_ld: int, N: int, adapter: int | None, out: int, out_ld: int, out_type: int,
+               ws: int | None, ws_bytes: int, stream: int) -> None:
+    _check(lib().wd_project(ctypes.byref(head), x, x_ld, N, adapter, out, out_ld, out_type, ws, ws_bytes, stream))
+
+
+def wd_loglikes_workspace_bytes(args: wd_loglikes_args) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().wd_loglikes_workspace_bytes(ctypes.byref(args), ctypes.byref(n)))
+    return n.value
+
+
+def wd_loglikes(args: wd_loglikes_args, ws: int | None, ws_bytes: int, stream: int) -> None:
+    _check(lib().wd_loglikes(ctypes.byref(args), ws, ws_bytes, stream))
+
+
+def wd_label_masks(handle: int, N: int, off: int, states: int, n_states: int, mask: int, mask_ld: int,
+                   stream: int) -> None:
+    _check(lib().wd_label_masks(handle, N, off, states, n_states, mask, mask_ld, stream))
 
 
 def wd_lattice_determinize(links, nodes, start_state: int, node_final=None, beam: float = float("inf"),
@@ -475,6 +533,30 @@ class Graph:
         eps = self._arrs["ilabel"] == 0
         return np.bincount(src[~eps], minlength=S), np.bincount(src[eps], minlength=S)
 
+    def label_masks(self, offsets, states, out=None):
+        """Masks of the input labels that leave sets of graph states, for
+        loglikes(): states (int32) of row n are states[offsets[n]:offsets[n+1]]
+        (offsets int64), all device tensors.  Epsilon arcs are not followed.
+        Returns int32 words [N, ceil(num_pdfs / 32)], bit k - 1 for label k;
+        `out`: rows of at least that many words to write into.  Enqueued on
+        the current stream."""
+        torch = _torch()
+        _vector(offsets, torch.int64, self.device, "offsets")
+        _vector(states, torch.int32, self.device, "states")
+        N, words = offsets.shape[0] - 1, (self.num_pdfs + 31) // 32
+        if N < 0:
+            raise ValueError("offsets need at least one entry")
+        if out is None:
+            out = torch.empty((N, words), dtype=torch.int32, device=self.device)
+        else:
+            _matrix(out, (torch.int32,), self.device, "out")
+            if out.shape[0] != N or out.shape[1] < words:
+                raise ValueError(f"out must be {N} rows of at least {words} words")
+        with _on(torch, self.device):
+            wd_label_masks(self.handle, N, offsets.data_ptr(), states.data_ptr(), states.shape[0], out.data_ptr(),
+                           max(out.stride(0), words), _stream(torch))
+        return out
+
     def workspace(self, lanes: int, max_T: int, params: wd_params, caps: wd_caps | None):
         """(pointer, bytes) of a workspace large enough; reuses one buffer."""
         torch = _torch()
@@ -621,6 +703,19 @@ class Stream:
         for i, n in enumerate(counts):
             self.T[i] += n
 
+    def advance(self, n_frames: list) -> None:
+        """n_frames[i] more rows of utterance i stand in `frames` behind the
+        T[i] decoded ones, written on the decoding stream (the one current at
+        construction), e.g. by loglikes(out=..., out_row=...): decodes them
+        without a copy."""
+        counts = [int(n) for n in n_frames]
+        if len(counts) != self.B:
+            raise ValueError(f"n_frames needs {self.B} counts")
+        torch = _torch()
+        with torch.cuda.device(self.graph.device):
+            wd_stream_advance(self.handle, counts)
+        self.T = [t + n for t, n in zip(self.T, counts)]
+
     def end(self) -> list:
         torch = _torch()
         with torch.cuda.device(self.graph.device):
@@ -648,3 +743,185 @@ class Stream:
             except Exception:
                 pass
             self.handle = None
+
+
+# ------------------------------------------- log-likelihoods from hidden rows
+
+def _on(torch, device):
+    """The device as the current one (nothing to do where it is)."""
+    return contextlib.nullcontext() if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+
+
+def _vector(t, dtype, device, what):
+    if t.dtype != dtype or t.dim() != 1 or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous 1-d {dtype} tensor on {device}")
+
+
+def _matrix(t, dtypes, device, what):
+    if t.dtype not in dtypes or t.dim() != 2 or t.device != device:
+        raise ValueError(f"{what} must be a 2-d tensor of {' or '.join(map(str, dtypes))} on {device}")
+    if t.shape[1] > 1 and t.stride(1) != 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+        raise ValueError(f"{what} must have contiguous, separate rows")
+
+
+def _ld(t):
+    """Row stride in elements (of no meaning for a single row)."""
+    return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
+
+
+class Head:
+    """A model's output layer with low-rank adapters (wd_project):
+    out[n] = W x[n] + bias + scale[g] B_g (A_g x[n]), g = adapter[n].
+
+    weight [P, D] (float16 or bfloat16), bias [P] (float32), adapter_a
+    [G, R, D] and adapter_b [G, P, R] (type of weight, R <= 128),
+    adapter_scale [G] (float32); all device tensors, kept by reference: weights
+    changed in place are the ones the next call uses."""
+
+    def __init__(self, weight, bias=None, adapter_a=None, adapter_b=None, adapter_scale=None):
+        torch = _torch()
+        types = {torch.float16: WD_F16, torch.bfloat16: WD_BF16}
+        _matrix(weight, tuple(types), weight.device, "weight")
+        P, D = weight.shape
+        dev = weight.device
+        if bias is not None:
+            _vector(bias, torch.float32, dev, "bias")
+            if bias.shape[0] != P:
+                raise ValueError(f"bias needs {P} values")
+        if (adapter_a is None) != (adapter_b is None) or adapter_scale is not None and adapter_a is None:
+            raise ValueError("adapters need adapter_a and adapter_b")
+        G = R = 0
+        if adapter_a is not None:
+            for t, what in ((adapter_a, "adapter_a"), (adapter_b, "adapter_b")):
+                if t.dim() != 3 or t.dtype != weight.dtype or t.device != dev or not t.is_contiguous():
+                    raise ValueError(f"{what} must be a contiguous 3-d {weight.dtype} tensor on {dev}")
+            G, R = adapter_a.shape[:2]
+            if tuple(adapter_a.shape) != (G, R, D) or tuple(adapter_b.shape) != (G, P, R):
+                raise ValueError(f"adapters must be [G, R, {D}] and [G, {P}, R]")
+            if adapter_scale is not None:
+                _vector(adapter_scale, torch.float32, dev, "adapter_scale")
+                if adapter_scale.shape[0] != G:
+                    raise ValueError(f"adapter_scale needs {G} values")
+        self.D, self.P, self.G, self.R = D, P, G, R
+        self.device, self.dtype = dev, weight.dtype
+        self._kept = (weight, bias, adapter_a, adapter_b, adapter_scale)
+        ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+        self.desc = wd_head(D, P, types[weight.dtype], G, R, _ld(weight), ptr(weight), ptr(bias), ptr(adapter_a),
+                            ptr(adapter_b), ptr(adapter_scale))
+        self._out_types = {torch.float32: WD_F32, weight.dtype: types[weight.dtype]}
+        wd_project_workspace_bytes(self.desc, 0)  # the library's checks
+
+    def project(self, x, adapter=None, out=None, out_dtype=None):
+        """Logits [N, P] of the rows x [N, D]; adapter: int32 [N], the rows'
+        adapters (negative: none).  out_dtype: float32 (default) or the
+        weight's type; `out`: a tensor to write instead.  Enqueued on the
+        current stream."""
+        torch = _torch()
+        _matrix(x, (self.dtype,), self.device, "x")
+        N = x.shape[0]
+        if x.shape[1] != self.D:
+            raise ValueError(f"x must be N x {self.D}")
+        if adapter is not None:
+            _vector(adapter, torch.int32, self.device, "adapter")
+            if adapter.shape[0] != N:
+                raise ValueError(f"adapter needs {N} entries")
+        if out is None:
+            out = torch.empty((N, self.P), dtype=torch.float32 if out_dtype is None else out_dtype, device=self.device)
+        else:
+            _matrix(out, tuple(self._out_types), self.device, "out")
+            if tuple(out.shape) != (N, self.P) or out_dtype not in (None, out.dtype):
+                raise ValueError(f"out must be {N} x {self.P} of out_dtype")
+        if out.dtype not in self._out_types:
+            raise ValueError(f"out_dtype must be float32 or {self.dtype}")
+        with _on(torch, self.device):
+            nbytes = wd_project_workspace_bytes(self.desc, N) if adapter is not None else 0
+            ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device) if nbytes else None
+            wd_project(self.desc, x.data_ptr(), _ld(x), N, None if adapter is None else adapter.data_ptr(),
+                       out.data_ptr(), _ld(out), self._out_types[out.dtype], None if ws is None else ws.data_ptr(),
+                       nbytes, _stream(torch))
+        return out
+
+
+def loglikes(logits, *, normalize: bool = True, scale: float = 1.0, log_prior=None, request=None, history=None,
+             repetition=None, presence=None, frequency=None, bias=None, mask=None, mask_of=None, out=None,
+             out_row=None):
+    """Log-likelihoods (float32) of logits [N, V] (float32, float16 or
+    bfloat16): penalties, biases, masks, log-softmax, priors and scale, in the
+    order and with the meaning of wd_loglikes.  All tensors are on one device:
+
+    log_prior       float32 [V]
+    request         int32 [N], the rows' requests (default: row n is request n)
+    history         (offsets int64 [Q+1], labels int32) of the Q requests
+    repetition, presence, frequency   float32 [Q], the penalties of the history's labels
+    bias            (offsets int64 [Q+1], labels int32, values float32)
+    mask, mask_of   int32 words [M, >= ceil(V/32)] (Graph.label_masks) and
+                    int32 [N], the rows' masks (default: row n has mask n)
+    out, out_row    rows of V float32 to write into, and int32 [N], the row of
+                    each result (default: row n), e.g. Stream.frames viewed as rows
+
+    Returns `out`.  Enqueued on the current stream."""
+    torch = _torch()
+    types = {torch.float32: WD_F32, torch.float16: WD_F16, torch.bfloat16: WD_BF16}
+    dev = logits.device
+    _matrix(logits, tuple(types), dev, "logits")
+    N, V = logits.shape
+    a = wd_loglikes_args(N=N, V=V, type=types[logits.dtype], logits=logits.data_ptr(), ld=_ld(logits),
+                         normalize=int(bool(normalize)), scale=scale)
+    if log_prior is not None:
+        _vector(log_prior, torch.float32, dev, "log_prior")
+        if log_prior.shape[0] != V:
+            raise ValueError(f"log_prior needs {V} values")
+        a.log_prior = log_prior.data_ptr()
+    for t, what in ((request, "request"), (mask_of, "mask_of"), (out_row, "out_row")):
+        if t is not None:
+            _vector(t, torch.int32, dev, what)
+            if t.shape[0] != N:
+                raise ValueError(f"{what} needs {N} entries")
+            setattr(a, what, t.data_ptr())
+    Q = None
+    for lists, names in ((history, ("hist_off", "hist")), (bias, ("bias_off", "bias_id", "bias_val"))):
+        if lists is None:
+            continue
+        if len(lists) != len(names):
+            raise ValueError("history is (offsets, labels), bias (offsets, labels, values)")
+        for t, name, dtype in zip(lists, names, (torch.int64, torch.int32, torch.float32)):
+            _vector(t, dtype, dev, name)
+            setattr(a, name, t.data_ptr())
+        if any(t.shape[0] != lists[1].shape[0] for t in lists[2:]):
+            raise ValueError("bias needs a value per label")
+        q = lists[0].shape[0] - 1
+        if q < 1 or Q not in (None, q):
+            raise ValueError("history and bias need offsets of the same requests, one more than requests")
+        Q = q
+    for t, what in ((repetition, "repetition"), (presence, "presence"), (frequency, "frequency")):
+        if t is not None:
+            if history is None:
+                raise ValueError(f"{what} needs a history")
+            _vector(t, torch.float32, dev, what)
+            if t.shape[0] != Q:
+                raise ValueError(f"{what} needs {Q} values")
+            setattr(a, what, t.data_ptr())
+    a.n_requests = Q or 0
+    a.n_hist = 0 if history is None else history[1].shape[0]
+    a.n_bias = 0 if bias is None else bias[1].shape[0]
+    if mask is not None:
+        _matrix(mask, (torch.int32,), dev, "mask")
+        if mask.shape[1] < (V + 31) // 32:
+            raise ValueError(f"mask needs {(V + 31) // 32} words per row")
+        a.mask, a.n_masks, a.mask_ld = mask.data_ptr(), mask.shape[0], _ld(mask)
+    elif mask_of is not None:
+        raise ValueError("mask_of needs a mask")
+    if out is None:
+        if out_row is not None:
+            raise ValueError("out_row needs out")
+        out = torch.empty((N, V), dtype=torch.float32, device=dev)
+    else:
+        _matrix(out, (torch.float32,), dev, "out")
+        if out.shape[1] != V or out_row is None and out.shape[0] != N:
+            raise ValueError(f"out must be rows of {V} float32, {N} of them without out_row")
+    a.out, a.out_ld, a.out_rows = out.data_ptr(), _ld(out), out.shape[0]
+    with _on(torch, dev):
+        nbytes = wd_loglikes_workspace_bytes(a)
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+        wd_loglikes(a, None if ws is None else ws.data_ptr(), nbytes, _stream(torch))
+    return out

@@ -1,0 +1,231 @@
+"""Projection with low-rank adapters (Head.project, wd_project) against a plain
+64-bit implementation, within the bounds of 32-bit sums: types, odd sizes,
+strides, ranks, rows of many adapters in any order, infinities beside them."""
+import pytest
+import torch
+
+import plain_scores as plain
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+F32, F16, BF16 = torch.float32, torch.float16, torch.bfloat16
+
+
+@pytest.fixture(scope="module")
+def wf():
+    from paper_1804_03243_amd import wfstdec
+    assert torch.cuda.is_available()
+    wfstdec.lib()
+    return wfstdec
+
+
+def make(N, D, P, G, R, dtype, seed=0, adapters="mixed"):
+    gen = torch.Generator().manual_seed(seed)
+    rnd = lambda *s: torch.randn(s, generator=gen)  # noqa: E731
+    d = dict(x=rnd(N, D).to(dtype), weight=(rnd(P, D) / D ** 0.5).to(dtype), bias=rnd(P))
+    if G:
+        d.update(a=(rnd(G, R, D) / D ** 0.5).to(dtype), b=(rnd(G, P, R) / R ** 0.5).to(dtype),
+                 scale=torch.rand(G, generator=gen) + 0.5)
+        if adapters == "mixed":  # any order, some without, some out of range
+            d["adapter"] = torch.randint(-2, G + 1, (N,), generator=gen, dtype=torch.int32)
+        elif adapters == "runs":
+            d["adapter"] = (torch.arange(N) * G // max(N, 1)).to(torch.int32)
+        else:
+            d["adapter"] = (torch.arange(N) % G).to(torch.int32)
+    return d
+
+
+def head_of(wf, d):
+    on = lambda k: d[k].to(DEV) if k in d else None  # noqa: E731
+    return wf.Head(on("weight"), on("bias"), on("a"), on("b"), on("scale"))
+
+
+def check(wf, d, out_dtype=F32):
+    y = head_of(wf, d).project(d["x"].to(DEV), d["adapter"].to(DEV) if "adapter" in d else None, out_dtype=out_dtype)
+    want, bound = plain.project(d["x"], d["weight"], d.get("bias"), d.get("a"), d.get("b"), d.get("scale"),
+                                d.get("adapter"), out_dtype)
+    plain.close(y, want, bound)
+    return y
+
+
+@pytest.mark.parametrize("dtype,same", [(BF16, False), (F16, False), (BF16, True), (F16, True)])
+@pytest.mark.parametrize("N,D,P,G,R", [
+    (1, 1, 1, 1, 1), (1, 8, 5, 2, 3), (2, 64, 16, 1, 8), (3, 100, 63, 3, 7), (15, 32, 64, 4, 16), (16, 31, 65, 16, 2),
+    (17, 129, 257, 5, 17), (33, 512, 500, 33, 8), (64, 256, 130, 64, 16), (65, 72, 300, 7, 12), (100, 1000, 77, 9, 33),
+    (129, 200, 129, 3, 64), (200, 64, 1000, 200, 4), (300, 320, 520, 6, 128), (520, 128, 513, 40, 16), (700, 96, 264, 2, 5),
+])
+def test_sizes(wf, dtype, same, N, D, P, G, R):
+    check(wf, make(N, D, P, G, R, dtype, seed=N + D), dtype if same else F32)
+
+
+@pytest.mark.parametrize("adapters", ["runs", "cycle", "mixed"])
+@pytest.mark.parametrize("N", [40, 260, 1030])
+def test_orders_of_adapters(wf, adapters, N):
+    check(wf, make(N, 128, 192, 13, 16, BF16, seed=N, adapters=adapters))
+
+
+@pytest.mark.parametrize("N", [1, 20, 300])
+def test_without_adapters_bias_or_scale(wf, N):
+    d = make(N, 96, 130, 0, 0, F16, seed=N)
+    del d["bias"]
+    check(wf, d)
+    d = make(N, 96, 130, 3, 8, F16, seed=N)
+    del d["scale"]
+    check(wf, d)
+    none = dict(d, adapter=torch.full((N,), -1, dtype=torch.int32))
+    y = check(wf, none)
+    z = head_of(wf, d).project(d["x"].to(DEV))  # no adapter given: the shared layer
+    assert torch.equal(y, z)
+
+
+def test_large_problem_many_tiles(wf):
+    """Rows and outputs beyond several tiles of every size, against 64 bits on the GPU."""
+    N, D, P, G, R = 4099, 328, 2056, 11, 24
+    d = make(N, D, P, G, R, BF16, seed=3, adapters="runs")
+    y = head_of(wf, d).project(d["x"].to(DEV), d["adapter"].to(DEV)).cpu().double()
+    X, W = d["x"].double(), d["weight"].double()
+    want = X @ W.T + d["bias"].double()
+    mag = X.abs() @ W.abs().T + d["bias"].double().abs()
+    low = torch.zeros(N, P, dtype=torch.float64)
+    for g in range(G):
+        r = d["adapter"] == g
+        low[r] = float(d["scale"][g]) * ((X[r].abs() @ d["a"][g].double().abs().T) @ d["b"][g].double().abs().T)
+        want[r] += float(d["scale"][g]) * ((X[r] @ d["a"][g].double().T) @ d["b"][g].double().T)
+    bound = (D + 8) * plain.EPS * mag + ((D + 2 * R + 16) * plain.EPS + 2.0 ** -16) * low + plain.EPS * want.abs()
+    plain.close(y, want, bound)
+
+
+@pytest.mark.parametrize("N,D", [(5, 64), (70, 64), (5, 60), (300, 72)])
+def test_strides_and_alignment(wf, N, D):
+    """Rows inside wider tensors, starting at odd elements; columns beside the output stay."""
+    P, G, R = 70, 3, 6
+    d = make(N, D, P, G, R, BF16, seed=7)
+    for first in (0, 1, 3, 8):
+        wide = torch.full((N, D + 13), float("nan"), dtype=BF16, device=DEV)
+        wide[:, first:first + D] = d["x"].to(DEV)
+        wwide = torch.full((P, D + 9), float("nan"), dtype=BF16, device=DEV)
+        wwide[:, first:first + D] = d["weight"].to(DEV)
+        head = wf.Head(wwide[:, first:first + D], d["bias"].to(DEV), d["a"].to(DEV), d["b"].to(DEV), d["scale"].to(DEV))
+        for dtype in (F32, BF16):
+            owide = torch.full((N + 2, P + 5), 7.0, dtype=dtype, device=DEV)
+            out = owide[1:N + 1, first % 4:first % 4 + P]
+            assert head.project(wide[:, first:first + D], d["adapter"].to(DEV), out=out) is out
+            want, bound = plain.project(d["x"], d["weight"], d["bias"], d["a"], d["b"], d["scale"], d["adapter"], dtype)
+            plain.close(out, want, bound)
+            owide[1:N + 1, first % 4:first % 4 + P] = 7.0
+            assert bool((owide == 7.0).all())
+
+
+@pytest.mark.parametrize("N", [6, 40, 300])
+def test_other_rows_adapters_do_not_reach_a_row(wf, N):
+    """Infinite and NaN adapters: only the rows that use them see them."""
+    d = make(N, 64, 80, 4, 8, BF16, seed=11)
+    d["b"][1] = float("inf")
+    d["a"][2] = float("nan")
+    y = head_of(wf, d).project(d["x"].to(DEV), d["adapter"].to(DEV)).cpu()
+    hit = (d["adapter"] == 1) | (d["adapter"] == 2)
+    want, bound = plain.project(d["x"], d["weight"], d["bias"], d["a"], d["b"], d["scale"], d["adapter"])
+    plain.close(y[~hit], want[~hit], bound[~hit])
+    assert not torch.isfinite(y[hit]).any()
+    x = d["x"].clone()
+    x[N // 2] = float("inf")  # nor does a row reach another row
+    z = head_of(wf, d).project(x.to(DEV), d["adapter"].to(DEV)).cpu()
+    rest = (torch.arange(N) != N // 2) & ~hit
+    assert torch.equal(z[rest], y[rest])
+    assert not torch.isfinite(z[N // 2]).any()
+
+
+@pytest.mark.parametrize("N", [3, 50, 280])
+def test_half_precision_low_rank_beyond_its_range(wf, N):
+    """A_g x above 65504 and far below 2^-24: held with the row's exponent."""
+    d = make(N, 64, 48, 4, 8, F16, seed=5)
+    d["a"][0] *= 3000.0
+    d["x"][: N // 2] *= 100.0
+    d["b"][0] /= 3000.0
+    d["scale"][1] = 1e-9
+    d["scale"][2] = 1e6
+    d["b"][2] *= 1e-3
+    check(wf, d)
+
+
+def test_weights_changed_in_place_and_repeated_calls(wf):
+    d = make(40, 64, 96, 3, 8, BF16, seed=9)
+    head, x, g = head_of(wf, d), d["x"].to(DEV), d["adapter"].to(DEV)
+    y = head.project(x, g)
+    assert torch.equal(y, head.project(x, g))
+    head._kept[0].mul_(2.0)
+    head._kept[3].mul_(2.0)
+    d["weight"], d["b"] = d["weight"] * 2, d["b"] * 2
+    want, bound = plain.project(d["x"], d["weight"], d["bias"], d["a"], d["b"], d["scale"], d["adapter"])
+    plain.close(head.project(x, g), want, bound)
+
+
+def test_empty_and_other_stream(wf):
+    d = make(30, 64, 96, 3, 8, BF16, seed=2)
+    head = head_of(wf, d)
+    x, g = d["x"].to(DEV), d["adapter"].to(DEV)
+    assert tuple(head.project(x[:0], g[:0]).shape) == (0, 96)
+    want = head.project(x, g)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        y = head.project(x, g)
+    s.synchronize()
+    assert torch.equal(y, want)
+
+
+def test_rows_beyond_32_bit_offsets(wf):
+    """Rows and outputs whose element offsets pass 2^31."""
+    N, D, P, ld = 40, 64, 96, 1 << 26
+    d = make(N, D, P, 3, 8, BF16, seed=4)
+    wide = torch.empty((N, ld), dtype=BF16, device=DEV)
+    wide[:, :D] = d["x"].to(DEV)
+    owide = torch.empty((N, ld), dtype=BF16, device=DEV)
+    out = head_of(wf, d).project(wide[:, :D], d["adapter"].to(DEV), out=owide[:, :P])
+    want, bound = plain.project(d["x"], d["weight"], d["bias"], d["a"], d["b"], d["scale"], d["adapter"], BF16)
+    plain.close(out, want, bound)
+
+
+def test_graph_capture_replays(wf):
+    """Recorded into a graph and replayed with new rows: the eager result each time."""
+    d = make(64, 128, 160, 5, 8, BF16, seed=6)
+    head, x, g = head_of(wf, d), d["x"].to(DEV), d["adapter"].to(DEV)
+    out = torch.empty((64, 160), device=DEV)
+    head.project(x, g, out=out)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        head.project(x, g, out=out)
+    for k in range(4):
+        x.copy_(torch.roll(d["x"], k, 0).to(DEV))
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, head.project(x, g))
+
+
+def test_refusals(wf):
+    d = make(8, 64, 32, 3, 8, BF16)
+    on = {k: v.to(DEV) for k, v in d.items()}
+    head = head_of(wf, d)
+    for bad in (on["x"].float(), on["x"][:, :60], on["x"].cpu(), on["x"].t(), on["x"][0]):
+        with pytest.raises(ValueError):
+            head.project(bad)
+    for bad in (on["adapter"].long(), on["adapter"][:5], d["adapter"]):
+        with pytest.raises(ValueError):
+            head.project(on["x"], bad)
+    with pytest.raises(ValueError):
+        head.project(on["x"], out_dtype=F16)
+    with pytest.raises(ValueError):
+        head.project(on["x"], out=torch.empty((8, 31), device=DEV))
+    with pytest.raises(ValueError):
+        wf.Head(on["weight"].float())
+    with pytest.raises(ValueError):
+        wf.Head(on["weight"], on["bias"][:5])
+    with pytest.raises(ValueError):
+        wf.Head(on["weight"], None, on["a"])
+    with pytest.raises(ValueError):
+        wf.Head(on["weight"], None, on["a"], on["b"][:, :5])
+    with pytest.raises(wf.WdError):
+        wf.Head(on["weight"], None, torch.zeros((1, 129, 64), dtype=BF16, device=DEV),
+                torch.zeros((1, 32, 129), dtype=BF16, device=DEV))
