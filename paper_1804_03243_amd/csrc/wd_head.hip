@@ -73,8 +73,6 @@ __device__ __forceinline__ void split(float u, T* t) {
   }
 }
 
-// u of 64 rows' worth of lanes: lane l holds the sums of rank r of its row in
-// s[r / step] ... written by the callers below.
 template <class T, int TERMS>
 __device__ __forceinline__ void store_u(const HeadArgs& a, int64_t n, int r, float u) {
   T t[TERMS];
@@ -83,104 +81,333 @@ __device__ __forceinline__ void store_u(const HeadArgs& a, int64_t n, int r, flo
   for (int k = 0; k < TERMS; ++k) a.u[n * a.uk + k * a.rp + r] = t[k].u;
 }
 
-// The power of two that a row's u are divided by: 1 for bfloat16.
+// The power of two that a row's u are divided by: 1 for bfloat16, which has the
+// range of 32 bits.
 template <class T>
 __device__ __forceinline__ float row_power(float largest) {
-  if constexpr (sizeof(T) && __is_same(T, Bf16)) return 1.0f;
-  const uint32_t e = __float_as_uint(largest) & 0x7f800000u;
-  return e == 0 || e >= 0x7e800000u ? (e == 0 ? 1.0f : 0x1p126f) : __uint_as_float(e);
+  if constexpr (__is_same(T, Bf16)) {
+    return 1.0f;
+  } else {
+    const uint32_t e = __float_as_uint(largest) & 0x7f800000u;
+    return e == 0 ? 1.0f : fminf(fmaxf(__uint_as_float(e), 0x1p-60f), 0x1p126f);
+  }
 }
 
-// u[n]: a workgroup per row, a wavefront per rank at a time.
+__device__ __forceinline__ float finite_abs(float u) { return fabsf(u) < INFINITY ? fabsf(u) : 0.0f; }
+
+// The products of a row of n elements with two others, by a wavefront.
+template <class T>
+__device__ __forceinline__ void row_products(const T* x, const T* w0, const T* w1, int n, float& s0, float& s1) {
+  s0 = s1 = 0.0f;
+#pragma unroll 2
+  for (int k = (threadIdx.x & 63) * 8; k < n; k += 512) {
+    const uint4 xv = load8(x + k, n - k), v0 = load8(w0 + k, n - k), v1 = load8(w1 + k, n - k);
+    const T *xe = (const T*)&xv, *e0 = (const T*)&v0, *e1 = (const T*)&v1;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      s0 = fmaf(xe[i].f(), e0[i].f(), s0);
+      s1 = fmaf(xe[i].f(), e1[i].f(), s1);
+    }
+  }
+  for (int o = 32; o > 0; o >>= 1) {
+    s0 += __shfl_xor(s0, o);
+    s1 += __shfl_xor(s1, o);
+  }
+}
+
+// u[n]: a workgroup per row, a wavefront per rank at a time (two, whose reads are
+// in flight together).
 template <class T, int TERMS>
-__global__ void __launch_bounds__(256) k_low_row(HeadArgs a) {
+__global__ void __launch_bounds__(512) k_low_row(HeadArgs a) {
   __shared__ float us[WD_MAX_RANK];
   const int64_t n = blockIdx.x;
   const int g = adapter_of(a, n), D = a.h.D, R = a.h.rank;
   if (g < 0) return;  // (never read)
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const T* x = (const T*)a.x + n * a.x_ld;
+  const T* w = (const T*)a.h.a + (int64_t)g * R * D;
   const float sc = a.h.scale ? a.h.scale[g] : 1.0f;
-  for (int r = wave; r < R; r += 4) {
-    const T* w = (const T*)a.h.a + ((int64_t)g * R + r) * D;
-    float s = 0.0f;
-    for (int k = lane * 8; k < D; k += 512) {
-      const uint4 xv = load8(x + k, D - k), wv = load8(w + k, D - k);
-      const T *xe = (const T*)&xv, *we = (const T*)&wv;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) s = fmaf(xe[i].f(), we[i].f(), s);
-    }
-    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
-    if (lane == 0) us[r] = s * sc;
+  for (int r = wave * 2; r < R; r += 16) {
+    float s0, s1;
+    row_products(x, w + (int64_t)r * D, w + (int64_t)min(r + 1, R - 1) * D, D, s0, s1);
+    if (lane < 2 && r + lane < R) us[r + lane] = (lane ? s1 : s0) * sc;
   }
   __syncthreads();
   float top = 0.0f;
-  for (int r = 0; r < R; ++r) top = fmaxf(top, fabsf(us[r]) < INFINITY ? fabsf(us[r]) : 0.0f);
+  for (int r = lane; r < R; r += 64) top = fmaxf(top, finite_abs(us[r]));
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
   const float p = row_power<T>(top);
   if (threadIdx.x == 0) a.us[n] = p;
-  for (int r = threadIdx.x; r < a.rp; r += 256) store_u<T, TERMS>(a, n, r, r < R ? us[r] / p : 0.0f);
+  if ((int)threadIdx.x < a.rp) store_u<T, TERMS>(a, n, threadIdx.x, (int)threadIdx.x < R ? us[threadIdx.x] / p : 0.0f);
+}
+
+// u of 16 rows per workgroup by matrix instructions, the columns split between
+// the wavefronts: A_g's ranks are the first operand, the rows the second, so
+// that lane l holds four ranks of row l % 16 per block of 16 ranks.  Lanes read
+// 32 consecutive bytes of their row, 128 of a row between them (the order of
+// the columns in a sum of products is free).  The adapters of the 16 rows are
+// taken one after another, each row keeping its own.  Rows of many adapters
+// (kLowMix) go one by one on the vector ALU instead.
+constexpr int kLowMix = 3;
+
+template <class T, int TERMS, int RB>
+__global__ void __launch_bounds__(256) k_low_tile(HeadArgs a) {
+  __shared__ float sums[4][16][RB * 16 + 1];  // [wavefront][row][rank]
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
+  const int64_t n0 = (int64_t)blockIdx.x * 16, n = n0 + col;
+  const int D = a.h.D, R = a.h.rank;
+  const int g = adapter_of(a, n);
+  uint64_t todo = __ballot(g >= 0);
+  if (!todo) return;
+  int kinds = 0;
+  for (uint64_t t = todo; t; ++kinds) t &= ~__ballot(g == __builtin_amdgcn_readlane(g, __ffsll((unsigned long long)t) - 1));
+  if (kinds <= kLowMix) {
+    const T* x = (const T*)a.x + (n < a.N ? n : a.N - 1) * a.x_ld;
+    while (todo) {
+      const int gg = __builtin_amdgcn_readlane(g, __ffsll((unsigned long long)todo) - 1);
+      const bool mine = g == gg;
+      todo &= ~__ballot(mine);
+      f32x4 acc[RB] = {};
+      const T* w[RB];
+#pragma unroll
+      for (int b = 0; b < RB; ++b) w[b] = (const T*)a.h.a + ((int64_t)gg * R + min(b * 16 + col, R - 1)) * D;
+      int k = wave * 64 + quad * 16;
+#pragma unroll 4
+      for (; (k & ~63) + 64 <= D; k += 256) {
+#pragma unroll
+        for (int h = 0; h < 16; h += 8) {
+          const uint4 xv = load8(x + k + h, 8);
+#pragma unroll
+          for (int b = 0; b < RB; ++b) acc[b] = mfma16(load8(w[b] + k + h, 8), xv, acc[b], T{});
+        }
+      }
+      if ((k & ~63) < D) {
+        for (int h = 0; h < 16; h += 8) {
+          const uint4 xv = load8(x + k + h, D - k - h);
+#pragma unroll
+          for (int b = 0; b < RB; ++b) acc[b] = mfma16(load8(w[b] + k + h, D - k - h), xv, acc[b], T{});
+        }
+      }
+#pragma unroll
+      for (int b = 0; b < RB; ++b)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (mine) sums[wave][col][b * 16 + quad * 4 + e] = acc[b][e];
+    }
+  } else {
+    for (int i = wave; i < 16; i += 4) {
+      const int gg = __builtin_amdgcn_readlane(g, i);
+      if (gg < 0) continue;
+      const T* x = (const T*)a.x + (n0 + i) * a.x_ld;
+      const T* w = (const T*)a.h.a + (int64_t)gg * R * D;
+      for (int r = 0; r < R; r += 2) {
+        float s0, s1;
+        row_products(x, w + (int64_t)r * D, w + (int64_t)min(r + 1, R - 1) * D, D, s0, s1);
+        // (the other wavefronts' parts of these sums are zero)
+        if (lane < 8 && r + (lane >> 2) < R) sums[lane & 3][i][r + (lane >> 2)] = lane == 0 ? s0 : lane == 4 ? s1 : 0.0f;
+      }
+    }
+  }
+  __syncthreads();
+  const int i = threadIdx.x >> 4, r0 = threadIdx.x & 15;
+  const int gi = adapter_of(a, n0 + i);
+  const float sc = gi >= 0 && a.h.scale ? a.h.scale[gi] : 1.0f;
+  float u[RB], top = 0.0f;
+#pragma unroll
+  for (int b = 0; b < RB; ++b) {
+    const int r = b * 16 + r0;
+    u[b] = r < R ? ((sums[0][i][r] + sums[1][i][r]) + (sums[2][i][r] + sums[3][i][r])) * sc : 0.0f;
+    top = fmaxf(top, finite_abs(u[b]));
+  }
+  for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  if (gi < 0) return;
+  const float p = row_power<T>(top);
+  if (r0 == 0) a.us[n0 + i] = p;
+#pragma unroll
+  for (int b = 0; b < RB; ++b)
+    if (b * 16 + r0 < a.rp) store_u<T, TERMS>(a, n0 + i, b * 16 + r0, u[b] / p);
+}
+
+// A workgroup per row spreads few rows over the chip; from kLowRows on the rows
+// share the reads of their adapter instead.
+constexpr int64_t kLowRows = 512;
+
+template <class T, int TERMS>
+void launch_low(const HeadArgs& a, hipStream_t s) {
+  if (a.N < kLowRows) {
+    hipLaunchKernelGGL((k_low_row<T, TERMS>), dim3((uint32_t)a.N), dim3(512), 0, s, a);
+    return;
+  }
+  const dim3 grid((uint32_t)((a.N + 15) / 16)), block(256);
+  if (a.h.rank <= 16)
+    hipLaunchKernelGGL((k_low_tile<T, TERMS, 1>), grid, block, 0, s, a);
+  else if (a.h.rank <= 32)
+    hipLaunchKernelGGL((k_low_tile<T, TERMS, 2>), grid, block, 0, s, a);
+  else if (a.h.rank <= 64)
+    hipLaunchKernelGGL((k_low_tile<T, TERMS, 4>), grid, block, 0, s, a);
+  else
+    hipLaunchKernelGGL((k_low_tile<T, TERMS, 8>), grid, block, 0, s, a);
 }
 
 // A lane's address for tile rows past the end of the inputs' columns.
 __device__ uint4 k_zeros;
 
-// The part of B_g u for the lane's rows, added to acc; `which(i)` is the row of
-// block i that the lane holds, `prow(j)` the output whose weights it reads.
-template <class T, int TM, int TN, class PRow>
-__device__ __forceinline__ void add_low(const HeadArgs& a, int64_t n0, PRow prow, f32x4 (&acc)[TM][TN]) {
-  const int lane = threadIdx.x & 63;
+// B_g u (before the row's power) of the four outputs from p on of one row per
+// lane, on the vector ALU.
+template <class T, int TERMS, int AHEAD>
+__device__ __forceinline__ f32x4 low_of_row(const HeadArgs& a, int64_t n, int g, int p) {
+  const int R = a.h.rank;
+  f32x4 low = {0, 0, 0, 0};
+  if (g < 0 || p >= a.h.P) return low;
+  const T* b = (const T*)a.h.b + ((int64_t)g * a.h.P + p) * R;
+  const uint16_t* ut = a.u + n * a.uk;
+  const int last = a.h.P - 1 - p;  // rows of B past the last are not read
+#pragma unroll AHEAD
+  for (int r = 0; r < R; r += 8) {
+    uint4 t[TERMS], w[4];
+#pragma unroll
+    for (int k = 0; k < TERMS; ++k) t[k] = *(const uint4*)(ut + k * a.rp + r);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = load8(b + (int64_t)min(e, last) * R + r, R - r);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float u = ((const T*)&t[TERMS - 1])[i].f();
+#pragma unroll
+      for (int k = TERMS - 2; k >= 0; --k) u += ((const T*)&t[k])[i].f();
+#pragma unroll
+      for (int e = 0; e < 4; ++e) low[e] = fmaf(((const T*)&w[e])[i].f(), u, low[e]);
+    }
+  }
+  return low;
+}
+
+// Whether one of the eight values is an infinity or NaN (all exponent bits set).
+template <class T>
+__device__ __forceinline__ bool not_finite(uint4 v) {
+  constexpr uint32_t e = __is_same(T, Bf16) ? 0x7f80u : 0x7c00u;
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  bool bad = false;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) bad |= (w[i] & e) == e || (w[i] & (e << 16)) == (e << 16);
+  return bad;
+}
+
+// A wavefront's rows of more adapters than this take the vector ALU, whose lanes
+// each read their own row's B; the matrix instructions take the adapters in turn.
+constexpr int kWaveMix = 16;
+
+// B_g u for the wavefront's rows n0.., added to acc; prow(j, i) is the output of
+// row i of operand block j, `mine` LDS of the wavefront's own, of 16 lane vectors
+// or as many as it has accumulators.  A row's terms are zero for the other
+// rows' adapters, so that a product with them adds nothing; where an adapter's
+// weights are not all finite (and zero times them would be a NaN), its rows
+// take the vector ALU.
+template <class T, int TERMS, int TM, int TN, class PRow>
+__device__ __forceinline__ void add_low(const HeadArgs& a, int64_t n0, PRow prow, f32x4* mine, f32x4 (&acc)[TM][TN]) {
+  const int lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
   const int R = a.h.rank, P = a.h.P;
+  const int chunks = a.uk / 8, per = a.rp / 8;
   int g[TM];
-  float us[TM];
-  uint64_t any = 0;
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
-    const int64_t n = n0 + i * 16 + (lane & 15);
-    g[i] = adapter_of(a, n);
-    us[i] = g[i] >= 0 ? a.us[n] : 0.0f;
-    any |= __ballot(g[i] >= 0);
+    const int64_t n = n0 + i * 16 + col;
+    const int v = a.adapter[n < a.N ? n : a.N - 1];
+    g[i] = n < a.N && v >= 0 && v < a.h.n_adapters ? v : -1;
   }
-  if (!any) return;
-  const int chunks = a.uk / 8, per = a.rp / 8;
-  for (int kk = 0; kk < chunks; kk += 4) {
-    const int c = kk + (lane >> 4), r = (c % per) * 8;
-    uint4 u[TM];
-#pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      u[i] = make_uint4(0, 0, 0, 0);
-      if (g[i] >= 0 && c < chunks) u[i] = *(const uint4*)(a.u + (n0 + i * 16 + (lane & 15)) * a.uk + c * 8);
-    }
-    // the adapters of the rows, one after another
-    uint64_t todo[TM];
+  uint64_t todo[TM];
+  const auto start = [&]() {
 #pragma unroll
     for (int i = 0; i < TM; ++i) todo[i] = __ballot(g[i] >= 0);
-    for (;;) {
-      int gg = -1;
+  };
+  const auto next = [&]() {  // the first adapter left
+    int gg = -1;
 #pragma unroll
-      for (int i = TM - 1; i >= 0; --i)
-        if (todo[i]) gg = __builtin_amdgcn_readlane(g[i], __ffsll((unsigned long long)todo[i]) - 1);
-      if (gg < 0) break;
-      uint4 b[TN];
+    for (int i = TM - 1; i >= 0; --i)
+      if (todo[i]) gg = __builtin_amdgcn_readlane(g[i], __ffsll((unsigned long long)todo[i]) - 1);
 #pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        const int p = prow(j);
-        b[j] = make_uint4(0, 0, 0, 0);
-        if (c < chunks && p < P) b[j] = load8((const T*)a.h.b + ((int64_t)gg * P + p) * R + r, R - r);
-      }
+    for (int i = 0; i < TM; ++i) todo[i] &= ~__ballot(g[i] == gg);
+    return gg;
+  };
+  start();
+  int kinds = 0;
+  while (kinds <= kWaveMix && next() >= 0) ++kinds;
+  if (kinds == 0) return;
+
+  float us[TM];
+  if constexpr (!__is_same(T, Bf16)) {
 #pragma unroll
-      for (int i = 0; i < TM; ++i) {
-        const bool mine = g[i] == gg;
-        const uint64_t m = __ballot(mine);
-        todo[i] &= ~m;
-        if (!m) continue;
+    for (int i = 0; i < TM; ++i) {
+      us[i] = g[i] >= 0 ? a.us[n0 + i * 16 + col] : 1.0f;
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-          const f32x4 t = mfma16(b[j], u[i], f32x4{0, 0, 0, 0}, T{});
-#pragma unroll
-          for (int e = 0; e < 4; ++e) acc[i][j][e] = mine ? fmaf(t[e], us[i], acc[i][j][e]) : acc[i][j][e];
-        }
-      }
+      for (int j = 0; j < TN; ++j) acc[i][j] *= 1.0f / us[i];  // (a power of two)
     }
+  }
+  // this lane's rows (bit i: of block i) that are left for the vector ALU
+  uint32_t by_row = 0;
+  start();
+#pragma unroll 1
+  for (int gg; (gg = next()) >= 0;) {
+    const T* B = (const T*)a.h.b + (int64_t)gg * P * R;
+    bool bad = kinds > kWaveMix;
+#pragma unroll 1
+    for (int r = quad * 8; r < R && !bad; r += 32)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) bad |= not_finite<T>(load8(B + (int64_t)min(prow(j, col), P - 1) * R + r, R - r));
+    if (!__any(bad)) continue;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      by_row |= (g[i] == gg) << i;
+      g[i] = g[i] == gg ? -1 : g[i];
+    }
+  }
+  start();
+  int gg = next();
+#pragma unroll 1
+  for (int kk = 0; gg >= 0;) {
+    const int c = kk + quad, r = (c % per) * 8;
+    const T* B = (const T*)a.h.b + (int64_t)gg * P * R + r;
+    uint4 b[TN], u[TM];
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      b[j] = load8(B + (int64_t)min(prow(j, col), P - 1) * R, R - r);
+      if (c >= chunks) b[j] = make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const int64_t n = n0 + i * 16 + col;
+      u[i] = *(const uint4*)(a.u + (n < a.N ? n : a.N - 1) * a.uk + min(c, chunks - 1) * 8);
+      if (c >= chunks || g[i] != gg) u[i] = make_uint4(0, 0, 0, 0);
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = mfma16(b[j], u[i], acc[i][j], T{});
+    kk += 4;
+    if (kk >= chunks) {
+      kk = 0;
+      gg = next();
+    }
+  }
+  if (__any(by_row != 0)) {
+    // through LDS, so that the accumulators' indices are constants and they stay in registers
+    constexpr int kHalf = TM * TN < 16 ? TM * TN : 16;
+#pragma unroll
+    for (int h = 0; h < TM * TN; h += kHalf) {
+#pragma unroll 1
+      for (int ij = h; ij < h + kHalf; ++ij) {
+        const int64_t n = n0 + (ij / TN) * 16 + col;
+        const int gi = by_row >> (ij / TN) & 1 ? adapter_of(a, n) : -1;
+        mine[(ij - h) * 64 + lane] = low_of_row<T, TERMS, 1>(a, n, gi, prow(ij % TN, quad * 4));
+      }
+#pragma unroll
+      for (int ij = h; ij < h + kHalf; ++ij) acc[ij / TN][ij % TN] += mine[(ij - h) * 64 + lane];
+    }
+  }
+  if constexpr (!__is_same(T, Bf16)) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] *= us[i];
   }
 }
 
@@ -209,9 +436,9 @@ __device__ __forceinline__ int out_of(int j, int i) {
 }
 
 template <class T, class O, int TM, int TN>
-__device__ __forceinline__ void finish_tile(const HeadArgs& a, int64_t n0, int p0, f32x4 (&acc)[TM][TN]) {
+__device__ __forceinline__ void finish_tile(const HeadArgs& a, int64_t n0, int p0, f32x4* mine, f32x4 (&acc)[TM][TN]) {
   const int lane = threadIdx.x & 63, P = a.h.P;
-  if (a.adapter) add_low<T>(a, n0, [&](int j) { return p0 + out_of<O>(j, lane & 15); }, acc);
+  if (a.adapter) add_low<T, kTerms<T, O>>(a, n0, [&](int j, int i) { return p0 + out_of<O>(j, i); }, mine, acc);
   constexpr int W = sizeof(O) == 4 ? 1 : 2;  // blocks of one store
 #pragma unroll
   for (int j = 0; j < TN; j += W) {
@@ -228,6 +455,89 @@ __device__ __forceinline__ void finish_tile(const HeadArgs& a, int64_t n0, int p
       if (n < a.N && p < P) store_out<O, 4 * W>((O*)a.out + n * a.out_ld + p, y, P - p);
     }
   }
+}
+
+// 16 bytes per lane from global memory straight to LDS at `to` + 16 * lane (the
+// same `to` in every lane).  The compiler does not see this load (its builtin
+// makes every LDS read wait for all of them): the data is there after
+// loads_done() and a barrier.
+__device__ __forceinline__ void load_to_lds(const void* from, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from),
+               "s"(__builtin_amdgcn_readfirstlane(to))
+               : "memory");
+}
+__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+
+// Few rows (up to 16 * NB): what counts is that W streams through the chip once.
+// A workgroup takes 32 outputs of every row, its eight wavefronts a part of the
+// columns each; the operands come straight from memory (x from the caches), 128
+// bytes of a row between the lanes, and the parts are added through LDS.
+template <class T, class O, int NB>
+__global__ void __launch_bounds__(512) k_rows(HeadArgs a) {
+  __shared__ f32x4 part[8][NB * 2][64];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
+  const int D = a.h.D, P = a.h.P, p0 = blockIdx.x * 32;
+  const T *w[2], *x[NB];
+#pragma unroll
+  for (int j = 0; j < 2; ++j) w[j] = (const T*)a.h.weight + (int64_t)min(p0 + j * 16 + col, P - 1) * a.h.weight_ld;
+#pragma unroll
+  for (int i = 0; i < NB; ++i) x[i] = (const T*)a.x + min<int64_t>(i * 16 + col, a.N - 1) * a.x_ld;
+  // the row and the outputs that this lane finishes
+  const int fi = (wave >> 1) * 16 + col, fp = p0 + (wave & 1) * 16 + quad * 4;
+  const int g = wave < NB * 2 ? adapter_of(a, fi) : -1;
+  f32x4 acc[NB][2] = {};
+  int k = wave * 64 + quad * 16;
+#pragma unroll 2
+  for (; (k & ~63) + 64 <= D; k += 512) {
+    uint4 wv[2][2], xv[NB][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) wv[j][h] = load8(w[j] + k + h * 8, 8);
+#pragma unroll
+      for (int i = 0; i < NB; ++i) xv[i][h] = load8(x[i] + k + h * 8, 8);
+    }
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[i][j] = mfma16(wv[j][h], xv[i][h], acc[i][j], T{});
+  }
+  if ((k & ~63) < D) {
+    for (int h = 0; h < 2; ++h) {
+      const int left = D - k - h * 8;
+      uint4 wv[2];
+#pragma unroll
+      for (int j = 0; j < 2; ++j) wv[j] = load8(w[j] + k + h * 8, left);
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        const uint4 xv = load8(x[i] + k + h * 8, left);
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[i][j] = mfma16(wv[j], xv, acc[i][j], T{});
+      }
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < NB; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j) part[wave][i * 2 + j][lane] = acc[i][j];
+  __syncthreads();
+  if (wave >= NB * 2) return;
+  f32x4 y = part[0][wave][lane];
+#pragma unroll
+  for (int v = 1; v < 8; ++v) y += part[v][wave][lane];
+  if (g >= 0) {
+    const f32x4 low = low_of_row<T, kTerms<T, O>, 2>(a, fi, g, fp);
+    const float us = a.us[fi];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) y[e] = fmaf(low[e], us, y[e]);
+  }
+  if (fi >= a.N || fp >= P) return;
+  float out[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) out[e] = y[e] + (a.h.bias && fp + e < P ? a.h.bias[fp + e] : 0.0f);
+  store_out<O, 4>((O*)a.out + fi * a.out_ld + fp, out, P - fp);
 }
 
 constexpr int kStepK = 64;  // columns of a step: 128 bytes of a row
@@ -272,8 +582,7 @@ __global__ void __launch_bounds__(64 * WM * WN) k_project(HeadArgs a, uint32_t r
       const int k = k0 + col[i];
       if constexpr (ALIGNED) {
         const T* p = k < D ? src[i] + k : (const T*)&k_zeros;
-        __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
-                                         (__attribute__((address_space(3))) void*)dst, 16, 0, 0);
+        load_to_lds(p, (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)dst);
       } else {
         *(uint4*)(dst + lane * 16) = load8(src[i] + k, D - k);
       }
@@ -284,6 +593,7 @@ __global__ void __launch_bounds__(64 * WM * WN) k_project(HeadArgs a, uint32_t r
   const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
   int buf = 0;
   stage(0, lds);
+  loads_done();
   __syncthreads();
   for (int k0 = 0; k0 < D; k0 += kStepK, buf ^= 1) {
     if (k0 + kStepK < D) stage(k0 + kStepK, lds + (buf ^ 1) * kTile);
@@ -308,9 +618,10 @@ __global__ void __launch_bounds__(64 * WM * WN) k_project(HeadArgs a, uint32_t r
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = mfma16(w[j], x[i], acc[i][j], T{});
     }
+    loads_done();
     __syncthreads();
   }
-  finish_tile<T, O>(a, n0 + wm, p0 + wn, acc);
+  finish_tile<T, O>(a, n0 + wm, p0 + wn, (f32x4*)lds + wave * (TM * TN < 16 ? TM * TN : 16) * 64, acc);
 }
 
 template <class T, class O, int BM, int BN, int WM, int WN, bool ALIGNED>
@@ -327,12 +638,19 @@ void launch_project(HeadArgs a, hipStream_t s) {
   if (a.adapter) {
     constexpr int terms = kTerms<T, O>;
     a.uk = terms * a.rp;
-    hipLaunchKernelGGL((k_low_row<T, terms>), dim3((uint32_t)a.N), dim3(256), 0, s, a);
+    launch_low<T, terms>(a, s);
   }
   const bool aligned = a.h.D % 8 == 0 && a.x_ld % 8 == 0 && a.h.weight_ld % 8 == 0 && !((uintptr_t)a.x & 15) &&
                        !((uintptr_t)a.h.weight & 15);
   const auto tiles = [&](int64_t m, int64_t n) { return ((a.N + m - 1) / m) * ((a.h.P + n - 1) / n); };
-  if (!aligned)
+  const dim3 outs(((uint32_t)a.h.P + 31) / 32), block(512);
+  if (a.N <= 16)
+    hipLaunchKernelGGL((k_rows<T, O, 1>), outs, block, 0, s, a);
+  else if (a.N <= 32)
+    hipLaunchKernelGGL((k_rows<T, O, 2>), outs, block, 0, s, a);
+  else if (a.N <= 64)
+    hipLaunchKernelGGL((k_rows<T, O, 4>), outs, block, 0, s, a);
+  else if (!aligned)
     launch_tiles<T, O, 64, 64, 2, 2, false>(a, s);
   else if (tiles(256, 256) >= 256)
     launch_tiles<T, O, 256, 256, 2, 4, true>(a, s);
