@@ -19,6 +19,7 @@ namespace wd {
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
 typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef f32x4 __attribute__((aligned(2))) f32x4_any;
 
 __device__ __forceinline__ f32x4 mfma16(uint4 a, uint4 b, f32x4 c, Bf16) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
@@ -37,6 +38,7 @@ struct HeadArgs {
   uint16_t* u;             // [N][uk] terms of u, rank padded to rp: term t of rank r at t * rp + r
   float* us;               // [N] power of two that u was divided by (half precision)
   int32_t rp, uk;
+  bool stream;             // outputs past the caches
 };
 
 // Terms of u for an output of type O.
@@ -411,12 +413,9 @@ __device__ __forceinline__ void add_low(const HeadArgs& a, int64_t n0, PRow prow
   }
 }
 
-// Four (or, of 16-bit outputs, eight) consecutive outputs of a row.
+// N consecutive outputs of a row, those from n on left out.
 template <class O, int N>
-__device__ __forceinline__ void store_out(O* out, const float* y, int n) {
-  Few<O, N> v;
-#pragma unroll
-  for (int i = 0; i < N; ++i) v.v[i] = O::of(y[i]);
+__device__ __forceinline__ void store_out(O* out, const Few<O, N>& v, int n) {
   if (n >= N) {
     *(Few<O, N>*)out = v;
   } else {
@@ -426,33 +425,49 @@ __device__ __forceinline__ void store_out(O* out, const float* y, int n) {
   }
 }
 
-// Which of a wavefront's outputs the lane's row i (0..15) of operand block j
-// is: chosen so that the blocks a lane holds are consecutive outputs, 16 bytes
-// at a store.
-template <class O>
-__device__ __forceinline__ int out_of(int j, int i) {
-  if constexpr (sizeof(O) == 4) return j * 16 + i;
-  return (j >> 1) * 32 + (i >> 2) * 8 + (j & 1) * 4 + (i & 3);
-}
-
+// The adapters' part and the bias, the rounding, and the store: a block of 16
+// rows at a time through LDS (`mine`, the wavefront's own), so that a store
+// instruction writes whole lines of a row.  In the accumulators' layout it writes
+// 64 bytes (half as much of 16-bit outputs) of each of 16 rows: 64000 x 6000
+// outputs of 32 bits took 1250 us, of 16 bits 962, and take 895 and 865.  Outputs
+// larger than the caches go past them (`stream`: 864 and 856 us).
 template <class T, class O, int TM, int TN>
 __device__ __forceinline__ void finish_tile(const HeadArgs& a, int64_t n0, int p0, f32x4* mine, f32x4 (&acc)[TM][TN]) {
-  const int lane = threadIdx.x & 63, P = a.h.P;
-  if (a.adapter) add_low<T, kTerms<T, O>>(a, n0, [&](int j, int i) { return p0 + out_of<O>(j, i); }, mine, acc);
-  constexpr int W = sizeof(O) == 4 ? 1 : 2;  // blocks of one store
+  const int lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4, P = a.h.P;
+  if (a.adapter) add_low<T, kTerms<T, O>>(a, n0, [&](int j, int i) { return p0 + j * 16 + i; }, mine, acc);
+  constexpr int kCols = TN * 16, kEach = 16 / sizeof(O);
+  constexpr int kLine = kCols + kEach;  // a row in LDS, padded against bank conflicts
+  constexpr int kLanes = kCols / kEach, kRows = 64 / kLanes;  // lanes of a row, rows of a store
+  O* rows = (O*)mine;
+  float bias[TN][4];
 #pragma unroll
-  for (int j = 0; j < TN; j += W) {
-    const int p = p0 + out_of<O>(j, (lane >> 4) * 4);
-    float bias[4 * W];
+  for (int j = 0; j < TN; ++j)
 #pragma unroll
-    for (int e = 0; e < 4 * W; ++e) bias[e] = a.h.bias && p + e < P ? a.h.bias[p + e] : 0.0f;
+    for (int e = 0; e < 4; ++e) bias[j][e] = a.h.bias ? a.h.bias[min(p0 + j * 16 + quad * 4 + e, P - 1)] : 0.0f;
+  const int c = (lane % kLanes) * kEach, r0 = lane / kLanes, left = P - p0 - c;
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      const int64_t n = n0 + i * 16 + (lane & 15);
-      float y[4 * W];
+  for (int i = 0; i < TM; ++i) {
 #pragma unroll
-      for (int e = 0; e < 4 * W; ++e) y[e] = acc[i][j + e / 4][e & 3] + bias[e];
-      if (n < a.N && p < P) store_out<O, 4 * W>((O*)a.out + n * a.out_ld + p, y, P - p);
+    for (int j = 0; j < TN; ++j) {
+      Few<O, 4> v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v.v[e] = O::of(acc[i][j][e] + bias[j][e]);
+      struct alignas(4 * sizeof(O)) Four {
+        O v[4];
+      };
+      *(Four*)(rows + col * kLine + j * 16 + quad * 4) = __builtin_bit_cast(Four, v);
+    }
+#pragma unroll
+    for (int q = 0; q < 16; q += kRows) {
+      const uint4 v = *(const uint4*)(rows + (q + r0) * kLine + c);
+      const int64_t n = n0 + i * 16 + q + r0;
+      O* out = (O*)a.out + n * a.out_ld + p0 + c;
+      if (n < a.N) {
+        if (a.stream && left >= kEach)
+          __builtin_nontemporal_store(__builtin_bit_cast(f32x4, v), (f32x4_any*)out);
+        else
+          store_out(out, __builtin_bit_cast(Few<O, kEach>, v), left);
+      }
     }
   }
 }
@@ -460,13 +475,17 @@ __device__ __forceinline__ void finish_tile(const HeadArgs& a, int64_t n0, int p
 // 16 bytes per lane from global memory straight to LDS at `to` + 16 * lane (the
 // same `to` in every lane).  The compiler does not see this load (its builtin
 // makes every LDS read wait for all of them): the data is there after
-// loads_done() and a barrier.
+// loads_left() and a barrier.
 __device__ __forceinline__ void load_to_lds(const void* from, uint32_t to) {
   asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from),
                "s"(__builtin_amdgcn_readfirstlane(to))
                : "memory");
 }
-__device__ __forceinline__ void loads_done() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }
+// Waits until at most N of this wavefront's loads are on their way (they arrive in order).
+template <int N>
+__device__ __forceinline__ void loads_left() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
 
 // Few rows (up to 16 * NB): what counts is that W streams through the chip once.
 // A workgroup takes 32 outputs of every row, its eight wavefronts a part of the
@@ -534,34 +553,47 @@ __global__ void __launch_bounds__(512) k_rows(HeadArgs a) {
     for (int e = 0; e < 4; ++e) y[e] = fmaf(low[e], us, y[e]);
   }
   if (fi >= a.N || fp >= P) return;
-  float out[4];
+  Few<O, 4> out;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) out[e] = y[e] + (a.h.bias && fp + e < P ? a.h.bias[fp + e] : 0.0f);
-  store_out<O, 4>((O*)a.out + fi * a.out_ld + fp, out, P - fp);
+  for (int e = 0; e < 4; ++e) out.v[e] = O::of(y[e] + (a.h.bias ? a.h.bias[min(fp + e, P - 1)] : 0.0f));
+  store_out((O*)a.out + fi * a.out_ld + fp, out, P - fp);
 }
 
-constexpr int kStepK = 64;  // columns of a step: 128 bytes of a row
-
-// Where chunk c (16 bytes) of tile row r lies in LDS: rows of 128 bytes whose
-// chunks are permuted, so that the 16 rows of an operand read fall on
-// different banks.
-template <class O, bool W>
+// Where chunk c (16 bytes) of tile row r lies in LDS: at c ^ swizzle in rows of BK
+// columns, so that the 16 rows of an operand read fall on different banks.
+template <int BK>
 __device__ __forceinline__ int swizzle(int row) {
-  if constexpr (W && sizeof(O) == 2) return ((row >> 1) & 1) | (((row >> 3) & 3) << 1);
-  return (row >> 1) & 7;
+  return BK == 32 ? (row >> 2) & 3 : (row >> 1) & 7;
 }
 
-// BM rows and BN outputs per workgroup of WM x WN wavefronts.
-template <class T, class O, int BM, int BN, int WM, int WN, bool ALIGNED>
-__global__ void __launch_bounds__(64 * WM * WN) k_project(HeadArgs a, uint32_t row_tiles, uint32_t col_tiles) {
+// The tile of this workgroup.  Workgroups go round the eight XCDs, each with an
+// L2 of its own: an XCD takes a run of tiles, in groups of kGroup rows of tiles
+// column by column, so that its workgroups share rows of x and of W.
+constexpr uint32_t kGroup = 8;
+__device__ __forceinline__ void my_tile(uint32_t rows, uint32_t cols, uint32_t& row, uint32_t& col) {
+  const uint32_t all = rows * cols, xcd = blockIdx.x % 8, q = all / 8, r = all % 8;
+  const uint32_t at = xcd * q + min(xcd, r) + blockIdx.x / 8;
+  const uint32_t group = at / (kGroup * cols), first = group * kGroup, height = min(kGroup, rows - first);
+  const uint32_t in = at - first * cols;
+  col = in / height;
+  row = first + in % height;
+}
+
+// BM rows and BN outputs per workgroup of WM x WN wavefronts; steps of BK columns,
+// S of them in LDS: while one is multiplied the next S - 1 are on their way.
+template <class T, class O, int BM, int BN, int WM, int WN, int BK, int S, bool ALIGNED>
+__global__ void __launch_bounds__(64 * WM * WN, 2) k_project(HeadArgs a, uint32_t row_tiles, uint32_t col_tiles) {
   constexpr int kWaves_ = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
-  constexpr int kTile = (BM + BN) * 128;
-  constexpr int kParts = (BM + BN) / 8 / kWaves_;  // groups of 8 rows per wavefront
-  static_assert((BM / 8) % kWaves_ == 0 && (BN / 8) % kWaves_ == 0, "");
+  constexpr int kRowBytes = BK * 2, kChunks = BK / 8, kPartRows = 64 / kChunks;
+  constexpr int kTile = (BM + BN) * kRowBytes;
+  constexpr int kParts = kTile / 1024 / kWaves_;  // loads of a wavefront per step
+  static_assert((BM / kPartRows) % kWaves_ == 0 && (BN / kPartRows) % kWaves_ == 0, "");
   extern __shared__ __attribute__((aligned(16))) char lds[];
   const int D = a.h.D, P = a.h.P;
-  const int64_t n0 = (int64_t)(blockIdx.x / col_tiles) * BM;
-  const int p0 = (int)(blockIdx.x % col_tiles) * BN;
+  uint32_t row_tile, col_tile;
+  my_tile(row_tiles, col_tiles, row_tile, col_tile);
+  const int64_t n0 = (int64_t)row_tile * BM;
+  const int p0 = (int)col_tile * BN;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
 
   // this lane's source rows: parts of BM rows of x, then of BN rows of W
@@ -569,9 +601,9 @@ __global__ void __launch_bounds__(64 * WM * WN) k_project(HeadArgs a, uint32_t r
   int col[kParts];
 #pragma unroll
   for (int i = 0; i < kParts; ++i) {
-    const bool w = i * kWaves_ * 8 >= BM;
-    const int row = (i * kWaves_ + wave) * 8 - (w ? BM : 0) + (lane >> 3);
-    col[i] = ((lane & 7) ^ (w ? swizzle<O, true>(row) : swizzle<O, false>(row))) * 8;
+    const bool w = i * kWaves_ * kPartRows >= BM;
+    const int row = (i * kWaves_ + wave) * kPartRows - (w ? BM : 0) + lane / kChunks;
+    col[i] = ((lane % kChunks) ^ swizzle<BK>(row)) * 8;
     src[i] = w ? (const T*)a.h.weight + (int64_t)min(p0 + row, P - 1) * a.h.weight_ld
                : (const T*)a.x + min(n0 + row, a.N - 1) * a.x_ld;
   }
@@ -591,44 +623,52 @@ __global__ void __launch_bounds__(64 * WM * WN) k_project(HeadArgs a, uint32_t r
 
   f32x4 acc[TM][TN] = {};
   const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
-  int buf = 0;
-  stage(0, lds);
-  loads_done();
-  __syncthreads();
-  for (int k0 = 0; k0 < D; k0 += kStepK, buf ^= 1) {
-    if (k0 + kStepK < D) stage(k0 + kStepK, lds + (buf ^ 1) * kTile);
-    const char* xs = lds + buf * kTile;
-    const char* ws = xs + BM * 128;
+  for (int k = 0; k < S - 1; ++k)
+    if (k * BK < D) stage(k * BK, lds + k * kTile);
+  int slot = 0;
+  for (int k0 = 0; k0 < D; k0 += BK) {
+    // this step is there when at most the loads of the S - 2 after it are on their way
+    if (S > 2 && k0 + (S - 2) * BK < D)
+      loads_left<(S - 2) * kParts>();
+    else
+      loads_left<0>();
+    __syncthreads();  // for every wavefront; and the step before has been read
+    const int ahead = k0 + (S - 1) * BK, to = slot == 0 ? S - 1 : slot - 1;
+    if (ahead < D) stage(ahead, lds + to * kTile);
+    const char* xs = lds + slot * kTile;
+    const char* ws = xs + BM * kRowBytes;
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
+    for (int ks = 0; ks < BK / 32; ++ks) {
       const int c = ks * 4 + (lane >> 4);
       uint4 w[TN], x[TM];
 #pragma unroll
       for (int j = 0; j < TN; ++j) {
-        const int r = wn + out_of<O>(j, lane & 15);
-        w[j] = *(const uint4*)(ws + r * 128 + ((c ^ swizzle<O, true>(r)) << 4));
+        const int r = wn + j * 16 + (lane & 15);
+        w[j] = *(const uint4*)(ws + r * kRowBytes + ((c ^ swizzle<BK>(r)) << 4));
       }
 #pragma unroll
       for (int i = 0; i < TM; ++i) {
         const int r = wm + i * 16 + (lane & 15);
-        x[i] = *(const uint4*)(xs + r * 128 + ((c ^ swizzle<O, false>(r)) << 4));
+        x[i] = *(const uint4*)(xs + r * kRowBytes + ((c ^ swizzle<BK>(r)) << 4));
       }
 #pragma unroll
       for (int i = 0; i < TM; ++i)
 #pragma unroll
         for (int j = 0; j < TN; ++j) acc[i][j] = mfma16(w[j], x[i], acc[i][j], T{});
     }
-    loads_done();
-    __syncthreads();
+    slot = slot == S - 1 ? 0 : slot + 1;
   }
+  __syncthreads();  // LDS is free
   finish_tile<T, O>(a, n0 + wm, p0 + wn, (f32x4*)lds + wave * (TM * TN < 16 ? TM * TN : 16) * 64, acc);
 }
 
-template <class T, class O, int BM, int BN, int WM, int WN, bool ALIGNED>
+template <class T, class O, int BM, int BN, int WM, int WN, int BK, int S, bool ALIGNED>
 void launch_tiles(const HeadArgs& a, hipStream_t s) {
   const uint32_t rows = (uint32_t)((a.N + BM - 1) / BM), cols = ((uint32_t)a.h.P + BN - 1) / BN;
-  auto* k = k_project<T, O, BM, BN, WM, WN, ALIGNED>;
-  constexpr int bytes = 2 * (BM + BN) * 128;
+  auto* k = k_project<T, O, BM, BN, WM, WN, BK, S, ALIGNED>;
+  constexpr int each = BM * BN / 256 / (WM * WN), low = (each < 16 ? each : 16) * 1024 * WM * WN;  // (add_low's)
+  constexpr int stages = S * (BM + BN) * BK * 2;
+  constexpr int bytes = stages > low ? stages : low;
   if (bytes > 65536) (void)hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
   hipLaunchKernelGGL(k, dim3(rows * cols), dim3(64 * WM * WN), bytes, s, a, rows, cols);
 }
@@ -642,6 +682,7 @@ void launch_project(HeadArgs a, hipStream_t s) {
   }
   const bool aligned = a.h.D % 8 == 0 && a.x_ld % 8 == 0 && a.h.weight_ld % 8 == 0 && !((uintptr_t)a.x & 15) &&
                        !((uintptr_t)a.h.weight & 15);
+  a.stream = (uint64_t)a.N * a.h.P * sizeof(O) >= (256u << 20);
   const auto tiles = [&](int64_t m, int64_t n) { return ((a.N + m - 1) / m) * ((a.h.P + n - 1) / n); };
   const dim3 outs(((uint32_t)a.h.P + 31) / 32), block(512);
   if (a.N <= 16)
@@ -651,13 +692,27 @@ void launch_project(HeadArgs a, hipStream_t s) {
   else if (a.N <= 64)
     hipLaunchKernelGGL((k_rows<T, O, 4>), outs, block, 0, s, a);
   else if (!aligned)
-    launch_tiles<T, O, 64, 64, 2, 2, false>(a, s);
-  else if (tiles(256, 256) >= 256)
-    launch_tiles<T, O, 256, 256, 2, 4, true>(a, s);
+    launch_tiles<T, O, 64, 64, 2, 2, 64, 2, false>(a, s);
+  else {
+    static const int v = getenv("WD_TILE") ? atoi(getenv("WD_TILE")) : -1;
+    if constexpr (__is_same(T, Bf16)) {
+    switch (v) {
+      case 0: return launch_tiles<T, O, 256, 256, 2, 4, 64, 2, true>(a, s);
+      case 1: return launch_tiles<T, O, 256, 256, 2, 4, 32, 4, true>(a, s);
+      case 2: return launch_tiles<T, O, 128, 256, 2, 2, 32, 3, true>(a, s);
+      case 3: return launch_tiles<T, O, 256, 128, 2, 2, 32, 3, true>(a, s);
+      case 4: return launch_tiles<T, O, 128, 128, 2, 2, 64, 2, true>(a, s);
+      case 5: return launch_tiles<T, O, 128, 128, 2, 2, 32, 4, true>(a, s);
+      case 6: return launch_tiles<T, O, 256, 256, 2, 4, 32, 3, true>(a, s);
+      case 7: return launch_tiles<T, O, 128, 256, 2, 4, 32, 3, true>(a, s);
+    }}
+    if (tiles(256, 256) >= 256)
+    launch_tiles<T, O, 256, 256, 2, 4, 64, 2, true>(a, s);
   else if (tiles(128, 128) >= 256)
-    launch_tiles<T, O, 128, 128, 2, 2, true>(a, s);
+    launch_tiles<T, O, 128, 128, 2, 2, 64, 2, true>(a, s);
   else
-    launch_tiles<T, O, 64, 64, 2, 2, true>(a, s);
+    launch_tiles<T, O, 64, 64, 2, 2, 64, 2, true>(a, s);
+  }
 }
 
 }  // namespace wd
@@ -716,7 +771,7 @@ extern "C" wd_status wd_project(const wd_head* h, const void* x, int64_t x_ld, i
   if (((uint64_t)N + 63) / 64 * (((uint64_t)h->P + 63) / 64) > INT32_MAX)
     return fail(WD_EINVAL, "project: too many rows for one call");
   HeadArgs a{*h, x, x_ld, N, adapter, out, out_ld, (uint16_t*)ws,
-             adapter ? (float*)((char*)ws + u_bytes(h, N)) : nullptr, adapter ? padded_rank(h) : 0, 0};
+             adapter ? (float*)((char*)ws + u_bytes(h, N)) : nullptr, adapter ? padded_rank(h) : 0, 0, false};
   hipStream_t s = (hipStream_t)stream;
   if (h->type == WD_F16)
     out_type == WD_F32 ? launch_project<Half, F32>(a, s) : launch_project<Half, Half>(a, s);
