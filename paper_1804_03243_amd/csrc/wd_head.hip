@@ -35,9 +35,12 @@ struct HeadArgs {
   const int32_t* adapter;  // NULL: none (also without adapters)
   void* out;
   int64_t out_ld;
-  uint16_t* u;             // [N][uk] terms of u, rank padded to rp: term t of rank r at t * rp + r
-  float* us;               // [N] power of two that u was divided by (half precision)
-  int32_t rp, uk;
+  // [N][ul] terms of u, the rank padded to rp: term t of rank r at t * rp + r, uk of
+  // them, zeros up to ul (a multiple of kStepK); zeros throughout for a row without an adapter
+  uint16_t* u;
+  float* us;               // [N] power of two that u was divided by
+  int32_t rp, uk, ul;
+  bool b16;                // B's rows start at multiples of 16 bytes
   bool stream;             // outputs past the caches
 };
 
@@ -80,18 +83,20 @@ __device__ __forceinline__ void store_u(const HeadArgs& a, int64_t n, int r, flo
   T t[TERMS];
   split<T, TERMS>(u, t);
 #pragma unroll
-  for (int k = 0; k < TERMS; ++k) a.u[n * a.uk + k * a.rp + r] = t[k].u;
+  for (int k = 0; k < TERMS; ++k) a.u[n * a.ul + k * a.rp + r] = t[k].u;
 }
 
 // The power of two that a row's u are divided by: 1 for bfloat16, which has the
-// range of 32 bits.
+// range of 32 bits, and where half precision's two terms hold the row as it is
+// (its largest value to 21 bits).
 template <class T>
 __device__ __forceinline__ float row_power(float largest) {
   if constexpr (__is_same(T, Bf16)) {
     return 1.0f;
   } else {
     const uint32_t e = __float_as_uint(largest) & 0x7f800000u;
-    return e == 0 ? 1.0f : fminf(fmaxf(__uint_as_float(e), 0x1p-60f), 0x1p126f);
+    if (e == 0 || (largest >= 0x1p-4f && largest < 0x1p15f)) return 1.0f;
+    return fminf(fmaxf(__uint_as_float(e), 0x1p-60f), 0x1p126f);
   }
 }
 
@@ -124,7 +129,11 @@ __global__ void __launch_bounds__(512) k_low_row(HeadArgs a) {
   __shared__ float us[WD_MAX_RANK];
   const int64_t n = blockIdx.x;
   const int g = adapter_of(a, n), D = a.h.D, R = a.h.rank;
-  if (g < 0) return;  // (never read)
+  if (g < 0) {
+    for (int k = threadIdx.x; k < a.ul; k += 512) a.u[n * a.ul + k] = 0;
+    if (threadIdx.x == 0) a.us[n] = 1.0f;
+    return;
+  }
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const T* x = (const T*)a.x + n * a.x_ld;
   const T* w = (const T*)a.h.a + (int64_t)g * R * D;
@@ -141,6 +150,7 @@ __global__ void __launch_bounds__(512) k_low_row(HeadArgs a) {
   const float p = row_power<T>(top);
   if (threadIdx.x == 0) a.us[n] = p;
   if ((int)threadIdx.x < a.rp) store_u<T, TERMS>(a, n, threadIdx.x, (int)threadIdx.x < R ? us[threadIdx.x] / p : 0.0f);
+  if (a.uk + (int)threadIdx.x < a.ul) a.u[n * a.ul + a.uk + threadIdx.x] = 0;
 }
 
 // u of 16 rows per workgroup by matrix instructions, the columns split between
@@ -160,7 +170,6 @@ __global__ void __launch_bounds__(256) k_low_tile(HeadArgs a) {
   const int D = a.h.D, R = a.h.rank;
   const int g = adapter_of(a, n);
   uint64_t todo = __ballot(g >= 0);
-  if (!todo) return;
   int kinds = 0;
   for (uint64_t t = todo; t; ++kinds) t &= ~__ballot(g == __builtin_amdgcn_readlane(g, __ffsll((unsigned long long)t) - 1));
   if (kinds <= kLowMix) {
@@ -222,12 +231,13 @@ __global__ void __launch_bounds__(256) k_low_tile(HeadArgs a) {
     top = fmaxf(top, finite_abs(u[b]));
   }
   for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-  if (gi < 0) return;
-  const float p = row_power<T>(top);
+  if (n0 + i >= a.N) return;
+  const float p = gi < 0 ? 1.0f : row_power<T>(top);
   if (r0 == 0) a.us[n0 + i] = p;
 #pragma unroll
   for (int b = 0; b < RB; ++b)
-    if (b * 16 + r0 < a.rp) store_u<T, TERMS>(a, n0 + i, b * 16 + r0, u[b] / p);
+    if (b * 16 + r0 < a.rp) store_u<T, TERMS>(a, n0 + i, b * 16 + r0, gi < 0 ? 0.0f : u[b] / p);
+  for (int k = a.uk + r0; k < a.ul; k += 16) a.u[(n0 + i) * a.ul + k] = 0;
 }
 
 // A workgroup per row spreads few rows over the chip; from kLowRows on the rows
@@ -251,9 +261,6 @@ void launch_low(const HeadArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((k_low_tile<T, TERMS, 8>), grid, block, 0, s, a);
 }
 
-// A lane's address for tile rows past the end of the inputs' columns.
-__device__ uint4 k_zeros;
-
 // B_g u (before the row's power) of the four outputs from p on of one row per
 // lane, on the vector ALU.
 template <class T, int TERMS, int AHEAD>
@@ -262,7 +269,7 @@ __device__ __forceinline__ f32x4 low_of_row(const HeadArgs& a, int64_t n, int g,
   f32x4 low = {0, 0, 0, 0};
   if (g < 0 || p >= a.h.P) return low;
   const T* b = (const T*)a.h.b + ((int64_t)g * a.h.P + p) * R;
-  const uint16_t* ut = a.u + n * a.uk;
+  const uint16_t* ut = a.u + n * a.ul;
   const int last = a.h.P - 1 - p;  // rows of B past the last are not read
 #pragma unroll AHEAD
   for (int r = 0; r < R; r += 8) {
@@ -334,6 +341,7 @@ __device__ __forceinline__ void add_low(const HeadArgs& a, int64_t n0, PRow prow
   int kinds = 0;
   while (kinds <= kWaveMix && next() >= 0) ++kinds;
   if (kinds == 0) return;
+  const bool all_by_row = kinds > kWaveMix;
 
   float us[TM];
   if constexpr (!__is_same(T, Bf16)) {
@@ -346,24 +354,28 @@ __device__ __forceinline__ void add_low(const HeadArgs& a, int64_t n0, PRow prow
   }
   // this lane's rows (bit i: of block i) that are left for the vector ALU
   uint32_t by_row = 0;
-  start();
-#pragma unroll 1
-  for (int gg; (gg = next()) >= 0;) {
-    const T* B = (const T*)a.h.b + (int64_t)gg * P * R;
-    bool bad = kinds > kWaveMix;
-#pragma unroll 1
-    for (int r = quad * 8; r < R && !bad; r += 32)
+  const auto leave = [&](int gg) {
 #pragma unroll
-      for (int j = 0; j < TN; ++j) bad |= not_finite<T>(load8(B + (int64_t)min(prow(j, col), P - 1) * R + r, R - r));
-    if (!__any(bad)) continue;
+    for (int i = 0; i < TM; ++i) by_row |= (all_by_row ? g[i] >= 0 : g[i] == gg) << i;
+  };
+  const auto usable = [&](int gg) {  // whether an adapter's weights for these outputs are finite
+    bool bad = false;
+#pragma unroll 1
+    for (int r = quad * 8; r < R; r += 32)
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      by_row |= (g[i] == gg) << i;
-      g[i] = g[i] == gg ? -1 : g[i];
-    }
-  }
+      for (int j = 0; j < TN; ++j)
+        bad |= not_finite<T>(load8((const T*)a.h.b + ((int64_t)gg * P + min(prow(j, col), P - 1)) * R + r, R - r));
+    if (!__any(bad)) return true;
+    leave(gg);
+    return false;
+  };
   start();
-  int gg = next();
+  int gg = -1;
+  if (all_by_row)
+    leave(-1);
+  else
+    do gg = next();
+    while (gg >= 0 && per > 4 && !usable(gg));
 #pragma unroll 1
   for (int kk = 0; gg >= 0;) {
     const int c = kk + quad, r = (c % per) * 8;
@@ -377,8 +389,19 @@ __device__ __forceinline__ void add_low(const HeadArgs& a, int64_t n0, PRow prow
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
       const int64_t n = n0 + i * 16 + col;
-      u[i] = *(const uint4*)(a.u + (n < a.N ? n : a.N - 1) * a.uk + min(c, chunks - 1) * 8);
+      u[i] = *(const uint4*)(a.u + (n < a.N ? n : a.N - 1) * a.ul + min(c, chunks - 1) * 8);
       if (c >= chunks || g[i] != gg) u[i] = make_uint4(0, 0, 0, 0);
+    }
+    if (per <= 4 && kk == 0) {  // (all of the adapter's columns are here)
+      bool bad = false;
+#pragma unroll
+      for (int j = 0; j < TN; ++j) bad |= not_finite<T>(b[j]);
+      if (__any(bad)) {
+        leave(gg);
+        kk = chunks;
+#pragma unroll
+        for (int j = 0; j < TN; ++j) b[j] = make_uint4(0, 0, 0, 0);
+      }
     }
 #pragma unroll
     for (int i = 0; i < TM; ++i)
@@ -387,7 +410,8 @@ __device__ __forceinline__ void add_low(const HeadArgs& a, int64_t n0, PRow prow
     kk += 4;
     if (kk >= chunks) {
       kk = 0;
-      gg = next();
+      do gg = next();
+      while (gg >= 0 && per > 4 && !usable(gg));
     }
   }
   if (__any(by_row != 0)) {
@@ -432,9 +456,9 @@ __device__ __forceinline__ void store_out(O* out, const Few<O, N>& v, int n) {
 // outputs of 32 bits took 1250 us, of 16 bits 962, and take 895 and 865.  Outputs
 // larger than the caches go past them (`stream`: 864 and 856 us).
 template <class T, class O, int TM, int TN>
-__device__ __forceinline__ void finish_tile(const HeadArgs& a, int64_t n0, int p0, f32x4* mine, f32x4 (&acc)[TM][TN]) {
+__device__ __forceinline__ void finish_tile(const HeadArgs& a, int64_t n0, int p0, f32x4* mine, bool low, f32x4 (&acc)[TM][TN]) {
   const int lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4, P = a.h.P;
-  if (a.adapter) add_low<T, kTerms<T, O>>(a, n0, [&](int j, int i) { return p0 + j * 16 + i; }, mine, acc);
+  if (low) add_low<T, kTerms<T, O>>(a, n0, [&](int j, int i) { return p0 + j * 16 + i; }, mine, acc);
   constexpr int kCols = TN * 16, kEach = 16 / sizeof(O);
   constexpr int kLine = kCols + kEach;  // a row in LDS, padded against bank conflicts
   constexpr int kLanes = kCols / kEach, kRows = 64 / kLanes;  // lanes of a row, rows of a store
@@ -472,13 +496,12 @@ __device__ __forceinline__ void finish_tile(const HeadArgs& a, int64_t n0, int p
   }
 }
 
-// 16 bytes per lane from global memory straight to LDS at `to` + 16 * lane (the
-// same `to` in every lane).  The compiler does not see this load (its builtin
-// makes every LDS read wait for all of them): the data is there after
-// loads_left() and a barrier.
-__device__ __forceinline__ void load_to_lds(const void* from, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, off" ::"v"(from),
-               "s"(__builtin_amdgcn_readfirstlane(to))
+// 16 bytes per lane from `base` (the same in every lane) + the lane's offset
+// straight to LDS at `to` + 16 * lane (the same `to` in every lane).  The compiler
+// does not see this load (its builtin makes every LDS read wait for all of them):
+// the data is there after loads_left() and a barrier.
+__device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(to)
                : "memory");
 }
 // Waits until at most N of this wavefront's loads are on their way (they arrive in order).
@@ -559,12 +582,11 @@ __global__ void __launch_bounds__(512) k_rows(HeadArgs a) {
   store_out((O*)a.out + fi * a.out_ld + fp, out, P - fp);
 }
 
-// Where chunk c (16 bytes) of tile row r lies in LDS: at c ^ swizzle in rows of BK
-// columns, so that the 16 rows of an operand read fall on different banks.
-template <int BK>
-__device__ __forceinline__ int swizzle(int row) {
-  return BK == 32 ? (row >> 2) & 3 : (row >> 1) & 7;
-}
+constexpr int kStepK = 64;  // columns of a step: 128 bytes of a row
+
+// Where chunk c (16 bytes) of tile row r lies in LDS: at c ^ swizzle, so that the
+// 16 rows of an operand read fall on different banks.
+__device__ __forceinline__ int swizzle(int row) { return (row >> 1) & 7; }
 
 // The tile of this workgroup.  Workgroups go round the eight XCDs, each with an
 // L2 of its own: an XCD takes a run of tiles, in groups of kGroup rows of tiles
@@ -579,12 +601,14 @@ __device__ __forceinline__ void my_tile(uint32_t rows, uint32_t cols, uint32_t& 
   row = first + in % height;
 }
 
-// BM rows and BN outputs per workgroup of WM x WN wavefronts; steps of BK columns,
-// S of them in LDS: while one is multiplied the next S - 1 are on their way.
-template <class T, class O, int BM, int BN, int WM, int WN, int BK, int S, bool ALIGNED>
-__global__ void __launch_bounds__(64 * WM * WN, 2) k_project(HeadArgs a, uint32_t row_tiles, uint32_t col_tiles) {
+// BM rows and BN outputs per workgroup of WM x WN wavefronts.  Two steps of kStepK
+// columns are in LDS.  A step is two halves: while one is multiplied, the next
+// half's operands are read into registers; between the halves of a step every
+// wavefront has read all of it, and the step after the next starts into its place.
+template <class T, class O, int BM, int BN, int WM, int WN, bool ALIGNED>
+__global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2) k_project(HeadArgs a, uint32_t row_tiles, uint32_t col_tiles) {
   constexpr int kWaves_ = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
-  constexpr int kRowBytes = BK * 2, kChunks = BK / 8, kPartRows = 64 / kChunks;
+  constexpr int kRowBytes = kStepK * 2, kChunks = kStepK / 8, kPartRows = 64 / kChunks;
   constexpr int kTile = (BM + BN) * kRowBytes;
   constexpr int kParts = kTile / 1024 / kWaves_;  // loads of a wavefront per step
   static_assert((BM / kPartRows) % kWaves_ == 0 && (BN / kPartRows) % kWaves_ == 0, "");
@@ -596,78 +620,136 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_project(HeadArgs a, uint32_
   const int p0 = (int)col_tile * BN;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
 
-  // this lane's source rows: parts of BM rows of x, then of BN rows of W
-  const T* src[kParts];
-  int col[kParts];
+  // a step's loads of this wavefront: parts of BM rows of x, then of BN rows of W;
+  // the lane's offset (bytes) in its row's part of the inputs
+  const T* xt = (const T*)a.x + n0 * a.x_ld;
+  const T* wt = (const T*)a.h.weight + (int64_t)p0 * a.h.weight_ld;
+  uint32_t from[kParts];
+  constexpr auto is_w = [](int i) { return i * kWaves_ * kPartRows >= BM; };
 #pragma unroll
   for (int i = 0; i < kParts; ++i) {
-    const bool w = i * kWaves_ * kPartRows >= BM;
-    const int row = (i * kWaves_ + wave) * kPartRows - (w ? BM : 0) + lane / kChunks;
-    col[i] = ((lane % kChunks) ^ swizzle<BK>(row)) * 8;
-    src[i] = w ? (const T*)a.h.weight + (int64_t)min(p0 + row, P - 1) * a.h.weight_ld
-               : (const T*)a.x + min(n0 + row, a.N - 1) * a.x_ld;
+    const int row = (i * kWaves_ + wave) * kPartRows - (is_w(i) ? BM : 0) + lane / kChunks;
+    const int64_t at = is_w(i) ? min(row, P - 1 - p0) * a.h.weight_ld : min<int64_t>(row, a.N - 1 - n0) * a.x_ld;
+    from[i] = (uint32_t)((at + ((lane % kChunks) ^ swizzle(row)) * 8) * 2);
   }
-  auto stage = [&](int k0, char* to) {
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  const int full = ALIGNED ? D / kStepK * kStepK : 0;  // columns of whole steps, loaded straight to LDS
+  const int main = (D + kStepK - 1) / kStepK * kStepK;
+  const auto stage_x = [&](int k0, int step) {
+    if (k0 < full) {
 #pragma unroll
+      for (int i = 0; i < kParts; ++i)
+        load_to_lds((is_w(i) ? wt : xt) + k0, from[i], __builtin_amdgcn_readfirstlane(lds0 + step + (i * kWaves_ + wave) * 1024));
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < kParts; ++i) {
+        const int row = (i * kWaves_ + wave) * kPartRows + lane / kChunks, c = ((lane % kChunks) ^ swizzle(row)) * 8;
+        const T* r = row < BM ? xt + min<int64_t>(row, a.N - 1 - n0) * a.x_ld
+                              : wt + (int64_t)min(row - BM, P - 1 - p0) * a.h.weight_ld;
+        *(uint4*)(lds + step + (i * kWaves_ + wave) * 1024 + lane * 16) = load8(r + k0 + c, D - k0 - c);
+      }
+    }
+  };
+  stage_x(0, 0);
+
+  // Rows of one adapter: B_g u is a step (or a few) more, of u's terms and B's
+  // columns, whose loads are under way while W x is still multiplied.
+  int low = -1, steps = main;
+  bool mixed = false;
+  if (a.adapter) {
+    bool any = false, same = a.rp <= kStepK;
+    low = __builtin_amdgcn_readfirstlane(adapter_of(a, n0));
+#pragma unroll
+    for (int q = 0; q < BM; q += 64) {
+      const int64_t n = n0 + q + lane;
+      const int g = adapter_of(a, n);
+      any |= g >= 0;
+      same &= g == low || n >= a.N;
+      if (!__is_same(T, Bf16) && g >= 0) same &= a.us[n] == 1.0f;
+    }
+    if (__any(any)) {
+      mixed = !__all(same);
+      if (!mixed) steps += a.ul;
+    }
+  }
+  const auto stage = [&](int k0, int step) {
+    if (k0 < main) return stage_x(k0, step);
+    const int c0 = (k0 - main) / 8, per = a.rp / 8, chunks = a.uk / 8, R = a.h.rank;
+    const uint16_t* ut = a.u + n0 * a.ul + (k0 - main);
+    const T* bt = (const T*)a.h.b + ((int64_t)low * P + p0) * R;
+#pragma unroll 1
     for (int i = 0; i < kParts; ++i) {
-      char* dst = to + (i * kWaves_ + wave) * 1024;
-      const int k = k0 + col[i];
-      if constexpr (ALIGNED) {
-        const T* p = k < D ? src[i] + k : (const T*)&k_zeros;
-        load_to_lds(p, (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)dst);
+      const int row = (i * kWaves_ + wave) * kPartRows + lane / kChunks, c = (lane % kChunks) ^ swizzle(row);
+      const uint32_t to = __builtin_amdgcn_readfirstlane(lds0 + step + (i * kWaves_ + wave) * 1024);
+      if (is_w(i)) {
+        const int r = c0 + c < chunks ? (c0 + c) % per * 8 : 0;  // (past the terms, u is zero)
+        const T* b = bt + (int64_t)min(row - BM, P - 1 - p0) * R + r;
+        if (a.b16)
+          load_to_lds(bt, (uint32_t)((b - bt) * 2), to);
+        else
+          *(uint4*)(lds + step + (i * kWaves_ + wave) * 1024 + lane * 16) = load8(b, R - r);
       } else {
-        *(uint4*)(dst + lane * 16) = load8(src[i] + k, D - k);
+        load_to_lds(ut, (uint32_t)((min<int64_t>(row, a.N - 1 - n0) * a.ul + c * 8) * 2), to);
       }
     }
   };
 
   f32x4 acc[TM][TN] = {};
   const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
-  for (int k = 0; k < S - 1; ++k)
-    if (k * BK < D) stage(k * BK, lds + k * kTile);
-  int slot = 0;
-  for (int k0 = 0; k0 < D; k0 += BK) {
-    // this step is there when at most the loads of the S - 2 after it are on their way
-    if (S > 2 && k0 + (S - 2) * BK < D)
-      loads_left<(S - 2) * kParts>();
-    else
-      loads_left<0>();
-    __syncthreads();  // for every wavefront; and the step before has been read
-    const int ahead = k0 + (S - 1) * BK, to = slot == 0 ? S - 1 : slot - 1;
-    if (ahead < D) stage(ahead, lds + to * kTile);
-    const char* xs = lds + slot * kTile;
-    const char* ws = xs + BM * kRowBytes;
+  struct Operands {
+    uint4 w[TN], x[TM];
+  } even, odd;
+  const int read_at = (lane & 15) * kRowBytes + (((lane >> 4) ^ swizzle(lane & 15)) << 4);
+  const auto read = [&](int step, int half, Operands& o) {
+    const int at = step + (read_at ^ (half << 6));
 #pragma unroll
-    for (int ks = 0; ks < BK / 32; ++ks) {
-      const int c = ks * 4 + (lane >> 4);
-      uint4 w[TN], x[TM];
+    for (int j = 0; j < TN; ++j) o.w[j] = *(const uint4*)(lds + at + (BM + wn + j * 16) * kRowBytes);
 #pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        const int r = wn + j * 16 + (lane & 15);
-        w[j] = *(const uint4*)(ws + r * kRowBytes + ((c ^ swizzle<BK>(r)) << 4));
-      }
+    for (int i = 0; i < TM; ++i) o.x[i] = *(const uint4*)(lds + at + (wm + i * 16) * kRowBytes);
+  };
+  const auto multiply = [&](const Operands& o) {
 #pragma unroll
-      for (int i = 0; i < TM; ++i) {
-        const int r = wm + i * 16 + (lane & 15);
-        x[i] = *(const uint4*)(xs + r * kRowBytes + ((c ^ swizzle<BK>(r)) << 4));
-      }
+    for (int i = 0; i < TM; ++i)
 #pragma unroll
-      for (int i = 0; i < TM; ++i)
+      for (int j = 0; j < TN; ++j) acc[i][j] = mfma16(o.w[j], o.x[i], acc[i][j], T{});
+    // an operand read between every few products
 #pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = mfma16(w[j], x[i], acc[i][j], T{});
+    for (int i = 0; i < TM + TN; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, TM * TN / (TM + TN), 0);
     }
-    slot = slot == S - 1 ? 0 : slot + 1;
+  };
+  int now = 0, next = kTile;
+  if (kStepK < steps) {
+    stage(kStepK, next);
+    kStepK < full ? loads_left<kParts>() : loads_left<0>();
+  } else {
+    loads_left<0>();
   }
-  __syncthreads();  // LDS is free
-  finish_tile<T, O>(a, n0 + wm, p0 + wn, (f32x4*)lds + wave * (TM * TN < 16 ? TM * TN : 16) * 64, acc);
+  __syncthreads();
+  read(now, 0, even);
+  // (One copy of the products and no branch around them: with more the compiler
+  // holds the accumulators twice.  The last step's reads of a next one are of no use.)
+  for (int k0 = 0; k0 < steps; k0 += kStepK) {
+    read(now, 1, odd);
+    multiply(even);
+    loads_left<0>();
+    __syncthreads();  // this step has been read, the next one is there
+    if (k0 + 2 * kStepK < steps) stage(k0 + 2 * kStepK, now);
+    read(next, 0, even);
+    multiply(odd);
+    now = next;
+    next = kTile - next;
+  }
+  finish_tile<T, O>(a, n0 + wm, p0 + wn, (f32x4*)lds + wave * (TM * TN < 16 ? TM * TN : 16) * 64, mixed, acc);
 }
 
-template <class T, class O, int BM, int BN, int WM, int WN, int BK, int S, bool ALIGNED>
+template <class T, class O, int BM, int BN, int WM, int WN, bool ALIGNED>
 void launch_tiles(const HeadArgs& a, hipStream_t s) {
   const uint32_t rows = (uint32_t)((a.N + BM - 1) / BM), cols = ((uint32_t)a.h.P + BN - 1) / BN;
-  auto* k = k_project<T, O, BM, BN, WM, WN, BK, S, ALIGNED>;
+  auto* k = k_project<T, O, BM, BN, WM, WN, ALIGNED>;
   constexpr int each = BM * BN / 256 / (WM * WN), low = (each < 16 ? each : 16) * 1024 * WM * WN;  // (add_low's)
-  constexpr int stages = S * (BM + BN) * BK * 2;
+  constexpr int stages = 2 * (BM + BN) * kStepK * 2;
   constexpr int bytes = stages > low ? stages : low;
   if (bytes > 65536) (void)hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
   hipLaunchKernelGGL(k, dim3(rows * cols), dim3(64 * WM * WN), bytes, s, a, rows, cols);
@@ -678,9 +760,12 @@ void launch_project(HeadArgs a, hipStream_t s) {
   if (a.adapter) {
     constexpr int terms = kTerms<T, O>;
     a.uk = terms * a.rp;
+    a.ul = (a.uk + kStepK - 1) / kStepK * kStepK;
+    a.b16 = a.h.rank % 8 == 0 && !((uintptr_t)a.h.b & 15);
     launch_low<T, terms>(a, s);
   }
-  const bool aligned = a.h.D % 8 == 0 && a.x_ld % 8 == 0 && a.h.weight_ld % 8 == 0 && !((uintptr_t)a.x & 15) &&
+  // (the loads straight to LDS: 16 bytes, 32-bit offsets within a tile)
+  const bool aligned = a.h.D % 8 == 0 && a.x_ld < (1 << 22) && a.h.weight_ld < (1 << 22) && a.x_ld % 8 == 0 && a.h.weight_ld % 8 == 0 && !((uintptr_t)a.x & 15) &&
                        !((uintptr_t)a.h.weight & 15);
   a.stream = (uint64_t)a.N * a.h.P * sizeof(O) >= (256u << 20);
   const auto tiles = [&](int64_t m, int64_t n) { return ((a.N + m - 1) / m) * ((a.h.P + n - 1) / n); };
@@ -692,27 +777,13 @@ void launch_project(HeadArgs a, hipStream_t s) {
   else if (a.N <= 64)
     hipLaunchKernelGGL((k_rows<T, O, 4>), outs, block, 0, s, a);
   else if (!aligned)
-    launch_tiles<T, O, 64, 64, 2, 2, 64, 2, false>(a, s);
-  else {
-    static const int v = getenv("WD_TILE") ? atoi(getenv("WD_TILE")) : -1;
-    if constexpr (__is_same(T, Bf16)) {
-    switch (v) {
-      case 0: return launch_tiles<T, O, 256, 256, 2, 4, 64, 2, true>(a, s);
-      case 1: return launch_tiles<T, O, 256, 256, 2, 4, 32, 4, true>(a, s);
-      case 2: return launch_tiles<T, O, 128, 256, 2, 2, 32, 3, true>(a, s);
-      case 3: return launch_tiles<T, O, 256, 128, 2, 2, 32, 3, true>(a, s);
-      case 4: return launch_tiles<T, O, 128, 128, 2, 2, 64, 2, true>(a, s);
-      case 5: return launch_tiles<T, O, 128, 128, 2, 2, 32, 4, true>(a, s);
-      case 6: return launch_tiles<T, O, 256, 256, 2, 4, 32, 3, true>(a, s);
-      case 7: return launch_tiles<T, O, 128, 256, 2, 4, 32, 3, true>(a, s);
-    }}
-    if (tiles(256, 256) >= 256)
-    launch_tiles<T, O, 256, 256, 2, 4, 64, 2, true>(a, s);
-  else if (tiles(128, 128) >= 256)
-    launch_tiles<T, O, 128, 128, 2, 2, 64, 2, true>(a, s);
+    launch_tiles<T, O, 64, 64, 2, 2, false>(a, s);
+  else if (tiles(256, 256) >= 192)
+    launch_tiles<T, O, 256, 256, 2, 4, true>(a, s);
+  else if (tiles(128, 128) >= 192)
+    launch_tiles<T, O, 128, 128, 2, 2, true>(a, s);
   else
-    launch_tiles<T, O, 64, 64, 2, 2, 64, 2, true>(a, s);
-  }
+    launch_tiles<T, O, 64, 64, 2, 2, true>(a, s);
 }
 
 }  // namespace wd
@@ -739,7 +810,7 @@ static wd_status check_head(const wd_head* h) {
 
 // Workspace: the terms of u (at most three), then the rows' powers of two.
 static int padded_rank(const wd_head* h) { return (h->rank + 7) / 8 * 8; }
-static size_t u_bytes(const wd_head* h, int64_t N) { return align_up((uint64_t)N * 3 * padded_rank(h) * 2, 256); }
+static size_t u_bytes(const wd_head* h, int64_t N) { return align_up((uint64_t)N * ((3 * padded_rank(h) + 63) / 64 * 64) * 2, 256); }
 static size_t project_bytes(const wd_head* h, int64_t N) {
   return h->n_adapters > 0 ? u_bytes(h, N) + align_up((uint64_t)N * sizeof(float), 256) : 0;
 }
@@ -771,7 +842,7 @@ extern "C" wd_status wd_project(const wd_head* h, const void* x, int64_t x_ld, i
   if (((uint64_t)N + 63) / 64 * (((uint64_t)h->P + 63) / 64) > INT32_MAX)
     return fail(WD_EINVAL, "project: too many rows for one call");
   HeadArgs a{*h, x, x_ld, N, adapter, out, out_ld, (uint16_t*)ws,
-             adapter ? (float*)((char*)ws + u_bytes(h, N)) : nullptr, adapter ? padded_rank(h) : 0, 0, false};
+             adapter ? (float*)((char*)ws + u_bytes(h, N)) : nullptr, adapter ? padded_rank(h) : 0, 0, 0, false, false};
   hipStream_t s = (hipStream_t)stream;
   if (h->type == WD_F16)
     out_type == WD_F32 ? launch_project<Half, F32>(a, s) : launch_project<Half, Half>(a, s);
