@@ -306,23 +306,20 @@ __device__ __forceinline__ bool not_finite(uint4 v) {
 constexpr int kWaveMix = 16;
 
 // B_g u for the wavefront's rows n0.., added to acc; prow(j, i) is the output of
-// row i of operand block j, `mine` LDS of the wavefront's own, of 16 lane vectors
-// or as many as it has accumulators.  A row's terms are zero for the other
+// row i of operand block j, `ids` the rows' adapters, `mine` LDS of the
+// wavefront's own, of 16 lane vectors or as many as it has accumulators.  A row's terms are zero for the other
 // rows' adapters, so that a product with them adds nothing; where an adapter's
 // weights are not all finite (and zero times them would be a NaN), its rows
 // take the vector ALU.
 template <class T, int TERMS, int TM, int TN, class PRow>
-__device__ __forceinline__ void add_low(const HeadArgs& a, int64_t n0, PRow prow, f32x4* mine, f32x4 (&acc)[TM][TN]) {
+__device__ __forceinline__ void add_low(const HeadArgs& a, int64_t n0, const int* ids, PRow prow, f32x4* mine,
+                                        f32x4 (&acc)[TM][TN]) {
   const int lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
   const int R = a.h.rank, P = a.h.P;
   const int chunks = a.uk / 8, per = a.rp / 8;
   int g[TM];
 #pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    const int64_t n = n0 + i * 16 + col;
-    const int v = a.adapter[n < a.N ? n : a.N - 1];
-    g[i] = n < a.N && v >= 0 && v < a.h.n_adapters ? v : -1;
-  }
+  for (int i = 0; i < TM; ++i) g[i] = ids[i * 16 + col];
   uint64_t todo[TM];
   const auto start = [&]() {
 #pragma unroll
@@ -378,19 +375,15 @@ __device__ __forceinline__ void add_low(const HeadArgs& a, int64_t n0, PRow prow
     while (gg >= 0 && per > 4 && !usable(gg));
 #pragma unroll 1
   for (int kk = 0; gg >= 0;) {
-    const int c = kk + quad, r = (c % per) * 8;
+    const int c = kk + quad, r = c < chunks ? (c % per) * 8 : 0;
     const T* B = (const T*)a.h.b + (int64_t)gg * P * R + r;
     uint4 b[TN], u[TM];
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      b[j] = load8(B + (int64_t)min(prow(j, col), P - 1) * R, R - r);
-      if (c >= chunks) b[j] = make_uint4(0, 0, 0, 0);
-    }
+    for (int j = 0; j < TN; ++j) b[j] = load8(B + (int64_t)min(prow(j, col), P - 1) * R, R - r);
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
       const int64_t n = n0 + i * 16 + col;
-      u[i] = *(const uint4*)(a.u + (n < a.N ? n : a.N - 1) * a.ul + min(c, chunks - 1) * 8);
-      if (c >= chunks || g[i] != gg) u[i] = make_uint4(0, 0, 0, 0);
+      u[i] = *(const uint4*)(a.u + (n < a.N ? n : a.N - 1) * a.ul + c * 8);
     }
     if (per <= 4 && kk == 0) {  // (all of the adapter's columns are here)
       bool bad = false;
@@ -399,10 +392,15 @@ __device__ __forceinline__ void add_low(const HeadArgs& a, int64_t n0, PRow prow
       if (__any(bad)) {
         leave(gg);
         kk = chunks;
-#pragma unroll
-        for (int j = 0; j < TN; ++j) b[j] = make_uint4(0, 0, 0, 0);
       }
     }
+    const bool used = kk + quad < chunks;
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+      if (!used) b[j] = make_uint4(0, 0, 0, 0);
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+      if (!used || g[i] != gg) u[i] = make_uint4(0, 0, 0, 0);
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
@@ -422,7 +420,7 @@ __device__ __forceinline__ void add_low(const HeadArgs& a, int64_t n0, PRow prow
 #pragma unroll 1
       for (int ij = h; ij < h + kHalf; ++ij) {
         const int64_t n = n0 + (ij / TN) * 16 + col;
-        const int gi = by_row >> (ij / TN) & 1 ? adapter_of(a, n) : -1;
+        const int gi = by_row >> (ij / TN) & 1 ? ids[(ij / TN) * 16 + col] : -1;
         mine[(ij - h) * 64 + lane] = low_of_row<T, TERMS, 1>(a, n, gi, prow(ij % TN, quad * 4));
       }
 #pragma unroll
@@ -456,9 +454,9 @@ __device__ __forceinline__ void store_out(O* out, const Few<O, N>& v, int n) {
 // outputs of 32 bits took 1250 us, of 16 bits 962, and take 895 and 865.  Outputs
 // larger than the caches go past them (`stream`: 864 and 856 us).
 template <class T, class O, int TM, int TN>
-__device__ __forceinline__ void finish_tile(const HeadArgs& a, int64_t n0, int p0, f32x4* mine, bool low, f32x4 (&acc)[TM][TN]) {
+__device__ __forceinline__ void finish_tile(const HeadArgs& a, int64_t n0, int p0, f32x4* mine, const int* ids, f32x4 (&acc)[TM][TN]) {
   const int lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4, P = a.h.P;
-  if (low) add_low<T, kTerms<T, O>>(a, n0, [&](int j, int i) { return p0 + j * 16 + i; }, mine, acc);
+  if (ids) add_low<T, kTerms<T, O>>(a, n0, ids, [&](int j, int i) { return p0 + j * 16 + i; }, mine, acc);
   constexpr int kCols = TN * 16, kEach = 16 / sizeof(O);
   constexpr int kLine = kCols + kEach;  // a row in LDS, padded against bank conflicts
   constexpr int kLanes = kCols / kEach, kRows = 64 / kLanes;  // lanes of a row, rows of a store
@@ -632,6 +630,7 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
     const int64_t at = is_w(i) ? min(row, P - 1 - p0) * a.h.weight_ld : min<int64_t>(row, a.N - 1 - n0) * a.x_ld;
     from[i] = (uint32_t)((at + ((lane % kChunks) ^ swizzle(row)) * 8) * 2);
   }
+  int* ids = (int*)(lds + 2 * kTile);  // the rows' adapters
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
   const int full = ALIGNED ? D / kStepK * kStepK : 0;  // columns of whole steps, loaded straight to LDS
   const int main = (D + kStepK - 1) / kStepK * kStepK;
@@ -663,6 +662,7 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
     for (int q = 0; q < BM; q += 64) {
       const int64_t n = n0 + q + lane;
       const int g = adapter_of(a, n);
+      if (wave == 0) ids[q + lane] = g;
       any |= g >= 0;
       same &= g == low || n >= a.N;
       if (!__is_same(T, Bf16) && g >= 0) same &= a.us[n] == 1.0f;
@@ -741,7 +741,7 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
     now = next;
     next = kTile - next;
   }
-  finish_tile<T, O>(a, n0 + wm, p0 + wn, (f32x4*)lds + wave * (TM * TN < 16 ? TM * TN : 16) * 64, mixed, acc);
+  finish_tile<T, O>(a, n0 + wm, p0 + wn, (f32x4*)lds + wave * (TM * TN < 16 ? TM * TN : 16) * 64, mixed ? ids + wm : nullptr, acc);
 }
 
 template <class T, class O, int BM, int BN, int WM, int WN, bool ALIGNED>
@@ -750,7 +750,8 @@ void launch_tiles(const HeadArgs& a, hipStream_t s) {
   auto* k = k_project<T, O, BM, BN, WM, WN, ALIGNED>;
   constexpr int each = BM * BN / 256 / (WM * WN), low = (each < 16 ? each : 16) * 1024 * WM * WN;  // (add_low's)
   constexpr int stages = 2 * (BM + BN) * kStepK * 2;
-  constexpr int bytes = stages > low ? stages : low;
+  static_assert(low <= stages, "");
+  constexpr int bytes = stages + BM * 4;
   if (bytes > 65536) (void)hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
   hipLaunchKernelGGL(k, dim3(rows * cols), dim3(64 * WM * WN), bytes, s, a, rows, cols);
 }
@@ -778,7 +779,7 @@ void launch_project(HeadArgs a, hipStream_t s) {
     hipLaunchKernelGGL((k_rows<T, O, 4>), outs, block, 0, s, a);
   else if (!aligned)
     launch_tiles<T, O, 64, 64, 2, 2, false>(a, s);
-  else if (tiles(256, 256) >= 192)
+  else if (tiles(256, 256) >= 256)
     launch_tiles<T, O, 256, 256, 2, 4, true>(a, s);
   else if (tiles(128, 128) >= 192)
     launch_tiles<T, O, 128, 128, 2, 2, true>(a, s);
