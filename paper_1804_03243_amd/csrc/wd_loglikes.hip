@@ -1,13 +1,14 @@
 // Logits to log-likelihoods: penalties for labels a request has had, its
 // biases, its row's label mask, log-softmax, log priors and the acoustic scale.
 //
-// A row is swept in chunks of labels.  A chunk's penalties need the count of
-// each label in the request's history: the history is scattered into a
-// table of the chunk's labels in LDS (integer atomics: the order of the entries
-// does not matter), and the last bias entry of a label is the maximum of the
-// entries' positions in the same table.  The log of the sum of exponentials is
-// kept as a running maximum m and a running sum s of exp(z - m) per thread, in
-// 32 bits; rows of more than one chunk are swept twice.
+// A workgroup holds a row, or a slice of one, in registers.  Its penalties need the
+// count of each label in the request's history: the history is scattered into a
+// table of the slice's labels in LDS (integer atomics: the order of the entries does
+// not matter), and the last bias entry of a label is the maximum of the entries'
+// positions in a second table.  Then m = max z and s = sum of exp(z - m) over the
+// workgroup, in 32 bits, and y = (z - m) - log s.  Bound by memory where rows are
+// many (48 thousand rows of 6000 labels of 32 bits: 600 us, 5.1 TB/s, what a copy
+// reaches), by the chain of reads request, offsets, list where they are few.
 #include <algorithm>
 #include <cmath>
 
@@ -16,153 +17,258 @@
 
 namespace wd {
 
-constexpr int kScoreThreads = 256;
-constexpr int kScoreEach = 32;                       // labels of a chunk per thread
-constexpr int kScoreChunk = kScoreThreads * kScoreEach;
-
 struct ScoreArgs {
   wd_loglikes_args a;
+  float2* part;     // [N][slices] maximum and sum of each slice of a row
+  uint32_t slices;  // slices of a row
+  bool stream;      // outputs past the caches
 };
 
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef f32x4 __attribute__((aligned(4))) f32x4_any;
+
 __device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896340736f); }
+
+// A finite number to subtract from logits of maximum m before their exponentials
+// are taken: with nothing above -inf, exp(z - 0) = 0 and a NaN stays one.
+__device__ __forceinline__ float shift_of(float m) { return m == -INFINITY ? 0.0f : m; }
 
 struct RowSpan {
   int64_t b, e;
 };
-
 __device__ __forceinline__ RowSpan span_of(const int64_t* off, int q, int64_t n) {
   return {max(off[q], (int64_t)0), min(off[q + 1], n)};
 }
 
-// The adjusted logits of the chunk's labels c0 + (j * threads + thread) * 4 + i
-// in z[j * 4 + i]; -inf past the row.
+// Four consecutive elements of a row of n, those past its end as `fill`.
 template <class T>
-__device__ __forceinline__ void score_chunk(const wd_loglikes_args& a, const T* row, int q, const uint32_t* mask, int c0,
-                                            uint32_t* table, float* z) {
-  const int V = a.V;
+__device__ __forceinline__ Few<T, 4> load4(const T* p, int n, T fill) {
+  if (n >= 4) return *(const Few<T, 4>*)p;
+  Few<T, 4> v;
 #pragma unroll
-  for (int j = 0; j < kScoreEach / 4; ++j) {
-    const int v = c0 + (j * kScoreThreads + (int)threadIdx.x) * 4;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) z[j * 4 + i] = v + i < V ? row[v + i].f() : -INFINITY;
+  for (int i = 0; i < 4; ++i) v.v[i] = i < n ? p[i] : fill;
+  return v;
+}
+
+// What a workgroup does with its slice of a row.
+enum ScorePhase {
+  kWhole,  // the slice is the row: normalise and write
+  kStats,  // its maximum and sum, to `part`
+  kWrite   // write, with the sums of all slices from `part`
+};
+
+// A workgroup per slice of THREADS * EACH labels, a thread's labels in registers:
+// (j * THREADS + thread) * 4 + i of the slice is z[j * 4 + i].
+template <class T, int THREADS, int EACH, int TABLES, ScorePhase PHASE>
+__global__ void __launch_bounds__(THREADS) k_loglikes(ScoreArgs args) {
+  constexpr int kSlice = THREADS * EACH, kVecs = EACH / 4, kWavesHere = THREADS / 64;
+  const wd_loglikes_args& a = args.a;
+  extern __shared__ uint32_t table[];  // [TABLES][kSlice], where there are histories or biases
+  __shared__ float red[2][kWavesHere];
+  const int64_t n = PHASE == kWhole ? blockIdx.x : blockIdx.x / args.slices;
+  const int c0 = PHASE == kWhole ? 0 : (int)(blockIdx.x % args.slices) * kSlice;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int64_t to = n;
+  if (a.out_row) {
+    to = a.out_row[n];
+    if (to < 0 || to >= a.out_rows) return;
   }
-  if (q >= 0 && a.hist_off) {
-    const RowSpan h = span_of(a.hist_off, q, a.n_hist);
-    if (h.b < h.e) {  // (the same for the whole workgroup)
-      for (int i = threadIdx.x; i < kScoreChunk; i += kScoreThreads) table[i] = 0;
-      __syncthreads();
-      for (int64_t i = h.b + threadIdx.x; i < h.e; i += kScoreThreads) {
-        const int l = a.hist[i];
-        if (l >= c0 && l < V && l - c0 < kScoreChunk) atomicAdd(&table[l - c0], 1u);
-      }
-      __syncthreads();
-      const float rho = a.repetition ? a.repetition[q] : 1.0f;
-      const float pres = a.presence ? a.presence[q] : 0.0f, freq = a.frequency ? a.frequency[q] : 0.0f;
+  int q = -1;
+  if (a.n_requests > 0) {
+    const int64_t r = a.request ? (int64_t)a.request[n] : n;
+    q = r >= 0 && r < a.n_requests ? (int)r : -1;
+  }
+  RowSpan hist{0, 0}, bias{0, 0};
+  if (q >= 0 && a.hist_off) hist = span_of(a.hist_off, q, a.n_hist);
+  if (q >= 0 && a.bias_off) bias = span_of(a.bias_off, q, a.n_bias);
+  const int V = a.V, at = c0 + (int)threadIdx.x * 4;
+  constexpr int kStep = THREADS * 4;
+  const T* row = (const T*)a.logits + n * a.ld;
+  Few<T, 4> raw[kVecs];
 #pragma unroll
-      for (int j = 0; j < kScoreEach; ++j) {
-        const uint32_t c = table[((j >> 2) * kScoreThreads + (int)threadIdx.x) * 4 + (j & 3)];
-        if (c) z[j] = (z[j] > 0.0f ? z[j] / rho : z[j] * rho) - (pres + freq * (float)c);
+  for (int j = 0; j < kVecs; ++j) raw[j] = load4(row + at + j * kStep, V - at - j * kStep, T::of(-INFINITY));
+
+  uint32_t keep[kVecs];  // bits of the mask
+  const uint32_t* mask = nullptr;
+  if (a.mask) {
+    const int64_t r = a.mask_of ? (int64_t)a.mask_of[n] : n;
+    if (r >= 0 && r < a.n_masks) mask = a.mask + r * a.mask_ld;
+  }
+#pragma unroll
+  for (int j = 0; j < kVecs; ++j) {
+    const int v = at + j * kStep;
+    keep[j] = mask && v < V ? mask[v >> 5] >> (v & 31) : 15u;
+  }
+
+  float z[EACH];
+#pragma unroll
+  for (int j = 0; j < EACH; ++j) z[j] = raw[j / 4].v[j & 3].f();
+  const bool has_hist = hist.b < hist.e, has_bias = bias.b < bias.e;  // (the same for the whole workgroup)
+  // tables of the slice's labels: counts in the history, positions in the biases
+  uint32_t* counts = table;
+  uint32_t* places = TABLES == 2 && has_hist ? table + kSlice : table;
+  const auto clear = [&](uint32_t* t) {
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) ((uint4*)t)[j * THREADS + threadIdx.x] = make_uint4(0, 0, 0, 0);
+  };
+  const auto count = [&]() {
+#pragma unroll 4
+    for (int64_t i = hist.b + threadIdx.x; i < hist.e; i += THREADS) {
+      const int l = a.hist[i];
+      if (l < V && (uint32_t)(l - c0) < (uint32_t)kSlice) atomicAdd(&counts[l - c0], 1u);
+    }
+  };
+  const auto place = [&]() {
+#pragma unroll 4
+    for (int64_t i = bias.b + threadIdx.x; i < bias.e; i += THREADS) {
+      const int l = a.bias_id[i];
+      if (l < V && (uint32_t)(l - c0) < (uint32_t)kSlice) atomicMax(&places[l - c0], (uint32_t)(i - bias.b) + 1u);
+    }
+  };
+  if (has_hist || (has_bias && TABLES == 2)) {
+    const float rho = has_hist && a.repetition ? a.repetition[q] : 1.0f;
+    const float pres = has_hist && a.presence ? a.presence[q] : 0.0f, freq = has_hist && a.frequency ? a.frequency[q] : 0.0f;
+    if (has_hist) clear(counts);
+    if (has_bias && TABLES == 2) clear(places);
+    __syncthreads();
+    count();
+    if (TABLES == 2) place();
+    __syncthreads();
+    if (has_hist) {
+#pragma unroll
+      for (int j = 0; j < kVecs; ++j) {
+        const uint4 e = ((const uint4*)counts)[j * THREADS + threadIdx.x];
+        if (!(e.x | e.y | e.z | e.w)) continue;
+        const uint32_t c[4] = {e.x, e.y, e.z, e.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float& x = z[j * 4 + i];
+          if (c[i]) x = (x > 0.0f ? x / rho : x * rho) - (pres + freq * (float)c[i]);
+        }
       }
-      __syncthreads();
     }
   }
-  if (q >= 0 && a.bias_off) {
-    const RowSpan h = span_of(a.bias_off, q, a.n_bias);
-    if (h.b < h.e) {
-      for (int i = threadIdx.x; i < kScoreChunk; i += kScoreThreads) table[i] = 0;
+  if (has_bias) {
+    if (TABLES == 1) {
+      if (has_hist) __syncthreads();
+      clear(places);
       __syncthreads();
-      for (int64_t i = h.b + threadIdx.x; i < h.e; i += kScoreThreads) {
-        const int l = a.bias_id[i];
-        if (l >= c0 && l < V && l - c0 < kScoreChunk) atomicMax(&table[l - c0], (uint32_t)(i - h.b) + 1u);
-      }
-      __syncthreads();
-#pragma unroll
-      for (int j = 0; j < kScoreEach; ++j) {
-        const uint32_t c = table[((j >> 2) * kScoreThreads + (int)threadIdx.x) * 4 + (j & 3)];
-        if (c) z[j] += a.bias_val[h.b + (c - 1)];
-      }
+      place();
       __syncthreads();
     }
-  }
-  if (mask) {
 #pragma unroll
-    for (int j = 0; j < kScoreEach / 4; ++j) {
-      const int v = c0 + (j * kScoreThreads + (int)threadIdx.x) * 4;
-      const uint32_t w = v < V ? mask[v >> 5] >> (v & 31) : 0u;
+    for (int j = 0; j < kVecs; ++j) {
+      const uint4 e = ((const uint4*)places)[j * THREADS + threadIdx.x];
+      if (!(e.x | e.y | e.z | e.w)) continue;
+      const uint32_t c[4] = {e.x, e.y, e.z, e.w};
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (!((w >> i) & 1u)) z[j * 4 + i] = -INFINITY;
+        if (c[i]) z[j * 4 + i] += a.bias_val[bias.b + (c[i] - 1)];
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < EACH; ++j)
+    if (!(keep[j / 4] >> (j & 3) & 1u)) z[j] = -INFINITY;
+
+  float m = 0.0f, lse = 0.0f;
+  if (PHASE != kWrite && a.normalize) {
+    m = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) m = fmaxf(m, z[j]);
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    if (lane == 0) red[0][wave] = m;
+    __syncthreads();
+    m = red[0][0];
+#pragma unroll
+    for (int w = 1; w < kWavesHere; ++w) m = fmaxf(m, red[0][w]);
+    const float top = m;
+    m = shift_of(m);
+    float s = 0.0f;
+#pragma unroll
+    for (int j = 0; j < EACH; ++j) s += exp_of(z[j] - m);
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+    if (lane == 0) red[1][wave] = s;
+    __syncthreads();
+    s = red[1][0];
+#pragma unroll
+    for (int w = 1; w < kWavesHere; ++w) s += red[1][w];
+    if (PHASE == kStats) {
+      if (threadIdx.x == 0) args.part[blockIdx.x] = make_float2(top, s);
+      return;
+    }
+    lse = logf(s);
+  }
+  if (PHASE == kWrite && a.normalize) {
+    const float2* p = args.part + n * args.slices;
+    m = -INFINITY;
+    for (uint32_t i = lane; i < args.slices; i += 64) m = fmaxf(m, p[i].x);
+    for (int o = 32; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor(m, o));
+    m = shift_of(m);
+    float s = 0.0f;
+    for (uint32_t i = lane; i < args.slices; i += 64) s += p[i].y == 0.0f ? 0.0f : p[i].y * exp_of(shift_of(p[i].x) - m);
+    for (int o = 32; o > 0; o >>= 1) s += __shfl_xor(s, o);
+    lse = logf(s);
+  }
+  float* out = a.out + to * a.out_ld;
+#pragma unroll
+  for (int j = 0; j < kVecs; ++j) {
+    const int v = at + j * kStep;
+    if (v >= V) break;
+    Few<F32, 4> prior{};
+    if (a.log_prior) prior = load4((const F32*)a.log_prior + v, V - v, F32{0.0f});
+    f32x4 y;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float x = z[j * 4 + i];
+      y[i] = x == -INFINITY ? x : a.scale * (((x - m) - lse) - prior.v[i].u);
+    }
+    if (V - v >= 4) {
+      if (args.stream)
+        __builtin_nontemporal_store(y, (f32x4_any*)(out + v));
+      else
+        *(f32x4_any*)(out + v) = y;
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (v + i < V) out[v + i] = y[i];
     }
   }
 }
 
+// Rows of up to kWholeLabels labels are one slice: they are read once and their
+// lists are scattered once (400 rows of 30000 labels of 16 bits with histories and
+// biases: 39 us, in slices 73; 8 rows: 23 and 27 with the launch).  Longer ones go
+// in slices, twice (400 rows of 100000 labels: 155 us in slices of 8192 labels, 171
+// of 16384, 190 of 32768: more workgroups hide each other's waits for the lists).
+constexpr int kWholeLabels = 32768;
+constexpr int kSliceThreads = 512, kSliceEach = 16, kSliceLabels = kSliceThreads * kSliceEach;
+
+template <class T, int THREADS, int EACH, int TABLES, ScorePhase PHASE>
+void launch_slices(const ScoreArgs& args, hipStream_t s) {
+  auto* k = k_loglikes<T, THREADS, EACH, TABLES, PHASE>;
+  const int lists = (args.a.hist_off ? 1 : 0) + (args.a.bias_off ? 1 : 0);
+  const int bytes = (lists < TABLES ? lists : TABLES) * THREADS * EACH * 4;
+  if (bytes > 65536) (void)hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  hipLaunchKernelGGL(k, dim3((uint32_t)args.a.N * args.slices), dim3(THREADS), bytes, s, args);
+}
+
 template <class T>
-__global__ void __launch_bounds__(kScoreThreads) k_loglikes(ScoreArgs args) {
-  const wd_loglikes_args& a = args.a;
-  __shared__ uint32_t table[kScoreChunk];
-  __shared__ float red[2 * kScoreThreads];
-  for (int64_t n = blockIdx.x; n < a.N; n += gridDim.x) {
-    int64_t to = n;
-    if (a.out_row) {
-      to = a.out_row[n];
-      if (to < 0 || to >= a.out_rows) continue;
-    }
-    const T* row = (const T*)a.logits + n * a.ld;
-    float* out = a.out + to * a.out_ld;
-    int q = -1;
-    if (a.n_requests > 0) {
-      const int64_t r = a.request ? (int64_t)a.request[n] : n;
-      q = r >= 0 && r < a.n_requests ? (int)r : -1;
-    }
-    const uint32_t* mask = nullptr;
-    if (a.mask) {
-      const int64_t r = a.mask_of ? (int64_t)a.mask_of[n] : n;
-      if (r >= 0 && r < a.n_masks) mask = a.mask + r * a.mask_ld;
-    }
-    float z[kScoreEach];
-    float m = -INFINITY, s = 0.0f, lse = 0.0f;
-    if (a.normalize) {
-      for (int c0 = 0; c0 < a.V; c0 += kScoreChunk) {
-        score_chunk(a, row, q, mask, c0, table, z);
-        float cm = m;
-#pragma unroll
-        for (int j = 0; j < kScoreEach; ++j) cm = fmaxf(cm, z[j]);
-        const float base = cm == -INFINITY ? 0.0f : cm;  // nothing above -inf: exp(z - 0) = 0, a NaN stays one
-        s = s == 0.0f ? 0.0f : s * exp_of(m - base);
-#pragma unroll
-        for (int j = 0; j < kScoreEach; ++j) s += exp_of(z[j] - base);
-        m = cm;
-      }
-      red[threadIdx.x] = m;
-      red[kScoreThreads + threadIdx.x] = s;
-      __syncthreads();
-      for (int w = kScoreThreads / 2; w > 0; w >>= 1) {
-        if ((int)threadIdx.x < w) {
-          const float m0 = red[threadIdx.x], m1 = red[threadIdx.x + w];
-          const float mm = fmaxf(m0, m1), base = mm == -INFINITY ? 0.0f : mm;
-          const float s0 = red[kScoreThreads + threadIdx.x], s1 = red[kScoreThreads + threadIdx.x + w];
-          red[threadIdx.x] = mm;
-          red[kScoreThreads + threadIdx.x] = (s0 == 0.0f ? 0.0f : s0 * exp_of(m0 - base)) + (s1 == 0.0f ? 0.0f : s1 * exp_of(m1 - base));
-        }
-        __syncthreads();
-      }
-      m = red[0] == -INFINITY ? 0.0f : red[0];
-      lse = logf(red[kScoreThreads]);
-      __syncthreads();
-    } else {
-      m = 0.0f;
-    }
-    for (int c0 = 0; c0 < a.V; c0 += kScoreChunk) {
-      if (!a.normalize || a.V > kScoreChunk) score_chunk(a, row, q, mask, c0, table, z);
-#pragma unroll
-      for (int j = 0; j < kScoreEach; ++j) {
-        const int v = c0 + ((j >> 2) * kScoreThreads + (int)threadIdx.x) * 4 + (j & 3);
-        if (v < a.V) {
-          const float y = (z[j] - m) - lse - (a.log_prior ? a.log_prior[v] : 0.0f);
-          out[v] = z[j] == -INFINITY ? z[j] : a.scale * y;
-        }
-      }
-    }
+void launch_loglikes(const wd_loglikes_args* a, void* ws, hipStream_t s) {
+  ScoreArgs args{*a, (float2*)ws, 1, (uint64_t)a->N * a->V * 4 >= (256u << 20)};
+  if (a->V <= 2048)
+    launch_slices<T, 256, 8, 2, kWhole>(args, s);
+  else if (a->V <= 4096)
+    launch_slices<T, 256, 16, 2, kWhole>(args, s);
+  else if (a->V <= 8192)
+    launch_slices<T, 256, 32, 2, kWhole>(args, s);
+  else if (a->V <= 16384)
+    launch_slices<T, 1024, 16, 2, kWhole>(args, s);
+  else if (a->V <= kWholeLabels)
+    launch_slices<T, 1024, 32, 1, kWhole>(args, s);
+  else {
+    args.slices = (uint32_t)((a->V + kSliceLabels - 1) / kSliceLabels);
+    if (a->normalize) launch_slices<T, kSliceThreads, kSliceEach, 2, kStats>(args, s);
+    launch_slices<T, kSliceThreads, kSliceEach, 2, kWrite>(args, s);
   }
 }
 
@@ -172,8 +278,8 @@ using namespace wd;
 
 static wd_status check_loglikes(const wd_loglikes_args* a) {
   if (!a) return fail(WD_EINVAL, "loglikes: null arguments");
-  if (a->N < 0) return fail(WD_EINVAL, "loglikes: negative N");
   if (a->V < 1 || a->V >= (1 << 24)) return fail(WD_EINVAL, "loglikes: V out of range");
+  if (a->N < 0 || a->N > INT32_MAX / (a->V / kSliceLabels + 1)) return fail(WD_EINVAL, "loglikes: N out of range");
   if (a->type != WD_F32 && a->type != WD_F16 && a->type != WD_BF16) return fail(WD_EINVAL, "loglikes: unknown type");
   if (a->ld < a->V || a->out_ld < a->V) return fail(WD_EINVAL, "loglikes: row stride below V");
   if (!(a->scale > 0.0f) || std::isinf(a->scale)) return fail(WD_EINVAL, "loglikes: scale must be finite and > 0");
@@ -198,27 +304,32 @@ static wd_status check_loglikes(const wd_loglikes_args* a) {
   return WD_OK;
 }
 
+// Workspace: the slices' maxima and sums.
+static size_t parts_bytes(const wd_loglikes_args* a) {
+  if (a->V <= kWholeLabels || !a->normalize) return 0;
+  return align_up((uint64_t)a->N * ((a->V + kSliceLabels - 1) / kSliceLabels) * sizeof(float2), 256);
+}
+
 extern "C" wd_status wd_loglikes_workspace_bytes(const wd_loglikes_args* a, size_t* bytes) {
   if (!bytes) return fail(WD_EINVAL, "loglikes_workspace_bytes: null output");
   wd_status st = check_loglikes(a);
   if (st != WD_OK) return st;
-  *bytes = 0;
+  *bytes = parts_bytes(a);
   return WD_OK;
 }
 
 extern "C" wd_status wd_loglikes(const wd_loglikes_args* a, void* ws, size_t ws_bytes, void* stream) {
   wd_status st = check_loglikes(a);
   if (st != WD_OK || a->N == 0) return st;
-  (void)ws;
-  (void)ws_bytes;
-  const ScoreArgs args{*a};
-  const dim3 grid((uint32_t)std::min<int64_t>(a->N, 1 << 20)), block(kScoreThreads);
+  const size_t need = parts_bytes(a);
+  if (need && (!ws || ws_bytes < need || (uintptr_t)ws & 255))
+    return fail(WD_EINVAL, "loglikes: workspace missing, too small or not 256-byte aligned");
   hipStream_t s = (hipStream_t)stream;
   if (a->type == WD_F32)
-    hipLaunchKernelGGL(k_loglikes<F32>, grid, block, 0, s, args);
+    launch_loglikes<F32>(a, ws, s);
   else if (a->type == WD_F16)
-    hipLaunchKernelGGL(k_loglikes<Half>, grid, block, 0, s, args);
+    launch_loglikes<Half>(a, ws, s);
   else
-    hipLaunchKernelGGL(k_loglikes<Bf16>, grid, block, 0, s, args);
+    launch_loglikes<Bf16>(a, ws, s);
   return hip_check(hipGetLastError(), "loglikes");
 }
