@@ -74,8 +74,9 @@ __device__ inline uint2 factor_bits(double f, bool eps, uint32_t lvl) {
 #endif
 
 // Device copy of the decoding graph, laid out in one caller-owned buffer.
-//   off[s]  = {first emitting arc, first epsilon arc, first epsilon path, 0} of
-//             state s (S+1 entries; the path index is 0 without a path table)
+//   off[s]  = {first emitting arc, first epsilon arc, first epsilon path, number
+//             of arcs} of state s (S+1 entries; the path index is 0 without a path
+//             table)
 //   earc[i] = {dst, weight bits, ilabel | dst_class << 24, arc id}
 //   xarc[j] = {dst, weight bits, dst_class, arc id}
 //   xnext[j] = epsilon arc range {first, end} of xarc[j]'s destination
