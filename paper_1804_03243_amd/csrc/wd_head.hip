@@ -512,9 +512,13 @@ __device__ __forceinline__ void loads_left() {
 // A workgroup takes 32 outputs of every row, its eight wavefronts a part of the
 // columns each; the operands come straight from memory (x from the caches), 128
 // bytes of a row between the lanes, and the parts are added through LDS.
-template <class T, class O, int NB>
+// With FEW rows (at most kFewRows) a workgroup first forms the rows' u itself,
+// which costs it the reads of their adapters but the call a launch.
+constexpr int kFewRows = 4;
+template <class T, class O, int NB, bool FEW>
 __global__ void __launch_bounds__(512) k_rows(HeadArgs a) {
   __shared__ f32x4 part[8][NB * 2][64];
+  __shared__ float low_u[FEW ? kFewRows : 1][FEW ? WD_MAX_RANK : 1];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
   const int D = a.h.D, P = a.h.P, p0 = blockIdx.x * 32;
   const T *w[2], *x[NB];
@@ -525,6 +529,19 @@ __global__ void __launch_bounds__(512) k_rows(HeadArgs a) {
   // the row and the outputs that this lane finishes
   const int fi = (wave >> 1) * 16 + col, fp = p0 + (wave & 1) * 16 + quad * 4;
   const int g = wave < NB * 2 ? adapter_of(a, fi) : -1;
+  if constexpr (FEW) {
+    const int R = a.h.rank, pairs = (R + 1) / 2;
+    for (int i = wave; i < (int)a.N * pairs; i += 8) {
+      const int n = i / pairs, r = i % pairs * 2, gn = adapter_of(a, n);
+      if (gn < 0) continue;
+      const T* w0 = (const T*)a.h.a + ((int64_t)gn * R + r) * D;
+      float s0, s1;
+      row_products((const T*)a.x + n * a.x_ld, w0, w0 + (r + 1 < R ? D : 0), D, s0, s1);
+      const float sc = a.h.scale ? a.h.scale[gn] : 1.0f;
+      if (lane < 2 && r + lane < R) low_u[n][r + lane] = (lane ? s1 : s0) * sc;
+    }
+    // (read behind the barrier below)
+  }
   f32x4 acc[NB][2] = {};
   int k = wave * 64 + quad * 16;
 #pragma unroll 2
@@ -567,7 +584,20 @@ __global__ void __launch_bounds__(512) k_rows(HeadArgs a) {
   f32x4 y = part[0][wave][lane];
 #pragma unroll
   for (int v = 1; v < 8; ++v) y += part[v][wave][lane];
-  if (g >= 0) {
+  if (FEW && g >= 0 && fp < P) {
+    const T* b = (const T*)a.h.b + ((int64_t)g * P + fp) * a.h.rank;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const T* be = b + (int64_t)min(e, P - 1 - fp) * a.h.rank;
+      float low = 0.0f;
+      for (int r = 0; r < a.h.rank; r += 8) {
+        const uint4 v = load8(be + r, a.h.rank - r);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) low = fmaf(((const T*)&v)[i].f(), r + i < a.h.rank ? low_u[fi][r + i] : 0.0f, low);
+      }
+      y[e] += low;
+    }
+  } else if (g >= 0) {
     const f32x4 low = low_of_row<T, kTerms<T, O>, 2>(a, fi, g, fp);
     const float us = a.us[fi];
 #pragma unroll
@@ -752,12 +782,18 @@ void launch_tiles(const HeadArgs& a, hipStream_t s) {
   constexpr int stages = 2 * (BM + BN) * kStepK * 2;
   static_assert(low <= stages, "");
   constexpr int bytes = stages + BM * 4;
-  if (bytes > 65536) (void)hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  static std::atomic<uint64_t> done{0};
+  allow_lds((const void*)k, bytes, done);
   hipLaunchKernelGGL(k, dim3(rows * cols), dim3(64 * WM * WN), bytes, s, a, rows, cols);
 }
 
 template <class T, class O>
 void launch_project(HeadArgs a, hipStream_t s) {
+  const dim3 outs(((uint32_t)a.h.P + 31) / 32), block(512);
+  if (a.adapter && a.N <= kFewRows) {
+    hipLaunchKernelGGL((k_rows<T, O, 1, true>), outs, block, 0, s, a);
+    return;
+  }
   if (a.adapter) {
     constexpr int terms = kTerms<T, O>;
     a.uk = terms * a.rp;
@@ -770,13 +806,12 @@ void launch_project(HeadArgs a, hipStream_t s) {
                        !((uintptr_t)a.h.weight & 15);
   a.stream = (uint64_t)a.N * a.h.P * sizeof(O) >= (256u << 20);
   const auto tiles = [&](int64_t m, int64_t n) { return ((a.N + m - 1) / m) * ((a.h.P + n - 1) / n); };
-  const dim3 outs(((uint32_t)a.h.P + 31) / 32), block(512);
   if (a.N <= 16)
-    hipLaunchKernelGGL((k_rows<T, O, 1>), outs, block, 0, s, a);
+    hipLaunchKernelGGL((k_rows<T, O, 1, false>), outs, block, 0, s, a);
   else if (a.N <= 32)
-    hipLaunchKernelGGL((k_rows<T, O, 2>), outs, block, 0, s, a);
+    hipLaunchKernelGGL((k_rows<T, O, 2, false>), outs, block, 0, s, a);
   else if (a.N <= 64)
-    hipLaunchKernelGGL((k_rows<T, O, 4>), outs, block, 0, s, a);
+    hipLaunchKernelGGL((k_rows<T, O, 4, false>), outs, block, 0, s, a);
   else if (!aligned)
     launch_tiles<T, O, 64, 64, 2, 2, false>(a, s);
   else if (tiles(256, 256) >= 256)

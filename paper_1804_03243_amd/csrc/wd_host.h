@@ -1,6 +1,7 @@
 // Host-side declarations shared by the library's translation units.
 #pragma once
 
+#include <atomic>
 #include <string>
 #include <vector>
 
@@ -60,6 +61,15 @@ void launch_set_frames(LaneDesc* lanes, int B, const int32_t* T, const int32_t* 
 // cluster headers again for a stream's advances).
 void launch_setup(const LaneDesc* lanes, int B, uint32_t* bad, uint64_t used_words, uint64_t S, uint64_t bitmap_words,
                   bool chip, hipStream_t s);
+
+// Lets a kernel have more than 64 KB of dynamic LDS; `done` (one per kernel) is
+// the devices where that has been said.
+inline void allow_lds(const void* kernel, int bytes, std::atomic<uint64_t>& done) {
+  int dev = 0;
+  if (bytes <= 65536 || hipGetDevice(&dev) != hipSuccess || (done.load(std::memory_order_relaxed) >> (dev & 63) & 1)) return;
+  if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes) == hipSuccess && dev < 64)
+    done.fetch_or(1ull << dev, std::memory_order_relaxed);
+}
 
 inline uint64_t align_up(uint64_t x, uint64_t a) { return (x + a - 1) / a * a; }
 

@@ -248,7 +248,8 @@ void launch_slices(const ScoreArgs& args, hipStream_t s) {
   auto* k = k_loglikes<T, THREADS, EACH, TABLES, PHASE>;
   const int lists = (args.a.hist_off ? 1 : 0) + (args.a.bias_off ? 1 : 0);
   const int bytes = (lists < TABLES ? lists : TABLES) * THREADS * EACH * 4;
-  if (bytes > 65536) (void)hipFuncSetAttribute((const void*)k, hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  static std::atomic<uint64_t> done{0};
+  allow_lds((const void*)k, TABLES * THREADS * EACH * 4, done);
   hipLaunchKernelGGL(k, dim3((uint32_t)args.a.N * args.slices), dim3(THREADS), bytes, s, args);
 }
 

@@ -12,7 +12,6 @@ is missing this module raises.
 """
 from __future__ import annotations
 
-import contextlib
 import ctypes
 import os
 from types import SimpleNamespace
@@ -552,9 +551,9 @@ class Graph:
             _matrix(out, (torch.int32,), self.device, "out")
             if out.shape[0] != N or out.shape[1] < words:
                 raise ValueError(f"out must be {N} rows of at least {words} words")
-        with _on(torch, self.device):
-            wd_label_masks(self.handle, N, offsets.data_ptr(), states.data_ptr(), states.shape[0], out.data_ptr(),
-                           max(out.stride(0), words), _stream(torch))
+        _enqueue(self.device, lambda stream: wd_label_masks(
+            self.handle, N, offsets.data_ptr(), states.data_ptr(), states.shape[0], out.data_ptr(),
+            max(out.stride(0), words), stream))
         return out
 
     def workspace(self, lanes: int, max_T: int, params: wd_params, caps: wd_caps | None):
@@ -747,9 +746,26 @@ class Stream:
 
 # ------------------------------------------- log-likelihoods from hidden rows
 
-def _on(torch, device):
-    """The device as the current one (nothing to do where it is)."""
-    return contextlib.nullcontext() if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+def _enqueue(device, call):
+    """call(stream) with the device as the current one and its current stream.
+    These calls take microseconds, so the handle comes from torch's binding
+    where it has one, without a Stream object around it."""
+    torch = _torch()
+    if torch.cuda.current_device() != device.index:
+        with torch.cuda.device(device):
+            return _enqueue(device, call)
+    raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return call(raw(device.index) if raw is not None else _stream(torch))
+
+
+_TYPES = {}
+
+
+def _types(torch):
+    """The library's code of a tensor's type."""
+    if not _TYPES:
+        _TYPES.update({torch.float32: WD_F32, torch.float16: WD_F16, torch.bfloat16: WD_BF16})
+    return _TYPES
 
 
 def _vector(t, dtype, device, what):
@@ -760,7 +776,7 @@ def _vector(t, dtype, device, what):
 def _matrix(t, dtypes, device, what):
     if t.dtype not in dtypes or t.dim() != 2 or t.device != device:
         raise ValueError(f"{what} must be a 2-d tensor of {' or '.join(map(str, dtypes))} on {device}")
-    if t.shape[1] > 1 and t.stride(1) != 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+    if not t.is_contiguous() and (t.shape[1] > 1 and t.stride(1) != 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1]):
         raise ValueError(f"{what} must have contiguous, separate rows")
 
 
@@ -780,8 +796,8 @@ class Head:
 
     def __init__(self, weight, bias=None, adapter_a=None, adapter_b=None, adapter_scale=None):
         torch = _torch()
-        types = {torch.float16: WD_F16, torch.bfloat16: WD_BF16}
-        _matrix(weight, tuple(types), weight.device, "weight")
+        types = {t: v for t, v in _types(torch).items() if v != WD_F32}
+        _matrix(weight, types, weight.device, "weight")
         P, D = weight.shape
         dev = weight.device
         if bias is not None:
@@ -828,17 +844,16 @@ class Head:
         if out is None:
             out = torch.empty((N, self.P), dtype=torch.float32 if out_dtype is None else out_dtype, device=self.device)
         else:
-            _matrix(out, tuple(self._out_types), self.device, "out")
+            _matrix(out, self._out_types, self.device, "out")
             if tuple(out.shape) != (N, self.P) or out_dtype not in (None, out.dtype):
                 raise ValueError(f"out must be {N} x {self.P} of out_dtype")
         if out.dtype not in self._out_types:
             raise ValueError(f"out_dtype must be float32 or {self.dtype}")
-        with _on(torch, self.device):
-            nbytes = wd_project_workspace_bytes(self.desc, N) if adapter is not None else 0
-            ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device) if nbytes else None
-            wd_project(self.desc, x.data_ptr(), _ld(x), N, None if adapter is None else adapter.data_ptr(),
-                       out.data_ptr(), _ld(out), self._out_types[out.dtype], None if ws is None else ws.data_ptr(),
-                       nbytes, _stream(torch))
+        nbytes = wd_project_workspace_bytes(self.desc, N) if adapter is not None and self.G else 0
+        ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device) if nbytes else None
+        _enqueue(self.device, lambda stream: wd_project(
+            self.desc, x.data_ptr(), _ld(x), N, None if adapter is None else adapter.data_ptr(), out.data_ptr(),
+            _ld(out), self._out_types[out.dtype], None if ws is None else ws.data_ptr(), nbytes, stream))
         return out
 
 
@@ -861,9 +876,9 @@ def loglikes(logits, *, normalize: bool = True, scale: float = 1.0, log_prior=No
 
     Returns `out`.  Enqueued on the current stream."""
     torch = _torch()
-    types = {torch.float32: WD_F32, torch.float16: WD_F16, torch.bfloat16: WD_BF16}
+    types = _types(torch)
     dev = logits.device
-    _matrix(logits, tuple(types), dev, "logits")
+    _matrix(logits, types, dev, "logits")
     N, V = logits.shape
     a = wd_loglikes_args(N=N, V=V, type=types[logits.dtype], logits=logits.data_ptr(), ld=_ld(logits),
                          normalize=int(bool(normalize)), scale=scale)
@@ -920,8 +935,7 @@ def loglikes(logits, *, normalize: bool = True, scale: float = 1.0, log_prior=No
         if out.shape[1] != V or out_row is None and out.shape[0] != N:
             raise ValueError(f"out must be rows of {V} float32, {N} of them without out_row")
     a.out, a.out_ld, a.out_rows = out.data_ptr(), _ld(out), out.shape[0]
-    with _on(torch, dev):
-        nbytes = wd_loglikes_workspace_bytes(a)
-        ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
-        wd_loglikes(a, None if ws is None else ws.data_ptr(), nbytes, _stream(torch))
+    nbytes = wd_loglikes_workspace_bytes(a)
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
+    _enqueue(dev, lambda stream: wd_loglikes(a, None if ws is None else ws.data_ptr(), nbytes, stream))
     return out
