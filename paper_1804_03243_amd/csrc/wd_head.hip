@@ -529,6 +529,34 @@ __global__ void __launch_bounds__(512) k_rows(HeadArgs a) {
   // the row and the outputs that this lane finishes
   const int fi = (wave >> 1) * 16 + col, fp = p0 + (wave & 1) * 16 + quad * 4;
   const int g = wave < NB * 2 ? adapter_of(a, fi) : -1;
+  struct Operands {
+    uint4 w[2][2], x[2][NB];
+  };
+  const auto read = [&](int k, Operands& o) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) o.w[h][j] = load8(w[j] + k + h * 8, 8);
+#pragma unroll
+      for (int i = 0; i < NB; ++i) o.x[h][i] = load8(x[i] + k + h * 8, 8);
+    }
+  };
+  f32x4 acc[NB][2] = {};
+  const auto multiply = [&](const Operands& o) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+#pragma unroll
+      for (int i = 0; i < NB; ++i)
+#pragma unroll
+        for (int j = 0; j < 2; ++j) acc[i][j] = mfma16(o.w[h][j], o.x[h][i], acc[i][j], T{});
+  };
+  // Two of this wavefront's steps of 64 columns are read at a time, the first two
+  // before the adapter's part, so that they are under way together.
+  const int step = 512, k1 = wave * 64 + quad * 16, whole = (D - wave * 64) / 64 > 0 ? ((D - wave * 64) / 64 + 7) / 8 : 0;
+  Operands o0, o1;
+  if (whole > 0) read(k1, o0);
+  if (whole > 1) read(k1 + step, o1);
+  f32x4 low = {0, 0, 0, 0};
   if constexpr (FEW) {
     const int R = a.h.rank, pairs = (R + 1) / 2;
     for (int i = wave; i < (int)a.N * pairs; i += 8) {
@@ -541,26 +569,21 @@ __global__ void __launch_bounds__(512) k_rows(HeadArgs a) {
       if (lane < 2 && r + lane < R) low_u[n][r + lane] = (lane ? s1 : s0) * sc;
     }
     // (read behind the barrier below)
+  } else if (g >= 0) {
+    low = low_of_row<T, kTerms<T, O>, 2>(a, fi, g, fp);
+    const float us = a.us[fi];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) low[e] *= us;
   }
-  f32x4 acc[NB][2] = {};
-  int k = wave * 64 + quad * 16;
-#pragma unroll 2
-  for (; (k & ~63) + 64 <= D; k += 512) {
-    uint4 wv[2][2], xv[NB][2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-#pragma unroll
-      for (int j = 0; j < 2; ++j) wv[j][h] = load8(w[j] + k + h * 8, 8);
-#pragma unroll
-      for (int i = 0; i < NB; ++i) xv[i][h] = load8(x[i] + k + h * 8, 8);
-    }
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-#pragma unroll
-      for (int i = 0; i < NB; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) acc[i][j] = mfma16(wv[j][h], xv[i][h], acc[i][j], T{});
+  if (whole > 0) multiply(o0);
+  if (whole > 1) multiply(o1);
+  for (int i = 2; i < whole; i += 2) {
+    read(k1 + i * step, o0);
+    if (i + 1 < whole) read(k1 + (i + 1) * step, o1);
+    multiply(o0);
+    if (i + 1 < whole) multiply(o1);
   }
+  const int k = k1 + whole * step;
   if ((k & ~63) < D) {
     for (int h = 0; h < 2; ++h) {
       const int left = D - k - h * 8;
@@ -589,20 +612,14 @@ __global__ void __launch_bounds__(512) k_rows(HeadArgs a) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const T* be = b + (int64_t)min(e, P - 1 - fp) * a.h.rank;
-      float low = 0.0f;
       for (int r = 0; r < a.h.rank; r += 8) {
         const uint4 v = load8(be + r, a.h.rank - r);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) low = fmaf(((const T*)&v)[i].f(), r + i < a.h.rank ? low_u[fi][r + i] : 0.0f, low);
+        for (int i = 0; i < 8; ++i) low[e] = fmaf(((const T*)&v)[i].f(), r + i < a.h.rank ? low_u[fi][r + i] : 0.0f, low[e]);
       }
-      y[e] += low;
     }
-  } else if (g >= 0) {
-    const f32x4 low = low_of_row<T, kTerms<T, O>, 2>(a, fi, g, fp);
-    const float us = a.us[fi];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) y[e] = fmaf(low[e], us, y[e]);
   }
+  y += low;
   if (fi >= a.N || fp >= P) return;
   Few<O, 4> out;
 #pragma unroll
