@@ -2,13 +2,15 @@
 // biases, its row's label mask, log-softmax, log priors and the acoustic scale.
 //
 // A workgroup holds a row, or a slice of one, in registers.  Its penalties need the
-// count of each label in the request's history: the history is scattered into a
-// table of the slice's labels in LDS (integer atomics: the order of the entries does
-// not matter), and the last bias entry of a label is the maximum of the entries'
-// positions in a second table.  Then m = max z and s = sum of exp(z - m) over the
-// workgroup, in 32 bits, and y = (z - m) - log s.  Bound by memory where rows are
-// many (48 thousand rows of 6000 labels of 32 bits: 600 us, 5.1 TB/s, what a copy
-// reaches), by the chain of reads request, offsets, list where they are few.
+// count of each label in the request's history, its biases the last entry of
+// the label: both lists are scattered into one table of the slice's labels in LDS, the
+// last entry as the maximum of the entries' positions in the upper 16 bits, then the
+// count by additions in the lower ones (integer atomics: the order of the entries
+// does not matter; longer lists take the table in turn).  Then m = max z and s = sum
+// of exp(z - m) over the workgroup, in 32 bits, and y = (z - m) - log s.  Bound by
+// memory where rows are many (48 thousand rows of 6000 labels of 32 bits: 600 us, 5.1
+// TB/s, what a copy reaches), by the chain of reads request, offsets, list where they
+// are few.
 #include <algorithm>
 #include <cmath>
 
@@ -59,11 +61,11 @@ enum ScorePhase {
 
 // A workgroup per slice of THREADS * EACH labels, a thread's labels in registers:
 // (j * THREADS + thread) * 4 + i of the slice is z[j * 4 + i].
-template <class T, int THREADS, int EACH, int TABLES, ScorePhase PHASE>
+template <class T, int THREADS, int EACH, ScorePhase PHASE, bool LISTS>
 __global__ void __launch_bounds__(THREADS) k_loglikes(ScoreArgs args) {
   constexpr int kSlice = THREADS * EACH, kVecs = EACH / 4, kWavesHere = THREADS / 64;
   const wd_loglikes_args& a = args.a;
-  extern __shared__ uint32_t table[];  // [TABLES][kSlice], where there are histories or biases
+  extern __shared__ uint32_t table[];  // [kSlice], where there are histories or biases
   __shared__ float red[2][kWavesHere];
   const int64_t n = PHASE == kWhole ? blockIdx.x : blockIdx.x / args.slices;
   const int c0 = PHASE == kWhole ? 0 : (int)(blockIdx.x % args.slices) * kSlice;
@@ -79,8 +81,8 @@ __global__ void __launch_bounds__(THREADS) k_loglikes(ScoreArgs args) {
     q = r >= 0 && r < a.n_requests ? (int)r : -1;
   }
   RowSpan hist{0, 0}, bias{0, 0};
-  if (q >= 0 && a.hist_off) hist = span_of(a.hist_off, q, a.n_hist);
-  if (q >= 0 && a.bias_off) bias = span_of(a.bias_off, q, a.n_bias);
+  if (LISTS && q >= 0 && a.hist_off) hist = span_of(a.hist_off, q, a.n_hist);
+  if (LISTS && q >= 0 && a.bias_off) bias = span_of(a.bias_off, q, a.n_bias);
   const int V = a.V, at = c0 + (int)threadIdx.x * 4;
   constexpr int kStep = THREADS * 4;
   const T* row = (const T*)a.logits + n * a.ld;
@@ -104,66 +106,57 @@ __global__ void __launch_bounds__(THREADS) k_loglikes(ScoreArgs args) {
 #pragma unroll
   for (int j = 0; j < EACH; ++j) z[j] = raw[j / 4].v[j & 3].f();
   const bool has_hist = hist.b < hist.e, has_bias = bias.b < bias.e;  // (the same for the whole workgroup)
-  // tables of the slice's labels: counts in the history, positions in the biases
-  uint32_t* counts = table;
-  uint32_t* places = TABLES == 2 && has_hist ? table + kSlice : table;
-  const auto clear = [&](uint32_t* t) {
-#pragma unroll
-    for (int j = 0; j < kVecs; ++j) ((uint4*)t)[j * THREADS + threadIdx.x] = make_uint4(0, 0, 0, 0);
-  };
-  const auto count = [&]() {
-#pragma unroll 4
-    for (int64_t i = hist.b + threadIdx.x; i < hist.e; i += THREADS) {
-      const int l = a.hist[i];
-      if (l < V && (uint32_t)(l - c0) < (uint32_t)kSlice) atomicAdd(&counts[l - c0], 1u);
-    }
-  };
-  const auto place = [&]() {
-#pragma unroll 4
-    for (int64_t i = bias.b + threadIdx.x; i < bias.e; i += THREADS) {
-      const int l = a.bias_id[i];
-      if (l < V && (uint32_t)(l - c0) < (uint32_t)kSlice) atomicMax(&places[l - c0], (uint32_t)(i - bias.b) + 1u);
-    }
-  };
-  if (has_hist || (has_bias && TABLES == 2)) {
+  if (LISTS && (has_hist || has_bias)) {
     const float rho = has_hist && a.repetition ? a.repetition[q] : 1.0f;
     const float pres = has_hist && a.presence ? a.presence[q] : 0.0f, freq = has_hist && a.frequency ? a.frequency[q] : 0.0f;
-    if (has_hist) clear(counts);
-    if (has_bias && TABLES == 2) clear(places);
-    __syncthreads();
-    count();
-    if (TABLES == 2) place();
-    __syncthreads();
-    if (has_hist) {
+    const auto clear = [&]() {
+#pragma unroll
+      for (int j = 0; j < kVecs; ++j) ((uint4*)table)[j * THREADS + threadIdx.x] = make_uint4(0, 0, 0, 0);
+      __syncthreads();
+    };
+    const auto inside = [&](int l) { return l < V && (uint32_t)(l - c0) < (uint32_t)kSlice; };
+    const auto place = [&](int shift) {
+#pragma unroll 4
+      for (int64_t i = bias.b + threadIdx.x; i < bias.e; i += THREADS) {
+        const int l = a.bias_id[i];
+        if (inside(l)) atomicMax(&table[l - c0], ((uint32_t)(i - bias.b) + 1u) << shift);
+      }
+      __syncthreads();
+    };
+    const auto count = [&]() {
+#pragma unroll 4
+      for (int64_t i = hist.b + threadIdx.x; i < hist.e; i += THREADS) {
+        const int l = a.hist[i];
+        if (inside(l)) atomicAdd(&table[l - c0], 1u);
+      }
+      __syncthreads();
+    };
+    // of each label: how often it stands in the history (e & counts), and which bias it has (e >> places)
+    const auto apply = [&](uint32_t counts, int places) {
 #pragma unroll
       for (int j = 0; j < kVecs; ++j) {
-        const uint4 e = ((const uint4*)counts)[j * THREADS + threadIdx.x];
-        if (!(e.x | e.y | e.z | e.w)) continue;
-        const uint32_t c[4] = {e.x, e.y, e.z, e.w};
+        const uint4 e4 = ((const uint4*)table)[j * THREADS + threadIdx.x];
+        if (!(e4.x | e4.y | e4.z | e4.w)) continue;
+        const uint32_t e[4] = {e4.x, e4.y, e4.z, e4.w};
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           float& x = z[j * 4 + i];
-          if (c[i]) x = (x > 0.0f ? x / rho : x * rho) - (pres + freq * (float)c[i]);
+          const uint32_t c = e[i] & counts, p = (uint32_t)((uint64_t)e[i] >> places);
+          if (c) x = (x > 0.0f ? x / rho : x * rho) - (pres + freq * (float)c);
+          if (p) x += a.bias_val[bias.b + (p - 1)];
         }
       }
-    }
-  }
-  if (has_bias) {
-    if (TABLES == 1) {
-      if (has_hist) __syncthreads();
-      clear(places);
-      __syncthreads();
-      place();
-      __syncthreads();
-    }
-#pragma unroll
-    for (int j = 0; j < kVecs; ++j) {
-      const uint4 e = ((const uint4*)places)[j * THREADS + threadIdx.x];
-      if (!(e.x | e.y | e.z | e.w)) continue;
-      const uint32_t c[4] = {e.x, e.y, e.z, e.w};
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (c[i]) z[j * 4 + i] += a.bias_val[bias.b + (c[i] - 1)];
+    };
+    // both lists at once, or one after the other where one is too long for 16 bits
+    const bool both = hist.e - hist.b < 65536 && bias.e - bias.b < 65536;
+#pragma unroll 1
+    for (int pass = 0; pass < (both ? 1 : 2); ++pass) {
+      const bool counts = has_hist && pass == 0, places = has_bias && (both || pass == 1);
+      if (pass) __syncthreads();
+      clear();
+      if (places) place(both ? 16 : 0);
+      if (counts) count();
+      apply(!counts ? 0u : both ? 0xffffu : 0xffffffffu, !places ? 32 : both ? 16 : 0);
     }
   }
 #pragma unroll
@@ -243,33 +236,36 @@ __global__ void __launch_bounds__(THREADS) k_loglikes(ScoreArgs args) {
 constexpr int kWholeLabels = 32768;
 constexpr int kSliceThreads = 512, kSliceEach = 16, kSliceLabels = kSliceThreads * kSliceEach;
 
-template <class T, int THREADS, int EACH, int TABLES, ScorePhase PHASE>
+template <class T, int THREADS, int EACH, ScorePhase PHASE>
 void launch_slices(const ScoreArgs& args, hipStream_t s) {
-  auto* k = k_loglikes<T, THREADS, EACH, TABLES, PHASE>;
-  const int lists = (args.a.hist_off ? 1 : 0) + (args.a.bias_off ? 1 : 0);
-  const int bytes = (lists < TABLES ? lists : TABLES) * THREADS * EACH * 4;
+  const dim3 grid((uint32_t)args.a.N * args.slices), block(THREADS);
+  if (!args.a.hist_off && !args.a.bias_off) {
+    hipLaunchKernelGGL((k_loglikes<T, THREADS, EACH, PHASE, false>), grid, block, 0, s, args);
+    return;
+  }
+  auto* k = k_loglikes<T, THREADS, EACH, PHASE, true>;
   static std::atomic<uint64_t> done{0};
-  allow_lds((const void*)k, TABLES * THREADS * EACH * 4, done);
-  hipLaunchKernelGGL(k, dim3((uint32_t)args.a.N * args.slices), dim3(THREADS), bytes, s, args);
+  allow_lds((const void*)k, THREADS * EACH * 4, done);
+  hipLaunchKernelGGL(k, grid, block, THREADS * EACH * 4, s, args);
 }
 
 template <class T>
 void launch_loglikes(const wd_loglikes_args* a, void* ws, hipStream_t s) {
   ScoreArgs args{*a, (float2*)ws, 1, (uint64_t)a->N * a->V * 4 >= (256u << 20)};
   if (a->V <= 2048)
-    launch_slices<T, 256, 8, 2, kWhole>(args, s);
+    launch_slices<T, 256, 8, kWhole>(args, s);
   else if (a->V <= 4096)
-    launch_slices<T, 256, 16, 2, kWhole>(args, s);
+    launch_slices<T, 256, 16, kWhole>(args, s);
   else if (a->V <= 8192)
-    launch_slices<T, 256, 32, 2, kWhole>(args, s);
+    launch_slices<T, 256, 32, kWhole>(args, s);
   else if (a->V <= 16384)
-    launch_slices<T, 1024, 16, 2, kWhole>(args, s);
+    launch_slices<T, 1024, 16, kWhole>(args, s);
   else if (a->V <= kWholeLabels)
-    launch_slices<T, 1024, 32, 1, kWhole>(args, s);
+    launch_slices<T, 1024, 32, kWhole>(args, s);
   else {
     args.slices = (uint32_t)((a->V + kSliceLabels - 1) / kSliceLabels);
-    if (a->normalize) launch_slices<T, kSliceThreads, kSliceEach, 2, kStats>(args, s);
-    launch_slices<T, kSliceThreads, kSliceEach, 2, kWrite>(args, s);
+    if (a->normalize) launch_slices<T, kSliceThreads, kSliceEach, kStats>(args, s);
+    launch_slices<T, kSliceThreads, kSliceEach, kWrite>(args, s);
   }
 }
 

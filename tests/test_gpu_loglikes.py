@@ -246,3 +246,21 @@ def test_refusals(wf):
     for scale in (0.0, -1.0, INF, float("nan")):
         with pytest.raises(wf.WdError):
             wf.loglikes(z, scale=scale)
+
+
+@pytest.mark.parametrize("V", [700, 20000, 50000])
+@pytest.mark.parametrize("most", ["history", "biases", "both"])
+def test_lists_beyond_16_bits(wf, V, most):
+    """Histories and bias lists of more than 65535 entries, one label more often than that."""
+    d = make(3, V, F32, seed=20, Q=2)
+    d["request"] = torch.tensor([0, 1, 0], dtype=torch.int32)
+    gen = torch.Generator().manual_seed(21)
+    n = 70000 if most in ("history", "both") else 300
+    ids = torch.randint(0, V, (n + 66000 * (n > 65536),), generator=gen, dtype=torch.int32)
+    ids[n:] = 7
+    d["history"] = (torch.tensor([0, len(ids) - 3, len(ids)]), ids)
+    d["frequency"] = torch.full((2,), 1e-4)
+    m = 70001 if most in ("biases", "both") else 200
+    d["bias"] = (torch.tensor([0, m - 5, m]), torch.randint(0, V, (m,), generator=gen, dtype=torch.int32),
+                 torch.randn(m, generator=gen))
+    check(wf, d)
