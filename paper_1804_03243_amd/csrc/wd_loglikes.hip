@@ -107,7 +107,7 @@ __global__ void __launch_bounds__(THREADS) k_loglikes(ScoreArgs args) {
   for (int j = 0; j < EACH; ++j) z[j] = raw[j / 4].v[j & 3].f();
   const bool has_hist = hist.b < hist.e, has_bias = bias.b < bias.e;  // (the same for the whole workgroup)
   if (LISTS && (has_hist || has_bias)) {
-    const float rho = has_hist && a.repetition ? a.repetition[q] : 1.0f;
+    const float rho = has_hist && a.repetition ? a.repetition[q] : 1.0f, inv_rho = 1.0f / rho;
     const float pres = has_hist && a.presence ? a.presence[q] : 0.0f, freq = has_hist && a.frequency ? a.frequency[q] : 0.0f;
     const auto clear = [&]() {
 #pragma unroll
@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(THREADS) k_loglikes(ScoreArgs args) {
         for (int i = 0; i < 4; ++i) {
           float& x = z[j * 4 + i];
           const uint32_t c = e[i] & counts, p = (uint32_t)((uint64_t)e[i] >> places);
-          if (c) x = (x > 0.0f ? x / rho : x * rho) - (pres + freq * (float)c);
+          if (c) x = x * (x > 0.0f ? inv_rho : rho) - (pres + freq * (float)c);
           if (p) x += a.bias_val[bias.b + (p - 1)];
         }
       }
