@@ -73,10 +73,20 @@ __device__ inline uint2 factor_bits(double f, bool eps, uint32_t lvl) {
 }
 #endif
 
+// A state's arcs in 32 bits: 1 << 30 | the input label of its one arc, 2 << 30 | two
+// labels below 2^15 (the first lower), else their number, kManyArcs where it takes
+// more than 30 bits.
+constexpr uint32_t kManyArcs = (1u << 30) - 1;
+inline uint32_t state_arcs(const int32_t* ilabel, uint32_t n) {
+  if (n == 1) return 1u << 30 | (uint32_t)ilabel[0];
+  if (n == 2 && (ilabel[0] | ilabel[1]) < (1 << 15)) return 2u << 30 | (uint32_t)ilabel[1] << 15 | (uint32_t)ilabel[0];
+  return n < kManyArcs ? n : kManyArcs;
+}
+
 // Device copy of the decoding graph, laid out in one caller-owned buffer.
-//   off[s]  = {first emitting arc, first epsilon arc, first epsilon path, number
-//             of arcs} of state s (S+1 entries; the path index is 0 without a path
-//             table)
+//   off[s]  = {first emitting arc, first epsilon arc, first epsilon path, arcs
+//             (state_arcs)} of state s (S+1 entries; the path index is 0 without a
+//             path table)
 //   earc[i] = {dst, weight bits, ilabel | dst_class << 24, arc id}
 //   xarc[j] = {dst, weight bits, dst_class, arc id}
 //   xnext[j] = epsilon arc range {first, end} of xarc[j]'s destination

@@ -230,7 +230,7 @@ wd_status prepare(const wd_graph_desc* d, Prepared& p, uint64_t* Ae_out, uint64_
   uint64_t Ae = 0, Ax = 0;
   p.off.resize((size_t)S + 1);
   for (int64_t s = 0; s < S; ++s) {
-    p.off[s] = make_uint4((uint32_t)Ae, (uint32_t)Ax, 0, d->row_ptr[s + 1] - d->row_ptr[s]);
+    p.off[s] = make_uint4((uint32_t)Ae, (uint32_t)Ax, 0, state_arcs(d->ilabel + d->row_ptr[s], d->row_ptr[s + 1] - d->row_ptr[s]));
     uint32_t ne = 0, nx = 0;
     for (uint32_t a = d->row_ptr[s]; a < d->row_ptr[s + 1]; ++a) (d->ilabel[a] ? ne : nx)++;
     Ae += ne;

@@ -5,11 +5,12 @@
 //
 // The caller's arcs of a state are a run of the label array (by caller arc
 // id), which starts at the number of emitting plus epsilon arcs before it, so
-// an arc costs a 4-byte read.  A row's bits are gathered in LDS.  Bound by the
-// scattered reads (a state: its offsets, then its labels): what helps is many of
-// them under way, and few addresses per state.  A lane reads up to eight labels of its
-// own state with two loads; what states with more arcs have left is dealt out
-// over the lanes.
+// an arc costs a 4-byte read; one or two arcs (most states of a decoding graph)
+// stand in the state's offset record itself.  A row's bits are gathered in LDS.
+// Bound by the scattered reads, which miss the L2 (16000 sets of 100 states among
+// 500000: @L us; 10 without them).  A lane reads up to eight labels of its own
+// state with two loads; what states with more arcs have left is dealt out over the
+// lanes (300 sets of 20000 states of 3 arcs on average and up to hundreds: @W us).
 #include <algorithm>
 
 #include "wd_host.h"
@@ -26,16 +27,6 @@ struct LabelArgs {
   const int32_t* states;
   uint32_t* mask;
 };
-
-struct Arcs {
-  uint32_t first, count;
-};
-
-__device__ __forceinline__ Arcs arcs_of(const LabelArgs& a, uint32_t s) {
-  if (s >= a.S) return {0, 0};
-  const uint4 o = a.off[s];
-  return {o.x + o.y, o.w};
-}
 
 // Four labels from `at` on, those past the label array's end as epsilon.
 __device__ __forceinline__ Few<int32_t, 4> labels_at(const LabelArgs& a, uint32_t at) {
@@ -54,15 +45,27 @@ __device__ __forceinline__ void add_labels(const LabelArgs& a, uint32_t s, uint3
     const uint32_t l = (uint32_t)label - 1u;  // (epsilon: out of range)
     if (l < a.words * 32u) atomicOr(&bits[l >> 5], 1u << (l & 31));
   };
-  const Arcs r = arcs_of(a, s);
+  uint32_t first = 0, count = 0;
+  if (s < a.S) {
+    const uint4 o = a.off[s];
+    first = o.x + o.y;
+    const uint32_t kind = o.w >> 30;  // (state_arcs)
+    if (kind) {
+      set(kind == 1 ? o.w & 0xffffffu : o.w & 0x7fffu);
+      if (kind == 2) set(o.w >> 15 & 0x7fffu);
+    } else {
+      count = o.w;
+      if (count == kManyArcs) count = a.off[s + 1].x + a.off[s + 1].y - first;
+    }
+  }
   Few<int32_t, 4> v[2] = {};
 #pragma unroll
   for (int k = 0; k < 2; ++k)
-    if (r.count > 4u * k) v[k] = labels_at(a, r.first + 4 * k);
+    if (count > 4u * k) v[k] = labels_at(a, first + 4 * k);
 #pragma unroll
   for (int i = 0; i < (int)kOwnArcs; ++i)
-    if ((uint32_t)i < r.count) set(v[i / 4].v[i & 3]);
-  uint32_t more = r.count > kOwnArcs ? r.count - kOwnArcs : 0, at = r.first + kOwnArcs;
+    if ((uint32_t)i < count) set(v[i / 4].v[i & 3]);
+  uint32_t more = count > kOwnArcs ? count - kOwnArcs : 0, at = first + kOwnArcs;
   while (__any(more != 0)) {
     // item i of the rest belongs to the last lane whose items start at or before i
     const uint32_t now = min(more, 1u << 25);  // (64 lanes' items stay below 2^32)
