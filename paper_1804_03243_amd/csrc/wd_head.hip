@@ -646,6 +646,15 @@ __device__ __forceinline__ void my_tile(uint32_t rows, uint32_t cols, uint32_t& 
   row = first + in % height;
 }
 
+// Adapters of a tile that are steps of its product.  A step more costs a tile of 256
+// rows 1.5 us, add_low about 2 per adapter with the first wait: 64 utterances of 1000 rows
+// 938 us with one adapter in the steps, 906 with two; rows in runs of 32 lose with
+// more (64000 rows: 1218 us by add_low, 1367 in up to eight steps).
+constexpr int kKinds = 2;
+
+// What a lane loads for the terms of another adapter's row.
+__device__ const uint4 k_zeros[kStepK / 8] = {};
+
 // BM rows and BN outputs per workgroup of WM x WN wavefronts.  Two steps of kStepK
 // columns are in LDS.  A step is two halves: while one is multiplied, the next
 // half's operands are read into registers; between the halves of a step every
@@ -698,32 +707,58 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
   };
   stage_x(0, 0);
 
-  // Rows of one adapter: B_g u is a step (or a few) more, of u's terms and B's
-  // columns, whose loads are under way while W x is still multiplied.
-  int low = -1, steps = main;
-  bool mixed = false;
+  // Rows of a few adapters: each adapter's B_g u is a step (or a few) more, of u's
+  // terms and B's columns, whose loads are under way while W x is still multiplied;
+  // the other adapters' rows have zeros for their terms there.
+  int steps = main;
+  bool one = false, mixed = false;  // all rows of one adapter; rows left for add_low
   if (a.adapter) {
-    bool any = false, same = a.rp <= kStepK;
-    low = __builtin_amdgcn_readfirstlane(adapter_of(a, n0));
+    int g[BM / 64], kinds = 0, least = 0;
+    bool fits = a.rp <= kStepK;
+    uint64_t todo[BM / 64];
 #pragma unroll
-    for (int q = 0; q < BM; q += 64) {
-      const int64_t n = n0 + q + lane;
-      const int g = adapter_of(a, n);
-      if (wave == 0) ids[q + lane] = g;
-      any |= g >= 0;
-      same &= g == low || n >= a.N;
-      if (!__is_same(T, Bf16) && g >= 0) same &= a.us[n] == 1.0f;
+    for (int q = 0; q < BM / 64; ++q) {
+      const int64_t n = n0 + q * 64 + lane;
+      g[q] = adapter_of(a, n);
+      if (wave == 0) ids[q * 64 + lane] = g[q];
+      if (!__is_same(T, Bf16) && g[q] >= 0) fits &= a.us[n] == 1.0f;
+      if (g[q] < 0 && n < a.N) least = -1;
+      todo[q] = __ballot(g[q] >= 0);
     }
-    if (__any(any)) {
-      mixed = !__all(same);
-      if (!mixed) steps += a.ul;
+    for (; kinds <= kKinds; ++kinds) {
+      int gg = -1;
+#pragma unroll
+      for (int q = 0; q < BM / 64; ++q)
+        if (todo[q]) gg = __builtin_amdgcn_readlane(g[q], __ffsll((unsigned long long)todo[q]) - 1);
+      if (gg < 0) break;
+#pragma unroll
+      for (int q = 0; q < BM / 64; ++q) todo[q] &= ~__ballot(g[q] == gg);
+      if (threadIdx.x == 0 && kinds < kKinds) ids[BM + kinds] = gg;
     }
+    if (kinds > 0) {
+      one = kinds == 1 && __all(least == 0);
+      mixed = kinds > kKinds || !__all(fits);
+      if (!mixed && !one) {
+        // zeros times an infinite weight would be a NaN in another adapter's row
+        __syncthreads();
+        const int per = a.rp / 8;
+        bool bad = false;
+        for (int i = threadIdx.x; i < kinds * BN * per; i += 64 * kWaves_) {
+          const int r = i % per * 8, p = min(p0 + i / per % BN, P - 1), gg = ids[BM + i / per / BN];
+          bad |= not_finite<T>(load8((const T*)a.h.b + ((int64_t)gg * P + p) * a.h.rank + r, a.h.rank - r));
+        }
+        mixed = __syncthreads_or(bad);
+      }
+      if (!mixed) steps += a.ul * kinds;
+    }
+    __syncthreads();
   }
   const auto stage = [&](int k0, int step) {
     if (k0 < main) return stage_x(k0, step);
-    const int c0 = (k0 - main) / 8, per = a.rp / 8, chunks = a.uk / 8, R = a.h.rank;
-    const uint16_t* ut = a.u + n0 * a.ul + (k0 - main);
-    const T* bt = (const T*)a.h.b + ((int64_t)low * P + p0) * R;
+    const int gg = __builtin_amdgcn_readfirstlane(ids[BM + (k0 - main) / a.ul]), at = (k0 - main) % a.ul;
+    const int c0 = at / 8, per = a.rp / 8, chunks = a.uk / 8, R = a.h.rank;
+    const uint16_t* ut = a.u + n0 * a.ul + at;
+    const T* bt = (const T*)a.h.b + ((int64_t)gg * P + p0) * R;
 #pragma unroll 1
     for (int i = 0; i < kParts; ++i) {
       const int row = (i * kWaves_ + wave) * kPartRows + lane / kChunks, c = (lane % kChunks) ^ swizzle(row);
@@ -735,8 +770,10 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
           load_to_lds(bt, (uint32_t)((b - bt) * 2), to);
         else
           *(uint4*)(lds + step + (i * kWaves_ + wave) * 1024 + lane * 16) = load8(b, R - r);
-      } else {
+      } else if (one || ids[row] == gg) {
         load_to_lds(ut, (uint32_t)((min<int64_t>(row, a.N - 1 - n0) * a.ul + c * 8) * 2), to);
+      } else {
+        load_to_lds(k_zeros, (uint32_t)c * 16, to);
       }
     }
   };
@@ -798,7 +835,7 @@ void launch_tiles(const HeadArgs& a, hipStream_t s) {
   constexpr int each = BM * BN / 256 / (WM * WN), low = (each < 16 ? each : 16) * 1024 * WM * WN;  // (add_low's)
   constexpr int stages = 2 * (BM + BN) * kStepK * 2;
   static_assert(low <= stages, "");
-  constexpr int bytes = stages + BM * 4;
+  constexpr int bytes = stages + (BM + kKinds) * 4;
   static std::atomic<uint64_t> done{0};
   allow_lds((const void*)k, bytes, done);
   hipLaunchKernelGGL(k, dim3(rows * cols), dim3(64 * WM * WN), bytes, s, a, rows, cols);

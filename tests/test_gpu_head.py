@@ -229,3 +229,35 @@ def test_refusals(wf):
     with pytest.raises(wf.WdError):
         wf.Head(on["weight"], None, torch.zeros((1, 129, 64), dtype=BF16, device=DEV),
                 torch.zeros((1, 32, 129), dtype=BF16, device=DEV))
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("run", [1000, 70, 33, 5])
+@pytest.mark.parametrize("N,P,R", [(1300, 1000, 16), (8300, 2100, 8), (8300, 2100, 40), (8300, 2100, 12)])
+def test_runs_of_adapters_in_large_tiles(wf, dtype, run, N, P, R):
+    """Tiles of one, two, several and many adapters, with rows of none between; the same
+    rows come out where another adapter is infinite."""
+    D, G = 72, 40
+    d = make(N, D, P, G, R, dtype, seed=run + R, adapters="runs")
+    d["adapter"] = ((torch.arange(N) // run) % (G + 1)).to(torch.int32)  # (G: out of range, none)
+    head = head_of(wf, d)
+    x, g = d["x"].to(DEV), d["adapter"].to(DEV)
+    y = head.project(x, g)
+    X, W = d["x"].double().to(DEV), d["weight"].double().to(DEV)
+    want = X @ W.T + d["bias"].double().to(DEV)
+    mag = X.abs() @ W.abs().T + d["bias"].double().abs().to(DEV)
+    low = torch.zeros_like(want)
+    for k in range(G):
+        r = g == k
+        A, B, s = d["a"][k].double().to(DEV), d["b"][k].double().to(DEV), float(d["scale"][k])
+        low[r] = s * ((X[r].abs() @ A.abs().T) @ B.abs().T)
+        want[r] += s * ((X[r] @ A.T) @ B.T)
+    bound = (D + 8) * plain.EPS * mag + ((D + 2 * R + 16) * plain.EPS + 2.0 ** -16) * low + plain.EPS * want.abs()
+    off = (y.double() - want).abs() - bound
+    assert float(off.max()) <= 0
+    head._kept[3][3] = float("inf")
+    z = head.project(x, g)
+    hit = g == 3
+    assert not torch.isfinite(z[hit]).any()
+    off = (z[~hit].double() - want[~hit]).abs() - bound[~hit]
+    assert float(off.max()) <= 0
