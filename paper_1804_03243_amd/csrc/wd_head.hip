@@ -690,22 +690,40 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
   const int full = ALIGNED ? D / kStepK * kStepK : 0;  // columns of whole steps, loaded straight to LDS
   const int main = (D + kStepK - 1) / kStepK * kStepK;
+  // Rows that are not aligned for that go through registers, read a half step before
+  // they are put in place.
+  const auto fetch = [&](int k0, int i) {
+    const int row = (i * kWaves_ + wave) * kPartRows + lane / kChunks, k = k0 + ((lane % kChunks) ^ swizzle(row)) * 8;
+    const T* r = row < BM ? xt + min<int64_t>(row, a.N - 1 - n0) * a.x_ld
+                          : wt + (int64_t)min(row - BM, P - 1 - p0) * a.h.weight_ld;
+    return load8(r + k, D - k);
+  };
+  uint4 held[ALIGNED ? 1 : kParts];
+  int held_for = -1;
   const auto stage_x = [&](int k0, int step) {
     if (k0 < full) {
 #pragma unroll
       for (int i = 0; i < kParts; ++i)
         load_to_lds((is_w(i) ? wt : xt) + k0, from[i], __builtin_amdgcn_readfirstlane(lds0 + step + (i * kWaves_ + wave) * 1024));
-    } else {
+    } else if constexpr (ALIGNED) {  // (the last columns)
 #pragma unroll 1
-      for (int i = 0; i < kParts; ++i) {
-        const int row = (i * kWaves_ + wave) * kPartRows + lane / kChunks, c = ((lane % kChunks) ^ swizzle(row)) * 8;
-        const T* r = row < BM ? xt + min<int64_t>(row, a.N - 1 - n0) * a.x_ld
-                              : wt + (int64_t)min(row - BM, P - 1 - p0) * a.h.weight_ld;
-        *(uint4*)(lds + step + (i * kWaves_ + wave) * 1024 + lane * 16) = load8(r + k0 + c, D - k0 - c);
-      }
+      for (int i = 0; i < kParts; ++i) *(uint4*)(lds + step + (i * kWaves_ + wave) * 1024 + lane * 16) = fetch(k0, i);
+    } else {
+#pragma unroll
+      for (int i = 0; i < kParts; ++i) held[i] = fetch(k0, i);
+      held_for = step;
+    }
+  };
+  const auto put = [&]() {  // what was fetched, to its place
+    if constexpr (!ALIGNED) {
+      if (held_for < 0) return;
+#pragma unroll
+      for (int i = 0; i < kParts; ++i) *(uint4*)(lds + held_for + (i * kWaves_ + wave) * 1024 + lane * 16) = held[i];
+      held_for = -1;
     }
   };
   stage_x(0, 0);
+  put();
 
   // Rows of a few adapters: each adapter's B_g u is a step (or a few) more, of u's
   // terms and B's columns, whose loads are under way while W x is still multiplied;
@@ -806,6 +824,7 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
   int now = 0, next = kTile;
   if (kStepK < steps) {
     stage(kStepK, next);
+    put();
     kStepK < full ? loads_left<kParts>() : loads_left<0>();
   } else {
     loads_left<0>();
@@ -817,6 +836,7 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
   for (int k0 = 0; k0 < steps; k0 += kStepK) {
     read(now, 1, odd);
     multiply(even);
+    put();
     loads_left<0>();
     __syncthreads();  // this step has been read, the next one is there
     if (k0 + 2 * kStepK < steps) stage(k0 + 2 * kStepK, now);
@@ -866,6 +886,8 @@ void launch_project(HeadArgs a, hipStream_t s) {
     hipLaunchKernelGGL((k_rows<T, O, 2, false>), outs, block, 0, s, a);
   else if (a.N <= 64)
     hipLaunchKernelGGL((k_rows<T, O, 4, false>), outs, block, 0, s, a);
+  else if (!aligned && tiles(128, 128) >= 192)
+    launch_tiles<T, O, 128, 128, 2, 2, false>(a, s);
   else if (!aligned)
     launch_tiles<T, O, 64, 64, 2, 2, false>(a, s);
   else if (tiles(256, 256) >= 256)
