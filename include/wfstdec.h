@@ -10,7 +10,8 @@
  * final merge (Sec. 3.5),
  * lattice posteriors (Sec. 4.1), the compact exact lattice (Sec. 3.4, on the
  * host), streaming decodes (the integration with acoustic inference the
- * paper leaves to future work, Sec. 5).
+ * paper leaves to future work, Sec. 5), and the operators that make the
+ * log-likelihoods of a model's hidden rows.
  *
  * Conventions for every entry point:
  *  - Return a wd_status; no exception crosses this boundary.  On a non-OK
