@@ -182,16 +182,32 @@ __global__ void __launch_bounds__(256) k_low_tile(HeadArgs a) {
       const T* w[RB];
 #pragma unroll
       for (int b = 0; b < RB; ++b) w[b] = (const T*)a.h.a + ((int64_t)gg * R + min(b * 16 + col, R - 1)) * D;
-      int k = wave * 64 + quad * 16;
-#pragma unroll 4
-      for (; (k & ~63) + 64 <= D; k += 256) {
+      // this wavefront's steps of 64 columns, the reads of some under way together
+      constexpr int kSets = RB <= 2 ? 4 : RB <= 4 ? 2 : 1;
+      const int k1 = wave * 64 + quad * 16, whole = (D - wave * 64) / 64 > 0 ? ((D - wave * 64) / 64 + 3) / 4 : 0;
+      for (int i = 0; i < whole; i += kSets) {
+        uint4 xv[kSets][2], wv[kSets][2][RB];
 #pragma unroll
-        for (int h = 0; h < 16; h += 8) {
-          const uint4 xv = load8(x + k + h, 8);
+        for (int t = 0; t < kSets; ++t)
+          if (i + t < whole) {
 #pragma unroll
-          for (int b = 0; b < RB; ++b) acc[b] = mfma16(load8(w[b] + k + h, 8), xv, acc[b], T{});
-        }
+            for (int h = 0; h < 2; ++h) {
+              const int k = k1 + (i + t) * 256 + h * 8;
+              xv[t][h] = load8(x + k, 8);
+#pragma unroll
+              for (int b = 0; b < RB; ++b) wv[t][h][b] = load8(w[b] + k, 8);
+            }
+          }
+#pragma unroll
+        for (int t = 0; t < kSets; ++t)
+          if (i + t < whole) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+              for (int b = 0; b < RB; ++b) acc[b] = mfma16(wv[t][h][b], xv[t][h], acc[b], T{});
+          }
       }
+      const int k = k1 + whole * 256;
       if ((k & ~63) < D) {
         for (int h = 0; h < 16; h += 8) {
           const uint4 xv = load8(x + k + h, D - k - h);
@@ -705,9 +721,17 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
 #pragma unroll
       for (int i = 0; i < kParts; ++i)
         load_to_lds((is_w(i) ? wt : xt) + k0, from[i], __builtin_amdgcn_readfirstlane(lds0 + step + (i * kWaves_ + wave) * 1024));
-    } else if constexpr (ALIGNED) {  // (the last columns)
+    } else if constexpr (ALIGNED) {  // the last columns, zeros behind them
 #pragma unroll 1
-      for (int i = 0; i < kParts; ++i) *(uint4*)(lds + step + (i * kWaves_ + wave) * 1024 + lane * 16) = fetch(k0, i);
+      for (int i = 0; i < kParts; ++i) {
+        const int row = (i * kWaves_ + wave) * kPartRows + lane / kChunks, c = (lane % kChunks) ^ swizzle(row);
+        const uint32_t to = __builtin_amdgcn_readfirstlane(lds0 + step + (i * kWaves_ + wave) * 1024);
+        const int64_t at = is_w(i) ? min(row - BM, P - 1 - p0) * a.h.weight_ld : min<int64_t>(row, a.N - 1 - n0) * a.x_ld;
+        if (k0 + c * 8 < D)
+          load_to_lds((is_w(i) ? wt : xt) + k0, (uint32_t)((at + c * 8) * 2), to);
+        else
+          load_to_lds(k_zeros, (uint32_t)c * 16, to);
+      }
     } else {
 #pragma unroll
       for (int i = 0; i < kParts; ++i) held[i] = fetch(k0, i);
@@ -786,13 +810,25 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
         const T* b = bt + (int64_t)min(row - BM, P - 1 - p0) * R + r;
         if (a.b16)
           load_to_lds(bt, (uint32_t)((b - bt) * 2), to);
-        else
+        else if (BM * BN > 128 * 128)
           *(uint4*)(lds + step + (i * kWaves_ + wave) * 1024 + lane * 16) = load8(b, R - r);
       } else if (one || ids[row] == gg) {
         load_to_lds(ut, (uint32_t)((min<int64_t>(row, a.N - 1 - n0) * a.ul + c * 8) * 2), to);
       } else {
         load_to_lds(k_zeros, (uint32_t)c * 16, to);
       }
+    }
+    if (BM * BN <= 128 * 128 && !a.b16) {  // (B's rows through registers, where there are some to spare their reads under way together)
+      uint4 v[kParts];
+#pragma unroll
+      for (int i = 0; i < kParts; ++i) {
+        const int row = (i * kWaves_ + wave) * kPartRows + lane / kChunks, c = (lane % kChunks) ^ swizzle(row);
+        const int r = c0 + c < chunks ? (c0 + c) % per * 8 : 0;
+        if (is_w(i)) v[i] = load8(bt + (int64_t)min(row - BM, P - 1 - p0) * R + r, R - r);
+      }
+#pragma unroll
+      for (int i = 0; i < kParts; ++i)
+        if (is_w(i)) *(uint4*)(lds + step + (i * kWaves_ + wave) * 1024 + lane * 16) = v[i];
     }
   };
 
