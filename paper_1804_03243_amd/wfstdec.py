@@ -472,11 +472,17 @@ def wd_result_free(r: int) -> None:
 
 # ---------------------------------------------------------------- helpers
 
+_TORCH = None
+
+
 def _torch():
-    import torch
-    if not torch.cuda.is_available():
-        raise RuntimeError("wfstdec needs a GPU (torch.cuda.is_available() is False)")
-    return torch
+    global _TORCH
+    if _TORCH is None:
+        import torch
+        if not torch.cuda.is_available():
+            raise RuntimeError("wfstdec needs a GPU (torch.cuda.is_available() is False)")
+        _TORCH = torch
+    return _TORCH
 
 
 def _stream(torch):
@@ -540,9 +546,9 @@ class Graph:
         `out`: rows of at least that many words to write into.  Enqueued on
         the current stream."""
         torch = _torch()
-        _vector(offsets, torch.int64, self.device, "offsets")
-        _vector(states, torch.int32, self.device, "states")
-        N, words = offsets.shape[0] - 1, (self.num_pdfs + 31) // 32
+        N, n_states, words = offsets.numel() - 1, states.numel(), (self.num_pdfs + 31) // 32
+        p_off = _vector(offsets, torch.int64, self.device, N + 1, "offsets")
+        p_states = _vector(states, torch.int32, self.device, n_states, "states")
         if N < 0:
             raise ValueError("offsets need at least one entry")
         if out is None:
@@ -552,8 +558,7 @@ class Graph:
             if out.shape[0] != N or out.shape[1] < words:
                 raise ValueError(f"out must be {N} rows of at least {words} words")
         _enqueue(self.device, lambda stream: wd_label_masks(
-            self.handle, N, offsets.data_ptr(), states.data_ptr(), states.shape[0], out.data_ptr(),
-            max(out.stride(0), words), stream))
+            self.handle, N, p_off, p_states, n_states, out.data_ptr(), max(out.stride(0), words), stream))
         return out
 
     def workspace(self, lanes: int, max_T: int, params: wd_params, caps: wd_caps | None):
@@ -768,9 +773,13 @@ def _types(torch):
     return _TYPES
 
 
-def _vector(t, dtype, device, what):
-    if t.dtype != dtype or t.dim() != 1 or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{what} must be a contiguous 1-d {dtype} tensor on {device}")
+def _vector(t, dtype, device, n, what):
+    """Address of a contiguous 1-d tensor of n values; None for None."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.dim() != 1 or t.numel() != n or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{what} must be a contiguous 1-d {dtype} tensor of {n} values on {device}")
+    return t.data_ptr()
 
 
 def _matrix(t, dtypes, device, what):
@@ -800,10 +809,7 @@ class Head:
         _matrix(weight, types, weight.device, "weight")
         P, D = weight.shape
         dev = weight.device
-        if bias is not None:
-            _vector(bias, torch.float32, dev, "bias")
-            if bias.shape[0] != P:
-                raise ValueError(f"bias needs {P} values")
+        _vector(bias, torch.float32, dev, P, "bias")
         if (adapter_a is None) != (adapter_b is None) or adapter_scale is not None and adapter_a is None:
             raise ValueError("adapters need adapter_a and adapter_b")
         G = R = 0
@@ -814,10 +820,7 @@ class Head:
             G, R = adapter_a.shape[:2]
             if tuple(adapter_a.shape) != (G, R, D) or tuple(adapter_b.shape) != (G, P, R):
                 raise ValueError(f"adapters must be [G, R, {D}] and [G, {P}, R]")
-            if adapter_scale is not None:
-                _vector(adapter_scale, torch.float32, dev, "adapter_scale")
-                if adapter_scale.shape[0] != G:
-                    raise ValueError(f"adapter_scale needs {G} values")
+            _vector(adapter_scale, torch.float32, dev, G, "adapter_scale")
         self.D, self.P, self.G, self.R = D, P, G, R
         self.device, self.dtype = dev, weight.dtype
         self._kept = (weight, bias, adapter_a, adapter_b, adapter_scale)
@@ -825,6 +828,7 @@ class Head:
         self.desc = wd_head(D, P, types[weight.dtype], G, R, _ld(weight), ptr(weight), ptr(bias), ptr(adapter_a),
                             ptr(adapter_b), ptr(adapter_scale))
         self._out_types = {torch.float32: WD_F32, weight.dtype: types[weight.dtype]}
+        self._ws_bytes = {}  # by number of rows
         wd_project_workspace_bytes(self.desc, 0)  # the library's checks
 
     def project(self, x, adapter=None, out=None, out_dtype=None):
@@ -837,10 +841,7 @@ class Head:
         N = x.shape[0]
         if x.shape[1] != self.D:
             raise ValueError(f"x must be N x {self.D}")
-        if adapter is not None:
-            _vector(adapter, torch.int32, self.device, "adapter")
-            if adapter.shape[0] != N:
-                raise ValueError(f"adapter needs {N} entries")
+        p_adapter = _vector(adapter, torch.int32, self.device, N, "adapter")
         if out is None:
             out = torch.empty((N, self.P), dtype=torch.float32 if out_dtype is None else out_dtype, device=self.device)
         else:
@@ -849,11 +850,15 @@ class Head:
                 raise ValueError(f"out must be {N} x {self.P} of out_dtype")
         if out.dtype not in self._out_types:
             raise ValueError(f"out_dtype must be float32 or {self.dtype}")
-        nbytes = wd_project_workspace_bytes(self.desc, N) if adapter is not None and self.G else 0
+        nbytes = self._ws_bytes.get(N, -1) if p_adapter is not None and self.G else 0
+        if nbytes < 0:
+            nbytes = wd_project_workspace_bytes(self.desc, N)
+            if len(self._ws_bytes) < 256:
+                self._ws_bytes[N] = nbytes
         ws = torch.empty(nbytes, dtype=torch.uint8, device=self.device) if nbytes else None
         _enqueue(self.device, lambda stream: wd_project(
-            self.desc, x.data_ptr(), _ld(x), N, None if adapter is None else adapter.data_ptr(), out.data_ptr(),
-            _ld(out), self._out_types[out.dtype], None if ws is None else ws.data_ptr(), nbytes, stream))
+            self.desc, x.data_ptr(), _ld(x), N, p_adapter, out.data_ptr(), _ld(out), self._out_types[out.dtype],
+            None if ws is None else ws.data_ptr(), nbytes, stream))
         return out
 
 
@@ -876,66 +881,54 @@ def loglikes(logits, *, normalize: bool = True, scale: float = 1.0, log_prior=No
 
     Returns `out`.  Enqueued on the current stream."""
     torch = _torch()
+    f32, i32, i64 = torch.float32, torch.int32, torch.int64
     types = _types(torch)
     dev = logits.device
     _matrix(logits, types, dev, "logits")
     N, V = logits.shape
-    a = wd_loglikes_args(N=N, V=V, type=types[logits.dtype], logits=logits.data_ptr(), ld=_ld(logits),
-                         normalize=int(bool(normalize)), scale=scale)
-    if log_prior is not None:
-        _vector(log_prior, torch.float32, dev, "log_prior")
-        if log_prior.shape[0] != V:
-            raise ValueError(f"log_prior needs {V} values")
-        a.log_prior = log_prior.data_ptr()
-    for t, what in ((request, "request"), (mask_of, "mask_of"), (out_row, "out_row")):
-        if t is not None:
-            _vector(t, torch.int32, dev, what)
-            if t.shape[0] != N:
-                raise ValueError(f"{what} needs {N} entries")
-            setattr(a, what, t.data_ptr())
-    Q = None
-    for lists, names in ((history, ("hist_off", "hist")), (bias, ("bias_off", "bias_id", "bias_val"))):
-        if lists is None:
-            continue
-        if len(lists) != len(names):
-            raise ValueError("history is (offsets, labels), bias (offsets, labels, values)")
-        for t, name, dtype in zip(lists, names, (torch.int64, torch.int32, torch.float32)):
-            _vector(t, dtype, dev, name)
-            setattr(a, name, t.data_ptr())
-        if any(t.shape[0] != lists[1].shape[0] for t in lists[2:]):
-            raise ValueError("bias needs a value per label")
-        q = lists[0].shape[0] - 1
-        if q < 1 or Q not in (None, q):
-            raise ValueError("history and bias need offsets of the same requests, one more than requests")
-        Q = q
-    for t, what in ((repetition, "repetition"), (presence, "presence"), (frequency, "frequency")):
-        if t is not None:
-            if history is None:
-                raise ValueError(f"{what} needs a history")
-            _vector(t, torch.float32, dev, what)
-            if t.shape[0] != Q:
-                raise ValueError(f"{what} needs {Q} values")
-            setattr(a, what, t.data_ptr())
-    a.n_requests = Q or 0
-    a.n_hist = 0 if history is None else history[1].shape[0]
-    a.n_bias = 0 if bias is None else bias[1].shape[0]
+    p_prior = _vector(log_prior, f32, dev, V, "log_prior")
+    p_request, p_mask_of = _vector(request, i32, dev, N, "request"), _vector(mask_of, i32, dev, N, "mask_of")
+    p_row = _vector(out_row, i32, dev, N, "out_row")
+    Q = n_hist = n_bias = 0
+    p_hoff = p_hist = p_rep = p_pres = p_freq = p_boff = p_bid = p_bval = None
+    if history is not None:
+        off, ids = history
+        Q, n_hist = off.numel() - 1, ids.numel()
+        p_hoff, p_hist = _vector(off, i64, dev, Q + 1, "history's offsets"), _vector(ids, i32, dev, n_hist, "history's labels")
+        p_rep, p_pres = _vector(repetition, f32, dev, Q, "repetition"), _vector(presence, f32, dev, Q, "presence")
+        p_freq = _vector(frequency, f32, dev, Q, "frequency")
+    elif repetition is not None or presence is not None or frequency is not None:
+        raise ValueError("penalties need a history")
+    if bias is not None:
+        off, ids, values = bias
+        if history is None:
+            Q = off.numel() - 1
+        n_bias = ids.numel()
+        p_boff, p_bid = _vector(off, i64, dev, Q + 1, "bias's offsets"), _vector(ids, i32, dev, n_bias, "bias's labels")
+        p_bval = _vector(values, f32, dev, n_bias, "bias's values")
+    if Q < 1 and (history is not None or bias is not None):
+        raise ValueError("history and bias need offsets, one more than requests")
+    p_mask, n_masks, mask_ld = None, 0, 0
     if mask is not None:
-        _matrix(mask, (torch.int32,), dev, "mask")
+        _matrix(mask, (i32,), dev, "mask")
+        n_masks = mask.shape[0]
         if mask.shape[1] < (V + 31) // 32:
             raise ValueError(f"mask needs {(V + 31) // 32} words per row")
-        a.mask, a.n_masks, a.mask_ld = mask.data_ptr(), mask.shape[0], _ld(mask)
+        p_mask, mask_ld = mask.data_ptr(), _ld(mask)
     elif mask_of is not None:
         raise ValueError("mask_of needs a mask")
     if out is None:
         if out_row is not None:
             raise ValueError("out_row needs out")
-        out = torch.empty((N, V), dtype=torch.float32, device=dev)
+        out = torch.empty((N, V), dtype=f32, device=dev)
     else:
-        _matrix(out, (torch.float32,), dev, "out")
+        _matrix(out, (f32,), dev, "out")
         if out.shape[1] != V or out_row is None and out.shape[0] != N:
             raise ValueError(f"out must be rows of {V} float32, {N} of them without out_row")
-    a.out, a.out_ld, a.out_rows = out.data_ptr(), _ld(out), out.shape[0]
-    nbytes = wd_loglikes_workspace_bytes(a)
+    a = wd_loglikes_args(N, V, types[logits.dtype], logits.data_ptr(), _ld(logits), 1 if normalize else 0, scale, p_prior, Q,
+                         p_request, p_hoff, p_hist, n_hist, p_rep, p_pres, p_freq, p_boff, p_bid, p_bval, n_bias, p_mask,
+                         n_masks, mask_ld, p_mask_of, out.data_ptr(), _ld(out), out.shape[0], p_row)
+    nbytes = wd_loglikes_workspace_bytes(a) if V > 8192 else 0  # (shorter rows need none)
     ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
     _enqueue(dev, lambda stream: wd_loglikes(a, None if ws is None else ws.data_ptr(), nbytes, stream))
     return out
