@@ -72,13 +72,22 @@ __device__ __forceinline__ void add_labels(const LabelArgs& a, uint32_t s, uint3
     const uint32_t end = wave_incl_scan(now), total = lane63(end), start = end - now;
     deal[lane_id()] = make_uint2(start, at - start);
     __builtin_amdgcn_wave_barrier();
-    for (uint32_t i = lane_id(); i < total; i += 64) {
+    const auto arc = [&](uint32_t i) {
       uint32_t owner = 0;
 #pragma unroll
       for (uint32_t step = 32; step > 0; step >>= 1)
         if (deal[owner + step].x <= i) owner += step;
-      set(a.ilabel[i + deal[owner].y]);
+      return i + deal[owner].y;
+    };
+    uint32_t i = lane_id();
+    for (; (i | 63) + 192 < total; i += 256) {  // (four reads under way)
+      int32_t l[4];
+#pragma unroll
+      for (uint32_t k = 0; k < 4; ++k) l[k] = a.ilabel[arc(i + 64 * k)];
+#pragma unroll
+      for (uint32_t k = 0; k < 4; ++k) set(l[k]);
     }
+    for (; i < total; i += 64) set(a.ilabel[arc(i)]);
     __builtin_amdgcn_wave_barrier();
     more -= now;
     at += now;
