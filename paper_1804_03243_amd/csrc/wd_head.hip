@@ -56,15 +56,67 @@ __device__ __forceinline__ int adapter_of(const HeadArgs& a, int64_t n) {
   return g >= 0 && g < a.h.n_adapters ? g : -1;
 }
 
-// Eight elements at p, those from `n` on as zero.
+// Rows that do not end at a multiple of eight elements are read with loads that
+// stay in the array: raw8 reads eight elements from p, or the array's last eight
+// (at `last`) where that would pass its end, and fix8 moves them to their places and
+// puts zeros from element n on.  Reads first, then the moves: several reads are under
+// way together.  (Element by element, under a branch each, 78 rows of 1133 -> 1516 with
+// as many adapters of rank 38 took 72 us for 60, 2548 of 67 -> 7042 41 for 36.)
+// Arrays of fewer than eight elements go to k_tiny.
 template <class T>
-__device__ __forceinline__ uint4 load8(const T* p, int n) {
-  if (n >= 8) return __builtin_bit_cast(uint4, *(const Few<T, 8>*)p);
+__device__ __forceinline__ uint4 load8(const T* p) {
+  return __builtin_bit_cast(uint4, *(const Few<T, 8>*)p);
+}
+
+template <class T>
+__device__ __forceinline__ uint4 raw8(const T* p, const T* last) {
+  return load8(p < last ? p : last);
+}
+
+template <class T>
+__device__ __forceinline__ uint4 fix8(uint4 v, const T* p, int n, const T* last) {
+  const int by = p > last ? (int)min(p - last, (ptrdiff_t)8) : 0;  // elements to move down
+  uint64_t lo = (uint64_t)v.y << 32 | v.x, hi = (uint64_t)v.w << 32 | v.z;
+  if (by & 4) lo = hi, hi = 0;
+  const int r = (by & 3) * 16;
+  lo = lo >> r | (hi << 1) << (63 - r);
+  hi >>= r;
+  const auto low = [](int k) { return k >= 4 ? ~0ull : k <= 0 ? 0ull : (1ull << (16 * k)) - 1; };
+  const int keep = by == 8 ? 0 : n;
+  lo &= low(keep);
+  hi &= low(keep - 4);
+  return make_uint4((uint32_t)lo, (uint32_t)(lo >> 32), (uint32_t)hi, (uint32_t)(hi >> 32));
+}
+
+// The first n of eight elements, one by one, and zeros: for the largest tiles, which
+// have no registers left to move elements in (64000 rows of 32 per adapter took 1470
+// us with raw8 and fix8, and take 1220).
+template <class T>
+__device__ __forceinline__ uint4 few8(const T* p, int n) {
+  if (n >= 8) return load8(p);
   Few<T, 8> v{};
 #pragma unroll
   for (int i = 0; i < 8; ++i)
     if (i < n) v.v[i] = p[i];
   return __builtin_bit_cast(uint4, v);
+}
+
+// The last eight elements of x, W, A and B.
+template <class T>
+__device__ __forceinline__ const T* last_x(const HeadArgs& a) {
+  return (const T*)a.x + (a.N - 1) * a.x_ld + a.h.D - 8;
+}
+template <class T>
+__device__ __forceinline__ const T* last_w(const HeadArgs& a) {
+  return (const T*)a.h.weight + (a.h.P - 1) * a.h.weight_ld + a.h.D - 8;
+}
+template <class T>
+__device__ __forceinline__ const T* last_a(const HeadArgs& a) {
+  return (const T*)a.h.a + (int64_t)a.h.n_adapters * a.h.rank * a.h.D - 8;
+}
+template <class T>
+__device__ __forceinline__ const T* last_b(const HeadArgs& a) {
+  return (const T*)a.h.b + (int64_t)a.h.n_adapters * a.h.P * a.h.rank - 8;
 }
 
 // The terms of one value; an infinity or NaN is its first term.
@@ -104,11 +156,20 @@ __device__ __forceinline__ float finite_abs(float u) { return fabsf(u) < INFINIT
 
 // The products of a row of n elements with two others, by a wavefront.
 template <class T>
-__device__ __forceinline__ void row_products(const T* x, const T* w0, const T* w1, int n, float& s0, float& s1) {
+__device__ __forceinline__ void row_products(const T* x, const T* sx, const T* w0, const T* w1, const T* sw, int n,
+                                             float& s0, float& s1) {
   s0 = s1 = 0.0f;
 #pragma unroll 2
   for (int k = (threadIdx.x & 63) * 8; k < n; k += 512) {
-    const uint4 xv = load8(x + k, n - k), v0 = load8(w0 + k, n - k), v1 = load8(w1 + k, n - k);
+    uint4 xv, v0, v1;
+    if (n % 8 == 0) {
+      xv = load8(x + k), v0 = load8(w0 + k), v1 = load8(w1 + k);
+    } else {
+      xv = raw8(x + k, sx), v0 = raw8(w0 + k, sw), v1 = raw8(w1 + k, sw);
+      xv = fix8(xv, x + k, n - k, sx);
+      v0 = fix8(v0, w0 + k, n - k, sw);
+      v1 = fix8(v1, w1 + k, n - k, sw);
+    }
     const T *xe = (const T*)&xv, *e0 = (const T*)&v0, *e1 = (const T*)&v1;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
@@ -140,7 +201,7 @@ __global__ void __launch_bounds__(512) k_low_row(HeadArgs a) {
   const float sc = a.h.scale ? a.h.scale[g] : 1.0f;
   for (int r = wave * 2; r < R; r += 16) {
     float s0, s1;
-    row_products(x, w + (int64_t)r * D, w + (int64_t)min(r + 1, R - 1) * D, D, s0, s1);
+    row_products(x, last_x<T>(a), w + (int64_t)r * D, w + (int64_t)min(r + 1, R - 1) * D, last_a<T>(a), D, s0, s1);
     if (lane < 2 && r + lane < R) us[r + lane] = (lane ? s1 : s0) * sc;
   }
   __syncthreads();
@@ -193,9 +254,9 @@ __global__ void __launch_bounds__(256) k_low_tile(HeadArgs a) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
               const int k = k1 + (i + t) * 256 + h * 8;
-              xv[t][h] = load8(x + k, 8);
+              xv[t][h] = load8(x + k);
 #pragma unroll
-              for (int b = 0; b < RB; ++b) wv[t][h][b] = load8(w[b] + k, 8);
+              for (int b = 0; b < RB; ++b) wv[t][h][b] = load8(w[b] + k);
             }
           }
 #pragma unroll
@@ -209,10 +270,20 @@ __global__ void __launch_bounds__(256) k_low_tile(HeadArgs a) {
       }
       const int k = k1 + whole * 256;
       if ((k & ~63) < D) {
-        for (int h = 0; h < 16; h += 8) {
-          const uint4 xv = load8(x + k + h, D - k - h);
+        const T *sx = last_x<T>(a), *sa = last_a<T>(a);
+        uint4 xv[2], wv[2][RB];
 #pragma unroll
-          for (int b = 0; b < RB; ++b) acc[b] = mfma16(load8(w[b] + k + h, D - k - h), xv, acc[b], T{});
+        for (int h = 0; h < 2; ++h) {
+          xv[h] = raw8(x + k + h * 8, sx);
+#pragma unroll
+          for (int b = 0; b < RB; ++b) wv[h][b] = raw8(w[b] + k + h * 8, sa);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int left = D - k - h * 8;
+          xv[h] = fix8(xv[h], x + k + h * 8, left, sx);
+#pragma unroll
+          for (int b = 0; b < RB; ++b) acc[b] = mfma16(fix8(wv[h][b], w[b] + k + h * 8, left, sa), xv[h], acc[b], T{});
         }
       }
 #pragma unroll
@@ -229,7 +300,7 @@ __global__ void __launch_bounds__(256) k_low_tile(HeadArgs a) {
       const T* w = (const T*)a.h.a + (int64_t)gg * R * D;
       for (int r = 0; r < R; r += 2) {
         float s0, s1;
-        row_products(x, w + (int64_t)r * D, w + (int64_t)min(r + 1, R - 1) * D, D, s0, s1);
+        row_products(x, last_x<T>(a), w + (int64_t)r * D, w + (int64_t)min(r + 1, R - 1) * D, last_a<T>(a), D, s0, s1);
         // (the other wavefronts' parts of these sums are zero)
         if (lane < 8 && r + (lane >> 2) < R) sums[lane & 3][i][r + (lane >> 2)] = lane == 0 ? s0 : lane == 4 ? s1 : 0.0f;
       }
@@ -286,14 +357,12 @@ __device__ __forceinline__ f32x4 low_of_row(const HeadArgs& a, int64_t n, int g,
   if (g < 0 || p >= a.h.P) return low;
   const T* b = (const T*)a.h.b + ((int64_t)g * a.h.P + p) * R;
   const uint16_t* ut = a.u + n * a.ul;
+  const T* sb = last_b<T>(a);
   const int last = a.h.P - 1 - p;  // rows of B past the last are not read
-#pragma unroll AHEAD
-  for (int r = 0; r < R; r += 8) {
-    uint4 t[TERMS], w[4];
+  const auto add = [&](int r, const uint4 (&w)[4]) {
+    uint4 t[TERMS];
 #pragma unroll
     for (int k = 0; k < TERMS; ++k) t[k] = *(const uint4*)(ut + k * a.rp + r);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] = load8(b + (int64_t)min(e, last) * R + r, R - r);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       float u = ((const T*)&t[TERMS - 1])[i].f();
@@ -302,6 +371,21 @@ __device__ __forceinline__ f32x4 low_of_row(const HeadArgs& a, int64_t n, int g,
 #pragma unroll
       for (int e = 0; e < 4; ++e) low[e] = fmaf(((const T*)&w[e])[i].f(), u, low[e]);
     }
+  };
+  uint4 w[4];
+  int r = 0;
+#pragma unroll AHEAD
+  for (; r + 8 <= R; r += 8) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = load8(b + (int64_t)min(e, last) * R + r);
+    add(r, w);
+  }
+  if (r < R) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = raw8(b + (int64_t)min(e, last) * R + r, sb);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = fix8(w[e], b + (int64_t)min(e, last) * R + r, R - r, sb);
+    add(r, w);
   }
   return low;
 }
@@ -371,13 +455,19 @@ __device__ __forceinline__ void add_low(const HeadArgs& a, int64_t n0, const int
 #pragma unroll
     for (int i = 0; i < TM; ++i) by_row |= (all_by_row ? g[i] >= 0 : g[i] == gg) << i;
   };
+  constexpr bool kSlim = TM * TN >= 32;
+  const T* sb = last_b<T>(a);
+  const auto b_part = [&](int gg, int p, int r) {
+    const T* b = (const T*)a.h.b + ((int64_t)gg * P + p) * R + r;
+    return kSlim ? few8(b, R - r) : fix8(raw8(b, sb), b, R - r, sb);
+  };
   const auto usable = [&](int gg) {  // whether an adapter's weights for these outputs are finite
     bool bad = false;
 #pragma unroll 1
     for (int r = quad * 8; r < R; r += 32)
 #pragma unroll
       for (int j = 0; j < TN; ++j)
-        bad |= not_finite<T>(load8((const T*)a.h.b + ((int64_t)gg * P + min(prow(j, col), P - 1)) * R + r, R - r));
+        bad |= not_finite<T>(b_part(gg, min(prow(j, col), P - 1), r));
     if (!__any(bad)) return true;
     leave(gg);
     return false;
@@ -395,11 +485,18 @@ __device__ __forceinline__ void add_low(const HeadArgs& a, int64_t n0, const int
     const T* B = (const T*)a.h.b + (int64_t)gg * P * R + r;
     uint4 b[TN], u[TM];
 #pragma unroll
-    for (int j = 0; j < TN; ++j) b[j] = load8(B + (int64_t)min(prow(j, col), P - 1) * R, R - r);
+    for (int j = 0; j < TN; ++j) {
+      const T* from = B + (int64_t)min(prow(j, col), P - 1) * R;
+      b[j] = kSlim ? few8(from, R - r) : raw8(from, sb);
+    }
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
       const int64_t n = n0 + i * 16 + col;
       u[i] = *(const uint4*)(a.u + (n < a.N ? n : a.N - 1) * a.ul + c * 8);
+    }
+    if (!kSlim && R % 8) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j) b[j] = fix8(b[j], B + (int64_t)min(prow(j, col), P - 1) * R, R - r, sb);
     }
     if (per <= 4 && kk == 0) {  // (all of the adapter's columns are here)
       bool bad = false;
@@ -515,6 +612,9 @@ __device__ __forceinline__ void finish_tile(const HeadArgs& a, int64_t n0, int p
 // does not see this load (its builtin makes every LDS read wait for all of them):
 // the data is there after loads_left() and a barrier.
 __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t to) {
+  const uint64_t p = (uint64_t)base;  // (into scalar registers, where the compiler would not hold it there)
+  base = (const void*)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(p >> 32)) << 32 |
+                       (uint32_t)__builtin_amdgcn_readfirstlane((int)p));
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(to)
                : "memory");
 }
@@ -524,7 +624,7 @@ __device__ __forceinline__ void loads_left() {
   asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
-// Few rows (up to 16 * NB): what counts is that W streams through the chip once.
+// Few rows (16 * NB to a workgroup): what counts is that W streams through the chip once.
 // A workgroup takes 32 outputs of every row, its eight wavefronts a part of the
 // columns each; the operands come straight from memory (x from the caches), 128
 // bytes of a row between the lanes, and the parts are added through LDS.
@@ -536,14 +636,14 @@ __global__ void __launch_bounds__(512) k_rows(HeadArgs a) {
   __shared__ f32x4 part[8][NB * 2][64];
   __shared__ float low_u[FEW ? kFewRows : 1][FEW ? WD_MAX_RANK : 1];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
-  const int D = a.h.D, P = a.h.P, p0 = blockIdx.x * 32;
+  const int D = a.h.D, P = a.h.P, p0 = blockIdx.x * 32, n0 = blockIdx.y * NB * 16;
   const T *w[2], *x[NB];
 #pragma unroll
   for (int j = 0; j < 2; ++j) w[j] = (const T*)a.h.weight + (int64_t)min(p0 + j * 16 + col, P - 1) * a.h.weight_ld;
 #pragma unroll
-  for (int i = 0; i < NB; ++i) x[i] = (const T*)a.x + min<int64_t>(i * 16 + col, a.N - 1) * a.x_ld;
+  for (int i = 0; i < NB; ++i) x[i] = (const T*)a.x + min<int64_t>(n0 + i * 16 + col, a.N - 1) * a.x_ld;
   // the row and the outputs that this lane finishes
-  const int fi = (wave >> 1) * 16 + col, fp = p0 + (wave & 1) * 16 + quad * 4;
+  const int fi = n0 + (wave >> 1) * 16 + col, fp = p0 + (wave & 1) * 16 + quad * 4;
   const int g = wave < NB * 2 ? adapter_of(a, fi) : -1;
   struct Operands {
     uint4 w[2][2], x[2][NB];
@@ -552,9 +652,9 @@ __global__ void __launch_bounds__(512) k_rows(HeadArgs a) {
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
 #pragma unroll
-      for (int j = 0; j < 2; ++j) o.w[h][j] = load8(w[j] + k + h * 8, 8);
+      for (int j = 0; j < 2; ++j) o.w[h][j] = load8(w[j] + k + h * 8);
 #pragma unroll
-      for (int i = 0; i < NB; ++i) o.x[h][i] = load8(x[i] + k + h * 8, 8);
+      for (int i = 0; i < NB; ++i) o.x[h][i] = load8(x[i] + k + h * 8);
     }
   };
   f32x4 acc[NB][2] = {};
@@ -580,7 +680,7 @@ __global__ void __launch_bounds__(512) k_rows(HeadArgs a) {
       if (gn < 0) continue;
       const T* w0 = (const T*)a.h.a + ((int64_t)gn * R + r) * D;
       float s0, s1;
-      row_products((const T*)a.x + n * a.x_ld, w0, w0 + (r + 1 < R ? D : 0), D, s0, s1);
+      row_products((const T*)a.x + n * a.x_ld, last_x<T>(a), w0, w0 + (r + 1 < R ? D : 0), last_a<T>(a), D, s0, s1);
       const float sc = a.h.scale ? a.h.scale[gn] : 1.0f;
       if (lane < 2 && r + lane < R) low_u[n][r + lane] = (lane ? s1 : s0) * sc;
     }
@@ -601,18 +701,23 @@ __global__ void __launch_bounds__(512) k_rows(HeadArgs a) {
   }
   const int k = k1 + whole * step;
   if ((k & ~63) < D) {
+    const T *sw = last_w<T>(a), *sx = last_x<T>(a);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+      for (int j = 0; j < 2; ++j) o0.w[h][j] = raw8(w[j] + k + h * 8, sw);
+#pragma unroll
+      for (int i = 0; i < NB; ++i) o0.x[h][i] = raw8(x[i] + k + h * 8, sx);
+    }
+#pragma unroll
     for (int h = 0; h < 2; ++h) {
       const int left = D - k - h * 8;
-      uint4 wv[2];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) wv[j] = load8(w[j] + k + h * 8, left);
+      for (int j = 0; j < 2; ++j) o0.w[h][j] = fix8(o0.w[h][j], w[j] + k + h * 8, left, sw);
 #pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        const uint4 xv = load8(x[i] + k + h * 8, left);
-#pragma unroll
-        for (int j = 0; j < 2; ++j) acc[i][j] = mfma16(wv[j], xv, acc[i][j], T{});
-      }
+      for (int i = 0; i < NB; ++i) o0.x[h][i] = fix8(o0.x[h][i], x[i] + k + h * 8, left, sx);
     }
+    multiply(o0);
   }
 #pragma unroll
   for (int i = 0; i < NB; ++i)
@@ -629,7 +734,7 @@ __global__ void __launch_bounds__(512) k_rows(HeadArgs a) {
     for (int e = 0; e < 4; ++e) {
       const T* be = b + (int64_t)min(e, P - 1 - fp) * a.h.rank;
       for (int r = 0; r < a.h.rank; r += 8) {
-        const uint4 v = load8(be + r, a.h.rank - r);
+        const uint4 v = a.h.rank % 8 == 0 ? load8(be + r) : fix8(raw8(be + r, last_b<T>(a)), be + r, a.h.rank - r, last_b<T>(a));
 #pragma unroll
         for (int i = 0; i < 8; ++i) low[e] = fmaf(((const T*)&v)[i].f(), r + i < a.h.rank ? low_u[fi][r + i] : 0.0f, low[e]);
       }
@@ -678,6 +783,7 @@ __device__ const uint4 k_zeros[kStepK / 8] = {};
 template <class T, class O, int BM, int BN, int WM, int WN, bool ALIGNED>
 __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2) k_project(HeadArgs a, uint32_t row_tiles, uint32_t col_tiles) {
   constexpr int kWaves_ = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
+  constexpr bool kSlim = BM * BN > 128 * 128;
   constexpr int kRowBytes = kStepK * 2, kChunks = kStepK / 8, kPartRows = 64 / kChunks;
   constexpr int kTile = (BM + BN) * kRowBytes;
   constexpr int kParts = kTile / 1024 / kWaves_;  // loads of a wavefront per step
@@ -708,14 +814,12 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
   const int main = (D + kStepK - 1) / kStepK * kStepK;
   // Rows that are not aligned for that go through registers, read a half step before
   // they are put in place.
-  const auto fetch = [&](int k0, int i) {
+  const auto source = [&](int k0, int i) {
     const int row = (i * kWaves_ + wave) * kPartRows + lane / kChunks, k = k0 + ((lane % kChunks) ^ swizzle(row)) * 8;
-    const T* r = row < BM ? xt + min<int64_t>(row, a.N - 1 - n0) * a.x_ld
-                          : wt + (int64_t)min(row - BM, P - 1 - p0) * a.h.weight_ld;
-    return load8(r + k, D - k);
+    return k + (row < BM ? xt + min<int64_t>(row, a.N - 1 - n0) * a.x_ld : wt + (int64_t)min(row - BM, P - 1 - p0) * a.h.weight_ld);
   };
   uint4 held[ALIGNED ? 1 : kParts];
-  int held_for = -1;
+  int held_for = -1, held_k = 0;
   const auto stage_x = [&](int k0, int step) {
     if (k0 < full) {
 #pragma unroll
@@ -734,13 +838,21 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
       }
     } else {
 #pragma unroll
-      for (int i = 0; i < kParts; ++i) held[i] = fetch(k0, i);
+      for (int i = 0; i < kParts; ++i) held[i] = is_w(i) ? raw8(source(k0, i), last_w<T>(a)) : raw8(source(k0, i), last_x<T>(a));
       held_for = step;
+      held_k = k0;
     }
   };
   const auto put = [&]() {  // what was fetched, to its place
     if constexpr (!ALIGNED) {
       if (held_for < 0) return;
+      if (held_k + kStepK > D) {  // (the row's last columns)
+#pragma unroll
+        for (int i = 0; i < kParts; ++i) {
+          const int row = (i * kWaves_ + wave) * kPartRows + lane / kChunks, k = held_k + ((lane % kChunks) ^ swizzle(row)) * 8;
+          held[i] = is_w(i) ? fix8(held[i], source(held_k, i), D - k, last_w<T>(a)) : fix8(held[i], source(held_k, i), D - k, last_x<T>(a));
+        }
+      }
 #pragma unroll
       for (int i = 0; i < kParts; ++i) *(uint4*)(lds + held_for + (i * kWaves_ + wave) * 1024 + lane * 16) = held[i];
       held_for = -1;
@@ -787,7 +899,8 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
         bool bad = false;
         for (int i = threadIdx.x; i < kinds * BN * per; i += 64 * kWaves_) {
           const int r = i % per * 8, p = min(p0 + i / per % BN, P - 1), gg = ids[BM + i / per / BN];
-          bad |= not_finite<T>(load8((const T*)a.h.b + ((int64_t)gg * P + p) * a.h.rank + r, a.h.rank - r));
+          const T* b = (const T*)a.h.b + ((int64_t)gg * P + p) * a.h.rank + r;
+          bad |= not_finite<T>(kSlim ? few8(b, a.h.rank - r) : fix8(raw8(b, last_b<T>(a)), b, a.h.rank - r, last_b<T>(a)));
         }
         mixed = __syncthreads_or(bad);
       }
@@ -810,25 +923,30 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
         const T* b = bt + (int64_t)min(row - BM, P - 1 - p0) * R + r;
         if (a.b16)
           load_to_lds(bt, (uint32_t)((b - bt) * 2), to);
-        else if (BM * BN > 128 * 128)
-          *(uint4*)(lds + step + (i * kWaves_ + wave) * 1024 + lane * 16) = load8(b, R - r);
+        else if (kSlim)
+          *(uint4*)(lds + step + (i * kWaves_ + wave) * 1024 + lane * 16) = few8(b, R - r);
       } else if (one || ids[row] == gg) {
         load_to_lds(ut, (uint32_t)((min<int64_t>(row, a.N - 1 - n0) * a.ul + c * 8) * 2), to);
       } else {
         load_to_lds(k_zeros, (uint32_t)c * 16, to);
       }
     }
-    if (BM * BN <= 128 * 128 && !a.b16) {  // (B's rows through registers, where there are some to spare their reads under way together)
+    if (!kSlim && !a.b16) {  // (B's rows through registers, where there are some to spare their reads under way together)
       uint4 v[kParts];
 #pragma unroll
       for (int i = 0; i < kParts; ++i) {
         const int row = (i * kWaves_ + wave) * kPartRows + lane / kChunks, c = (lane % kChunks) ^ swizzle(row);
         const int r = c0 + c < chunks ? (c0 + c) % per * 8 : 0;
-        if (is_w(i)) v[i] = load8(bt + (int64_t)min(row - BM, P - 1 - p0) * R + r, R - r);
+        if (is_w(i)) v[i] = raw8(bt + (int64_t)min(row - BM, P - 1 - p0) * R + r, last_b<T>(a));
       }
 #pragma unroll
-      for (int i = 0; i < kParts; ++i)
-        if (is_w(i)) *(uint4*)(lds + step + (i * kWaves_ + wave) * 1024 + lane * 16) = v[i];
+      for (int i = 0; i < kParts; ++i) {
+        const int row = (i * kWaves_ + wave) * kPartRows + lane / kChunks, c = (lane % kChunks) ^ swizzle(row);
+        const int r = c0 + c < chunks ? (c0 + c) % per * 8 : 0;
+        if (is_w(i))
+          *(uint4*)(lds + step + (i * kWaves_ + wave) * 1024 + lane * 16) =
+              fix8(v[i], bt + (int64_t)min(row - BM, P - 1 - p0) * R + r, R - r, last_b<T>(a));
+      }
     }
   };
 
@@ -897,8 +1015,35 @@ void launch_tiles(const HeadArgs& a, hipStream_t s) {
   hipLaunchKernelGGL(k, dim3(rows * cols), dim3(64 * WM * WN), bytes, s, a, rows, cols);
 }
 
+// A thread per output, for heads whose arrays are too small for loads of eight
+// elements: the formula as it stands.
+template <class T, class O>
+__global__ void __launch_bounds__(256) k_tiny(HeadArgs a) {
+  const int D = a.h.D, R = a.h.rank;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.N * a.h.P; i += (int64_t)gridDim.x * 256) {
+    const int64_t n = i / a.h.P;
+    const int p = (int)(i % a.h.P), g = adapter_of(a, n);
+    const T *x = (const T*)a.x + n * a.x_ld, *w = (const T*)a.h.weight + p * a.h.weight_ld;
+    float y = 0.0f, low = 0.0f;
+    for (int k = 0; k < D; ++k) y = fmaf(x[k].f(), w[k].f(), y);
+    for (int r = 0; g >= 0 && r < R; ++r) {
+      const T* ar = (const T*)a.h.a + ((int64_t)g * R + r) * D;
+      float u = 0.0f;
+      for (int k = 0; k < D; ++k) u = fmaf(x[k].f(), ar[k].f(), u);
+      low = fmaf(a.h.scale ? a.h.scale[g] * u : u, ((const T*)a.h.b)[((int64_t)g * a.h.P + p) * R + r].f(), low);
+    }
+    ((O*)a.out)[n * a.out_ld + p] = O::of(y + low + (a.h.bias ? a.h.bias[p] : 0.0f));
+  }
+}
+
 template <class T, class O>
 void launch_project(HeadArgs a, hipStream_t s) {
+  const int64_t G = a.adapter ? a.h.n_adapters : 8, R = a.adapter ? a.h.rank : 8;
+  if ((a.h.D < 8 && (a.N == 1 || a.h.P == 1)) || G * R * a.h.D < 8 || G * R * a.h.P < 8) {
+    const uint64_t blocks = ((uint64_t)a.N * a.h.P + 255) / 256;
+    hipLaunchKernelGGL((k_tiny<T, O>), dim3((uint32_t)std::min<uint64_t>(blocks, 1 << 16)), dim3(256), 0, s, a);
+    return;
+  }
   const dim3 outs(((uint32_t)a.h.P + 31) / 32), block(512);
   if (a.adapter && a.N <= kFewRows) {
     hipLaunchKernelGGL((k_rows<T, O, 1, true>), outs, block, 0, s, a);
@@ -916,12 +1061,19 @@ void launch_project(HeadArgs a, hipStream_t s) {
                        !((uintptr_t)a.h.weight & 15);
   a.stream = (uint64_t)a.N * a.h.P * sizeof(O) >= (256u << 20);
   const auto tiles = [&](int64_t m, int64_t n) { return ((a.N + m - 1) / m) * ((a.h.P + n - 1) / n); };
+  // Rows of many adapters each in a small output stay with k_rows while its workgroups
+  // are one per compute unit at most: 128 rows of as many adapters, 512 -> 3000, take
+  // 13.0 us and in tiles 18.8, 256 of 300 -> 1500 13.3 and 20.5; past that the tiles
+  // are ahead (256 of 1024 -> 6000 33 us for 41), and for rows of one adapter throughout
+  // (128 of 1133 -> 1516 24 us for 30).
+  const bool many = a.adapter && (int64_t)a.h.n_adapters * 16 > a.N;
+  const int64_t blocks64 = (a.N + 63) / 64;
   if (a.N <= 16)
     hipLaunchKernelGGL((k_rows<T, O, 1, false>), outs, block, 0, s, a);
   else if (a.N <= 32)
     hipLaunchKernelGGL((k_rows<T, O, 2, false>), outs, block, 0, s, a);
-  else if (a.N <= 64)
-    hipLaunchKernelGGL((k_rows<T, O, 4, false>), outs, block, 0, s, a);
+  else if (a.N <= 64 || (many && outs.x * blocks64 <= 256))
+    hipLaunchKernelGGL((k_rows<T, O, 4, false>), dim3(outs.x, (uint32_t)blocks64), block, 0, s, a);
   else if (!aligned && tiles(128, 128) >= 192)
     launch_tiles<T, O, 128, 128, 2, 2, false>(a, s);
   else if (!aligned)

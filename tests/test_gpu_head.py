@@ -261,3 +261,23 @@ def test_runs_of_adapters_in_large_tiles(wf, dtype, run, N, P, R):
     assert not torch.isfinite(z[hit]).any()
     off = (z[~hit].double() - want[~hit]).abs() - bound[~hit]
     assert float(off.max()) <= 0
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("N,D,P,G,R", [
+    (1, 3, 40, 2, 2), (40, 3, 1, 2, 2), (1, 7, 1, 1, 1), (300, 7, 90, 1, 1), (30, 2, 300, 3, 1), (70, 200, 1, 2, 3), (600, 90, 7, 1, 1),
+    (1, 9, 1, 1, 1), (9, 9, 9, 1, 1), (3, 15, 17, 1, 9), (90, 17, 3, 2, 2), (530, 8, 33, 1, 1), (700, 33, 10, 1, 15), (90, 9, 1, 90, 9),
+])
+def test_small_arrays_and_their_last_elements(wf, dtype, N, D, P, G, R):
+    """Arrays of less than a load, and those whose last rows end inside one."""
+    check(wf, make(N, D, P, G, R, dtype, seed=N + D + P), F32)
+
+
+@pytest.mark.parametrize("N,D,P,G,R", [(66, 300, 700, 66, 9), (128, 512, 1000, 20, 16), (250, 1133, 500, 250, 38), (500, 96, 200, 60, 5)])
+def test_blocks_of_rows_of_many_adapters(wf, N, D, P, G, R):
+    d = make(N, D, P, G, R, BF16, seed=N + R)
+    y = check(wf, d)
+    d["b"][int(d["adapter"][N - 1])] = float("inf")  # only its own rows change
+    z = head_of(wf, d).project(d["x"].to(DEV), d["adapter"].to(DEV))
+    same = d["adapter"] != d["adapter"][N - 1]
+    assert torch.equal(y.cpu()[same], z.cpu()[same])
