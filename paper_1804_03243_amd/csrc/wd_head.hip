@@ -13,6 +13,7 @@
 // consecutive outputs of one row.
 #include "wd_host.h"
 #include "wd_num.h"
+#include "wd_rows.h"
 
 namespace wd {
 
@@ -62,7 +63,7 @@ __device__ __forceinline__ int adapter_of(const HeadArgs& a, int64_t n) {
 // puts zeros from element n on.  Reads first, then the moves: several reads are under
 // way together.  (Element by element, under a branch each, 78 rows of 1133 -> 1516 with
 // as many adapters of rank 38 took 72 us for 60, 2548 of 67 -> 7042 41 for 36.)
-// Arrays of fewer than eight elements go to k_tiny.
+// Arrays of fewer than eight elements (shorter_than_a_load) go to k_tiny.
 template <class T>
 __device__ __forceinline__ uint4 load8(const T* p) {
   return __builtin_bit_cast(uint4, *(const Few<T, 8>*)p);
@@ -1038,8 +1039,9 @@ __global__ void __launch_bounds__(256) k_tiny(HeadArgs a) {
 
 template <class T, class O>
 void launch_project(HeadArgs a, hipStream_t s) {
-  const int64_t G = a.adapter ? a.h.n_adapters : 8, R = a.adapter ? a.h.rank : 8;
-  if ((a.h.D < 8 && (a.N == 1 || a.h.P == 1)) || G * R * a.h.D < 8 || G * R * a.h.P < 8) {
+  const int64_t GR = a.adapter ? (int64_t)a.h.n_adapters * a.h.rank : kLoad;
+  if (shorter_than_a_load(a.N, a.x_ld, a.h.D) || shorter_than_a_load(a.h.P, a.h.weight_ld, a.h.D) ||
+      shorter_than_a_load(GR, a.h.D, a.h.D) || shorter_than_a_load(GR, a.h.P, a.h.P)) {
     const uint64_t blocks = ((uint64_t)a.N * a.h.P + 255) / 256;
     hipLaunchKernelGGL((k_tiny<T, O>), dim3((uint32_t)std::min<uint64_t>(blocks, 1 << 16)), dim3(256), 0, s, a);
     return;

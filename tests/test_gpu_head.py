@@ -281,3 +281,12 @@ def test_blocks_of_rows_of_many_adapters(wf, N, D, P, G, R):
     z = head_of(wf, d).project(d["x"].to(DEV), d["adapter"].to(DEV))
     same = d["adapter"] != d["adapter"][N - 1]
     assert torch.equal(y.cpu()[same], z.cpu()[same])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("G", [0, 1, 3])
+@pytest.mark.parametrize("N,D,P", [(2, 1, 40), (7, 1, 3), (8, 1, 3), (2, 3, 40), (3, 2, 7), (4, 2, 7), (40, 1, 5), (40, 3, 2),
+                                   (5, 1, 8), (2, 4, 2), (2, 5, 1), (300, 1, 2), (600, 2, 3)])
+def test_arrays_that_end_before_a_load_does(wf, dtype, G, N, D, P):
+    """Rows and weights of fewer than eight elements in all, and of just as many."""
+    check(wf, make(N, D, P, G, 2, dtype, seed=N + D + P), F32)
