@@ -800,8 +800,10 @@ class Head:
 
     weight [P, D] (float16 or bfloat16), bias [P] (float32), adapter_a
     [G, R, D] and adapter_b [G, P, R] (type of weight, R <= 128),
-    adapter_scale [G] (float32); all device tensors, kept by reference: weights
-    changed in place are the ones the next call uses."""
+    adapter_scale [G] (float32); all device tensors.  The memory they have now is
+    kept and read by every call: weights changed in place are the ones the next
+    call uses; a parameter that is given other memory later (module.to, .half,
+    p.data = ...) needs a new Head."""
 
     def __init__(self, weight, bias=None, adapter_a=None, adapter_b=None, adapter_scale=None):
         torch = _torch()
@@ -823,7 +825,8 @@ class Head:
             _vector(adapter_scale, torch.float32, dev, G, "adapter_scale")
         self.D, self.P, self.G, self.R = D, P, G, R
         self.device, self.dtype = dev, weight.dtype
-        self._kept = (weight, bias, adapter_a, adapter_b, adapter_scale)
+        # (tensors of our own on the same memory: a caller's may be given another's)
+        self._kept = tuple(None if t is None else t.detach() for t in (weight, bias, adapter_a, adapter_b, adapter_scale))
         ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
         self.desc = wd_head(D, P, types[weight.dtype], G, R, _ld(weight), ptr(weight), ptr(bias), ptr(adapter_a),
                             ptr(adapter_b), ptr(adapter_scale))

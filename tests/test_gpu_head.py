@@ -290,3 +290,21 @@ def test_blocks_of_rows_of_many_adapters(wf, N, D, P, G, R):
 def test_arrays_that_end_before_a_load_does(wf, dtype, G, N, D, P):
     """Rows and weights of fewer than eight elements in all, and of just as many."""
     check(wf, make(N, D, P, G, 2, dtype, seed=N + D + P), F32)
+
+
+def test_parameters_given_other_memory(wf):
+    """A head reads the memory that it was made with, also when the module's parameters
+    have moved on and nobody else holds it."""
+    d = make(40, 64, 96, 3, 8, BF16, seed=12)
+    layer = torch.nn.Linear(64, 96).to(BF16).to(DEV)
+    layer.weight.data.copy_(d["weight"])
+    params = {k: torch.nn.Parameter(d[k].to(DEV)) for k in ("bias", "a", "b", "scale")}
+    head = wf.Head(layer.weight, *(params[k] for k in ("bias", "a", "b", "scale")))
+    layer.half()
+    for p in params.values():
+        p.data = torch.zeros_like(p.data)
+    taken = [torch.full((k,), float("nan"), dtype=BF16, device=DEV) for k in (96 * 64, 3 * 8 * 64, 3 * 96 * 8, 2 * 96, 2 * 3)
+             for _ in range(4)]  # (memory that was given back would be taken by these)
+    y = head.project(d["x"].to(DEV), d["adapter"].to(DEV))
+    plain.close(y, *plain.project(d["x"], d["weight"], d["bias"], d["a"], d["b"], d["scale"], d["adapter"]))
+    del taken
