@@ -546,19 +546,20 @@ class Graph:
         `out`: rows of at least that many words to write into.  Enqueued on
         the current stream."""
         torch = _torch()
+        dev = self.buf.device  # (self.device may be "cuda" without an index)
         N, n_states, words = offsets.numel() - 1, states.numel(), (self.num_pdfs + 31) // 32
-        p_off = _vector(offsets, torch.int64, self.device, N + 1, "offsets")
-        p_states = _vector(states, torch.int32, self.device, n_states, "states")
+        p_off = _vector(offsets, torch.int64, dev, N + 1, "offsets")
+        p_states = _vector(states, torch.int32, dev, n_states, "states")
         if N < 0:
             raise ValueError("offsets need at least one entry")
         if out is None:
-            out = torch.empty((N, words), dtype=torch.int32, device=self.device)
+            out = torch.empty((N, words), dtype=torch.int32, device=dev)
         else:
-            _matrix(out, (torch.int32,), self.device, "out")
+            _matrix(out, (torch.int32,), dev, "out")
             if out.shape[0] != N or out.shape[1] < words:
                 raise ValueError(f"out must be {N} rows of at least {words} words")
-        _enqueue(self.device, lambda stream: wd_label_masks(
-            self.handle, N, p_off, p_states, n_states, out.data_ptr(), max(out.stride(0), words), stream))
+        _enqueue(dev, lambda stream: wd_label_masks(
+            self.handle, N, p_off, p_states, n_states, out.data_ptr(), _ld(out), stream))
         return out
 
     def workspace(self, lanes: int, max_T: int, params: wd_params, caps: wd_caps | None):

@@ -104,3 +104,9 @@ def test_second_pass_within_a_first_pass_lattice(wf):
     assert torch.equal(y[y > -float("inf")], x[y > -float("inf")])
     again = wf.decode(graph, y, cfg["beam"], cfg["max_active"], cfg["lattice_beam"])
     assert again.cost == r.cost and list(again.words) == list(r.words)
+
+
+def test_graph_on_the_current_device(wf):
+    """A graph made on "cuda" takes tensors of the device that it is on."""
+    g = wide_graph(40, 200, 90, 1)
+    check(wf, wf.Graph(g, 90, "cuda"), g, 90, np.array([0, 4, 9], np.int64), np.arange(9, dtype=np.int32))
