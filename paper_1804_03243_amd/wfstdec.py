@@ -710,14 +710,18 @@ class Stream:
 
     def advance(self, n_frames: list) -> None:
         """n_frames[i] more rows of utterance i stand in `frames` behind the
-        T[i] decoded ones, written on the decoding stream (the one current at
-        construction), e.g. by loglikes(out=..., out_row=...): decodes them
-        without a copy."""
+        T[i] decoded ones, written on the caller's current stream, e.g. by
+        loglikes(out=..., out_row=...): decodes them without a copy, on the
+        decoding stream (the one current at construction) after it has waited
+        for the current stream."""
         counts = [int(n) for n in n_frames]
         if len(counts) != self.B:
             raise ValueError(f"n_frames needs {self.B} counts")
         torch = _torch()
         with torch.cuda.device(self.graph.device):
+            cur = torch.cuda.current_stream(self.graph.device)
+            if cur != self._stream:
+                self._stream.wait_stream(cur)
             wd_stream_advance(self.handle, counts)
         self.T = [t + n for t, n in zip(self.T, counts)]
 

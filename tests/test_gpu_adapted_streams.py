@@ -71,3 +71,22 @@ def test_advance_refuses_other_counts(example):
     with pytest.raises(wf.WdError):
         s.advance([11, 0])
     assert s.T == [0, 0]
+
+
+def test_advance_waits_for_rows_of_another_stream(example):
+    """Rows that the caller's stream is still to write are decoded after it has."""
+    wf = example.wfstdec
+    cfg = synth.workload("tiny_10k")
+    graph = wf.Graph(synth.make_graph(cfg), cfg["P"])
+    decoding = (cfg["beam"], cfg["max_active"], cfg["lattice_beam"])
+    L = torch.from_numpy(synth.make_loglikes(cfg)[:40]).to("cuda:0")
+    s = wf.Stream(graph, 1, 40, *decoding)
+    s.frames.zero_()
+    torch.cuda.synchronize()
+    other = torch.cuda.Stream()
+    with torch.cuda.stream(other):
+        torch.cuda._sleep(100_000_000)  # (some tens of milliseconds)
+        s.frames[0].copy_(L)
+        s.advance([40])
+    r, w = s.end()[0], wf.decode(graph, L, *decoding)
+    assert r.cost == w.cost and list(r.words) == list(w.words) and np.array_equal(r.links["arc_id"], w.links["arc_id"])
