@@ -32,7 +32,9 @@
 //      the cutoff (level by level without a path table);
 //   C  survivors of the beam cutoff, and the histogram for max-active;
 //   D  further digits of the max-active radix select, when it binds;
-//   E  kept tokens into the bitmap (in C when max-active cannot bind).
+//   E  kept tokens into the bitmap (in C when max-active cannot bind), the other
+//      touched states' slots emptied; a barrier where max-active may bind or
+//      a workgroup still reads lists that the next frame's A writes.
 // Results are those of the LDS path bit for bit: the same sums, the same
 // minima, the same cutoffs.
 #pragma once
@@ -89,7 +91,8 @@ struct alignas(128) ClusterCtl {
     uint32_t n_bx;       // reached by epsilon paths (bucketed by level without a path table)
     uint32_t n_surv;
     uint32_t regroup;    // helpers wait for the next run: the leader ends this one
-    uint32_t pad0[2];
+    uint32_t reform;     // a workgroup's candidates exceed its LDS: formed again at the frame's end
+    uint32_t pad0;
     unsigned long long work;  // emitting arcs
     unsigned long long eps;   // epsilon arcs of the closure
     uint32_t pad1[20];
@@ -608,6 +611,7 @@ __device__ __forceinline__ void cl_run(const DevGraph& g, const LaneDesc& L, con
       if (my_best != 0xffffffffu)
         (void)__hip_atomic_fetch_max(&F->best, ~my_best, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       if (my_work) cl_add<unsigned long long>(&F->work, (unsigned long long)my_work);
+      if (my_work > kClCand) cl_store(&F->reform, 1u);
     }
     stored = false;
     cl_barrier(C, N, gen);
@@ -822,6 +826,10 @@ __device__ __forceinline__ void cl_run(const DevGraph& g, const LaneDesc& L, con
     cl_barrier(C, N, gen);
     stamp(t, 3);
     regroup = cl_load(&F->regroup) != 0;
+    // Whether somebody reads the frame's lists of touched states or tokens until the
+    // frame's end: the next frame's phase A writes both, so it waits (frames of up to
+    // kHeld * kThreads states a workgroup need no such barrier).
+    const bool reads = !shares_held(nt, N, kHeld * kThreads) || cl_load(&F->reform) != 0;
     ++frames;
     if (w == 0 && tid == 0) S.out.eps += cl_load(&F->eps);
     cut_key = kcutb;
@@ -892,11 +900,8 @@ __device__ __forceinline__ void cl_run(const DevGraph& g, const LaneDesc& L, con
       const uint32_t s = cl_load(&L.touched[i]);
       finish(s, (uint32_t)(cl_load(&cur[s]) >> 32));
     }
-    if (may_bind) {
-      cl_barrier(C, N, gen);
-    } else {
-      stamp(t, 4);
-    }
+    if (!may_bind) stamp(t, 4);
+    if (may_bind || reads) cl_barrier(C, N, gen);
     stamp(t, 5);
     small = nt <= kSmallTouched;
     ++t;

@@ -21,6 +21,11 @@ constexpr uint32_t kSpinLooks = 8;         // looks at the arrivals (about 0.7 Â
 // arrivals a frame); it is never 2^31 away from a target that is waited for.
 WD_HOST_DEVICE bool arrived(uint32_t now, uint32_t target) { return (int32_t)(now - target) >= 0; }
 
+// Whether each of N workgroups holds its share (n w / N to n (w + 1) / N) of n states in
+// registers, `held` of them a workgroup.  Where not, it reads the rest of the list
+// again at the frame's end, and nobody may write the next frame's list before it has.
+WD_HOST_DEVICE bool shares_held(uint32_t n, uint32_t N, uint32_t held) { return n <= (uint64_t)held * N; }
+
 // The time a wait has been running.  A workgroup's queue may be descheduled
 // while it waits: that time passes between two looks at the clock and does not
 // count, nobody can arrive in it.

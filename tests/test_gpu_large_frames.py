@@ -486,3 +486,20 @@ def test_chip_wide_many_paths(wf, oracle_mod, fan, levels):
         check(wf, oracle_mod, g, graph, L, args, "chip")
         r = wf.decode(graph, torch.from_numpy(L).to(graph.device), *args, mode="chip", flags=wf.WD_FLAG_EPS_LEVELS)
         assert_same(r, oracle_mod.decode(g, L, *args))
+
+
+@pytest.mark.parametrize("mode", ["workgroup", "workgroup_levels"])
+def test_shares_beyond_the_registers(wf, oracle_mod, mode):
+    """Frames of more touched states and arcs than the workgroups of a cluster hold,
+    without a limit on tokens: nobody's list is written over while it is still read."""
+    import torch
+    g = graph_of(700_000, 2_400_000, 300, 0.25, 5, 70)
+    graph = wf.Graph(g, 300)
+    L = flat(9, 300, 71)
+    x, args = torch.from_numpy(L).to(graph.device), (16.0, 0, 6.0)
+    print(f"\n[gpu case] shares beyond the registers, mode={mode}", flush=True)
+    o = oracle_mod.decode(g, L, *args)
+    for _ in range(4):
+        r = wf.decode(graph, x, *args, mode=mode)
+        assert r.needed["frame_tokens"] > 32 * 3 * 1024 and r.needed["frame_arcs"] > 32 * 12288
+        assert_same(r, o)
