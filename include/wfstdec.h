@@ -42,7 +42,8 @@ typedef enum {
   WD_ENOPATH = 3,    /* no token survived some frame */
   WD_ECAPACITY = 4,  /* the workspace was too small; wd_result_stats reports
                         the capacities needed, retry with a larger workspace */
-  WD_EDEVICE = 5     /* a HIP call failed */
+  WD_EDEVICE = 5     /* a HIP call failed, or a check that kernels make of their own results
+                        (wd_last_error names it) */
 } wd_status;
 
 /* Decoding graph (host memory, CSR; arc id = index into the arc arrays).

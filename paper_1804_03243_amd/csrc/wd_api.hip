@@ -409,13 +409,8 @@ static wd_stats lane_stats(const LaneInfo& I, int32_t T, float fwd_ms, float lat
   return stt;
 }
 
-static const char* status_message(wd_status st) {
-  return st == WD_ENOPATH     ? "decode: no token survived a frame"
-         : st == WD_EINVAL    ? "decode: log-likelihoods contain NaN, +inf or values above 1e30"
-         : st == WD_ECAPACITY ? "decode: workspace capacity exceeded; see stats.needed"
-         : st == WD_EDEVICE   ? "decode: a kernel's internal consistency check failed"
-                              : "decode failed";
-}
+// A decode's status, the traceback's check among them.
+static int32_t lane_status(const LaneInfo& I) { return I.status == 0 && I.tb_fail ? kTraceback : I.status; }
 
 // The current device's pinned memory.
 static wd_status pinned_of_current_device(HipPinned** out) {
@@ -461,7 +456,7 @@ static wd_status run_finish(wd_stream* run, wd_result** out) {
     (void)hipEventElapsedTime(&fwd_ms, run->ev[0], run->ev[1]);
     (void)hipEventElapsedTime(&lat_ms, run->ev[1], run->ev[2]);
   }
-  wd_status first_bad = WD_OK;
+  int32_t first_bad = WD_OK;
   const bool debug = (p->flags & WD_FLAG_DEBUG) != 0;
   // Without the debug outputs, the finished lanes' links, nodes and words
   // are packed on the device (into the candidate buffer, free after the
@@ -508,8 +503,8 @@ static wd_status run_finish(wd_stream* run, wd_result** out) {
     const LaneInfo& I = info[b];
     const LaneDesc& L = run->lanes[b];
     const int32_t Tb = run->T[b];
-    const wd_status ls = (I.status == 0 && I.tb_fail) ? WD_EDEVICE : (wd_status)I.status;
-    if (ls != WD_OK && first_bad == WD_OK) first_bad = ls;
+    const wd_status ls = status_of(lane_status(I));
+    if (ls != WD_OK && first_bad == WD_OK) first_bad = lane_status(I);
     if (ls != WD_OK && ls != WD_ECAPACITY) continue;
     wd_result* r = new wd_result();
     r->status = ls;
@@ -585,7 +580,7 @@ static wd_status run_finish(wd_stream* run, wd_result** out) {
   }
   if ((st = hip_check(hipStreamSynchronize(s), "result download"))) return st;
   if (first_bad != WD_OK) set_error(status_message(first_bad));
-  return first_bad;
+  return status_of(first_bad);
 }
 
 static wd_status check_lanes(const wd_graph* g, int32_t B, const float* const* ll, const int32_t* T,
@@ -751,9 +746,9 @@ extern "C" wd_status wd_decode_noalloc(const wd_graph* g, const float* loglikes,
       (st = hip_check(hipMemcpyAsync(&I, R.info, sizeof(LaneInfo), hipMemcpyDeviceToHost, s), "info download")) ||
       (st = hip_check(hipStreamSynchronize(s), "decode")))
     return st;
-  const wd_status ls = (I.status == 0 && I.tb_fail) ? WD_EDEVICE : (wd_status)I.status;
+  const wd_status ls = status_of(lane_status(I));
   *stats = lane_stats(I, T, 0.0f, 0.0f, false);
-  if (ls != WD_OK) return fail(ls, status_message(ls));
+  if (ls != WD_OK) return fail(ls, status_message(lane_status(I)));
   *cost = I.best_cost;
   *n_words = (int32_t)I.nwords;
   if ((int64_t)I.nwords > words_cap || (int64_t)I.kept > links_cap || (int64_t)I.out_nodes > nodes_cap)

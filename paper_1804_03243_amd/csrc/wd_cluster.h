@@ -616,7 +616,7 @@ __device__ __forceinline__ void cl_run(const DevGraph& g, const LaneDesc& L, con
     stored = false;
     cl_barrier(C, N, gen);
     if (cl_load(&C->bad)) {
-      status = kStatusInternal;
+      status = kClusterWait;
       break;
     }
     // ---------------------------------------------------- B: epsilon closure
@@ -731,7 +731,7 @@ __device__ __forceinline__ void cl_run(const DevGraph& g, const LaneDesc& L, con
     }
     if (nlev == 0) cl_barrier(C, N, gen);
     if (cl_load(&C->bad)) {
-      status = kStatusInternal;
+      status = kClusterWait;
       break;
     }
     stamp(t, 2);

@@ -10,6 +10,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "wd_status.h"
+
 namespace wd {
 
 struct ClusterCtl;
@@ -140,7 +142,7 @@ struct Params {
 
 // Per-utterance counters and status, written by the kernels.
 struct LaneInfo {
-  int32_t status;              // WD_* code
+  int32_t status;              // wd_status.h
   int32_t frames_done;
   int32_t final_used;
   uint32_t overflow;           // bit mask of exceeded capacities (kOvf*)
@@ -176,9 +178,6 @@ constexpr uint32_t kFlagSwept = 1u << 30;
 // Params::flags bit set by the host for chip-wide decodes whose lattice is
 // pruned from the node store: the forward pass only counts the raw links.
 constexpr uint32_t kFlagSparse = 1u << 29;
-// LaneInfo::status value for an internal consistency failure caught by a
-// kernel's own bounds checks (reported as WD_EDEVICE).
-constexpr int32_t kStatusInternal = 5;
 
 // Device output records (match wd_lat_arc / wd_lat_node / wd_token of wfstdec.h).
 struct OutLink {

@@ -876,7 +876,7 @@ __device__ __forceinline__ void forward_body(FwdShared& sh, const DevGraph& g, c
               sh.hist[2 * tid + 1] = ex + h0;
             }
             if (nk != n_keep) {
-              status = kStatusInternal;
+              status = kKeptCount;
               break;
             }
             __syncthreads();
@@ -1061,7 +1061,7 @@ __device__ __forceinline__ void forward_body(FwdShared& sh, const DevGraph& g, c
   const uint64_t arcs = sh.c_arcs + eps;  // (the bookkeeping thread's writes, before the barrier)
   if (tid == 0) {
     LaneInfo* info = L.info;
-    if (status == 0 && wb) status = kStatusInternal;
+    if (status == 0 && wb) status = kWarmPayload;
     if (status == 0 && (ovf & kOvfNodes)) status = 4;
     info->status = status;
     info->frames_done = t;

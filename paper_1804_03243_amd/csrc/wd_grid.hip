@@ -1322,7 +1322,7 @@ __global__ void __launch_bounds__(kGT) k_g_end(const LaneDesc* __restrict__ lane
   for (uint32_t i = threadIdx.x; i < (uint32_t)kHistBins; i += kGT) G.hist[i] = 0;
   if (threadIdx.x != 0) return;
   if (G.bad) {
-    G.status = kStatusInternal;
+    G.status = kGridFrame;
     G.stop = 1;
     return;
   }

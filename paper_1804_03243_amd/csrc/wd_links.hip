@@ -473,7 +473,7 @@ __global__ void __launch_bounds__(kLT) k_links_write(DevGraph g, const LaneDesc*
     const uint32_t all = block_or<kLWv>(xmask, sh.bs, par);
     if (threadIdx.x == 0) L.xmask[t] = all;
   }
-  if (bad) L.info->status = kStatusInternal;
+  if (bad) L.info->status = kLinkTarget;
 }
 
 void launch_links(const DevGraph& g, const LaneDesc* lanes, int B, const Params& prm, hipStream_t s) {

@@ -422,7 +422,7 @@ __global__ void __launch_bounds__(kThreads) k_sp_sweep(DevGraph g, const LaneDes
   const uint32_t lb = cost_key(prm.lattice_beam);
   sp_sweep(g, L, S, C, w, N, lb < kInfKey ? lb : kInfKey - 1u, (prm.flags & kFlagSwept) == 0);
   if (lead && threadIdx.x == 0) {
-    if (cl_load(&C->bad)) L.info->status = kStatusInternal;
+    if (cl_load(&C->bad)) L.info->status = kSweepWait;
     cl_store(&C->quit, 1u);
   }
 }
