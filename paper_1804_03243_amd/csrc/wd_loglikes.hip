@@ -21,6 +21,7 @@ namespace wd {
 
 struct ScoreArgs {
   wd_loglikes_args a;
+  int64_t n0;       // first row of this launch
   float2* part;     // [N][slices] maximum and sum of each slice of a row
   uint32_t slices;  // slices of a row
   bool stream;      // outputs past the caches
@@ -67,7 +68,7 @@ __global__ void __launch_bounds__(THREADS) k_loglikes(ScoreArgs args) {
   const wd_loglikes_args& a = args.a;
   extern __shared__ uint32_t table[];  // [kSlice], where there are histories or biases
   __shared__ float red[2][kWavesHere];
-  const int64_t n = PHASE == kWhole ? blockIdx.x : blockIdx.x / args.slices;
+  const int64_t n = args.n0 + (PHASE == kWhole ? blockIdx.x : blockIdx.x / args.slices);
   const int c0 = PHASE == kWhole ? 0 : (int)(blockIdx.x % args.slices) * kSlice;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int64_t to = n;
@@ -186,7 +187,7 @@ __global__ void __launch_bounds__(THREADS) k_loglikes(ScoreArgs args) {
 #pragma unroll
     for (int w = 1; w < kWavesHere; ++w) s += red[1][w];
     if (PHASE == kStats) {
-      if (threadIdx.x == 0) args.part[blockIdx.x] = make_float2(top, s);
+      if (threadIdx.x == 0) args.part[n * args.slices + blockIdx.x % args.slices] = make_float2(top, s);
       return;
     }
     lse = logf(s);
@@ -236,22 +237,26 @@ __global__ void __launch_bounds__(THREADS) k_loglikes(ScoreArgs args) {
 constexpr int kWholeLabels = 32768;
 constexpr int kSliceThreads = 512, kSliceEach = 16, kSliceLabels = kSliceThreads * kSliceEach;
 
+// (A launch has fewer than 2^32 threads: more rows than that take several.)
 template <class T, int THREADS, int EACH, ScorePhase PHASE>
-void launch_slices(const ScoreArgs& args, hipStream_t s) {
-  const dim3 grid((uint32_t)args.a.N * args.slices), block(THREADS);
-  if (!args.a.hist_off && !args.a.bias_off) {
-    hipLaunchKernelGGL((k_loglikes<T, THREADS, EACH, PHASE, false>), grid, block, 0, s, args);
-    return;
+void launch_slices(ScoreArgs args, hipStream_t s) {
+  const int64_t most = (((int64_t)1 << 32) / THREADS - 1) / args.slices;
+  for (; args.n0 < args.a.N; args.n0 += most) {
+    const dim3 grid((uint32_t)(std::min(most, args.a.N - args.n0) * args.slices)), block(THREADS);
+    if (!args.a.hist_off && !args.a.bias_off) {
+      hipLaunchKernelGGL((k_loglikes<T, THREADS, EACH, PHASE, false>), grid, block, 0, s, args);
+      continue;
+    }
+    auto* k = k_loglikes<T, THREADS, EACH, PHASE, true>;
+    static std::atomic<uint64_t> done{0};
+    allow_lds((const void*)k, THREADS * EACH * 4, done);
+    hipLaunchKernelGGL(k, grid, block, THREADS * EACH * 4, s, args);
   }
-  auto* k = k_loglikes<T, THREADS, EACH, PHASE, true>;
-  static std::atomic<uint64_t> done{0};
-  allow_lds((const void*)k, THREADS * EACH * 4, done);
-  hipLaunchKernelGGL(k, grid, block, THREADS * EACH * 4, s, args);
 }
 
 template <class T>
 void launch_loglikes(const wd_loglikes_args* a, void* ws, hipStream_t s) {
-  ScoreArgs args{*a, (float2*)ws, 1, (uint64_t)a->N * a->V * 4 >= (256u << 20)};
+  ScoreArgs args{*a, 0, (float2*)ws, 1, (uint64_t)a->N * a->V * 4 >= (256u << 20)};
   if (a->V <= 2048)
     launch_slices<T, 256, 8, kWhole>(args, s);
   else if (a->V <= 4096)

@@ -264,3 +264,14 @@ def test_lists_beyond_16_bits(wf, V, most):
     d["bias"] = (torch.tensor([0, m - 5, m]), torch.randint(0, V, (m,), generator=gen, dtype=torch.int32),
                  torch.randn(m, generator=gen))
     check(wf, d)
+
+
+def test_more_rows_than_a_launch_takes(wf):
+    """Rows beyond 2^32 threads, in one call."""
+    N, V = (1 << 24) + 3, 2
+    z = torch.randn((N, V), generator=torch.Generator(DEV).manual_seed(30), device=DEV)
+    prior = torch.tensor([-0.5, -1.5], device=DEV)
+    y = wf.loglikes(z, log_prior=prior, scale=0.5)
+    want = 0.5 * (torch.log_softmax(z.double(), 1) - prior.double())
+    # (three roundings of values below 16, those of the sum and the logarithm, halved)
+    assert float((y.double() - want).abs().max()) <= 64 * 2.0 ** -24
