@@ -110,3 +110,18 @@ def test_graph_on_the_current_device(wf):
     """A graph made on "cuda" takes tensors of the device that it is on."""
     g = wide_graph(40, 200, 90, 1)
     check(wf, wf.Graph(g, 90, "cuda"), g, 90, np.array([0, 4, 9], np.int64), np.arange(9, dtype=np.int32))
+
+
+def test_more_rows_than_a_launch_takes(wf):
+    """Rows beyond 2^32 threads of the kernel for long sets, in one call."""
+    S, P, N = 500, 90, (1 << 22) + 2
+    g = wide_graph(S, 1500, P, 7)
+    graph = wf.Graph(g, P)
+    n_states = 513 * N  # (most of the list is past the last row's end)
+    states = torch.empty(n_states, dtype=torch.int32, device=DEV)
+    states[:2 * N] = torch.randint(0, S, (2 * N,), generator=torch.Generator(DEV).manual_seed(8), device=DEV, dtype=torch.int32)
+    offsets = 2 * torch.arange(N + 1, device=DEV)
+    got = graph.label_masks(offsets, states)
+    bits = torch.from_numpy(plain.label_masks(g, P, np.arange(S + 1), np.arange(S))).to(DEV)  # of each state alone
+    want = bits[states[:2 * N:2].long()] | bits[states[1:2 * N:2].long()]
+    assert torch.equal(got, want)
