@@ -11,6 +11,8 @@
 // rounding to the output's type are added as a tile is stored.  W is the
 // matrix instruction's first operand and x its second, so that a lane holds
 // consecutive outputs of one row.
+#include <algorithm>
+
 #include "wd_host.h"
 #include "wd_num.h"
 #include "wd_rows.h"
@@ -1110,10 +1112,13 @@ static wd_status check_head(const wd_head* h) {
   return WD_OK;
 }
 
+constexpr int64_t kMostRows = 1 << 27;  // rows of a launch
+
 // Workspace: the terms of u (at most three), then the rows' powers of two.
 static int padded_rank(const wd_head* h) { return (h->rank + 7) / 8 * 8; }
 static size_t u_bytes(const wd_head* h, int64_t N) { return align_up((uint64_t)N * ((3 * padded_rank(h) + 63) / 64 * 64) * 2, 256); }
 static size_t project_bytes(const wd_head* h, int64_t N) {
+  N = std::min(N, kMostRows);
   return h->n_adapters > 0 ? u_bytes(h, N) + align_up((uint64_t)N * sizeof(float), 256) : 0;
 }
 
@@ -1143,12 +1148,17 @@ extern "C" wd_status wd_project(const wd_head* h, const void* x, int64_t x_ld, i
     return fail(WD_EINVAL, "project: workspace missing, too small or not 256-byte aligned");
   if (((uint64_t)N + 63) / 64 * (((uint64_t)h->P + 63) / 64) > INT32_MAX)
     return fail(WD_EINVAL, "project: too many rows for one call");
-  HeadArgs a{*h, x, x_ld, N, adapter, out, out_ld, (uint16_t*)ws,
-             adapter ? (float*)((char*)ws + u_bytes(h, N)) : nullptr, adapter ? padded_rank(h) : 0, 0, 0, false, false};
   hipStream_t s = (hipStream_t)stream;
-  if (h->type == WD_F16)
-    out_type == WD_F32 ? launch_project<Half, F32>(a, s) : launch_project<Half, Half>(a, s);
-  else
-    out_type == WD_F32 ? launch_project<Bf16, F32>(a, s) : launch_project<Bf16, Bf16>(a, s);
+  // (a launch has fewer than 2^32 threads: 2^28 rows in tiles of 16 are as many)
+  for (int64_t n0 = 0; n0 < N; n0 += kMostRows) {
+    const int64_t n = std::min(kMostRows, N - n0);
+    HeadArgs a{*h, (const uint16_t*)x + n0 * x_ld, x_ld, n, adapter ? adapter + n0 : nullptr,
+               (char*)out + n0 * out_ld * (out_type == WD_F32 ? 4 : 2), out_ld, (uint16_t*)ws,
+               adapter ? (float*)((char*)ws + u_bytes(h, n)) : nullptr, adapter ? padded_rank(h) : 0, 0, 0, false, false};
+    if (h->type == WD_F16)
+      out_type == WD_F32 ? launch_project<Half, F32>(a, s) : launch_project<Half, Half>(a, s);
+    else
+      out_type == WD_F32 ? launch_project<Bf16, F32>(a, s) : launch_project<Bf16, Bf16>(a, s);
+  }
   return hip_check(hipGetLastError(), "project");
 }

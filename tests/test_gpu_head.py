@@ -308,3 +308,20 @@ def test_parameters_given_other_memory(wf):
     y = head.project(d["x"].to(DEV), d["adapter"].to(DEV))
     plain.close(y, *plain.project(d["x"], d["weight"], d["bias"], d["a"], d["b"], d["scale"], d["adapter"]))
     del taken
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+def test_more_rows_than_a_launch_takes(wf, dtype):
+    """Rows whose 16-row tiles would be 2^32 threads, in one call."""
+    N, D, P, G, R = (1 << 28) + 21, 8, 2, 3, 3
+    d = make(4096, D, P, G, R, dtype, seed=13)
+    x = d["x"].to(DEV).repeat(N // 4096 + 1, 1)[:N]
+    g = d["adapter"].to(DEV).repeat(N // 4096 + 1)[:N]
+    y = head_of(wf, d).project(x, g, out_dtype=dtype)
+    want, bound = plain.project(d["x"], d["weight"], d["bias"], d["a"], d["b"], d["scale"], d["adapter"], dtype)
+    plain.close(y[:4096], want, bound)
+    for n0 in range(4096, N, 4096):  # (the rows repeat)
+        if n0 % (1 << 26) == 0 or N - n0 < 8192:
+            plain.close(y[n0:n0 + 4096], want[:N - n0], bound[:N - n0])
+    assert torch.equal(y[4096:1 << 27].view(-1, 4096, P), y[:4096].expand((1 << 27) // 4096 - 1, 4096, P))
+    assert torch.equal(y[1 << 27:1 << 28].view(-1, 4096, P), y[:4096].expand((1 << 27) // 4096, 4096, P))
