@@ -618,8 +618,13 @@ __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, u
   const uint64_t p = (uint64_t)base;  // (into scalar registers, where the compiler would not hold it there)
   base = (const void*)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(p >> 32)) << 32 |
                        (uint32_t)__builtin_amdgcn_readfirstlane((int)p));
+  // (m0 is a register that the compiler keeps to itself, and warns of here; it holds no
+  // value there across other code, and is named so that none of its uses is put around this)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
   asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(to)
-               : "memory");
+               : "memory", "m0");
+#pragma clang diagnostic pop
 }
 // Waits until at most N of this wavefront's loads are on their way (they arrive in order).
 template <int N>
