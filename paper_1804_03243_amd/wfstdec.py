@@ -794,6 +794,13 @@ def _matrix(t, dtypes, device, what):
         raise ValueError(f"{what} must have contiguous, separate rows")
 
 
+def _no_gradient(torch, what, *tensors):
+    """Refuses tensors whose gradient a call would lose in silence."""
+    for t in tensors:
+        if t is not None and t.requires_grad and torch.is_grad_enabled():
+            raise ValueError(f"{what} has no backward pass: call it under torch.no_grad() or on detached tensors")
+
+
 def _ld(t):
     """Row stride in elements (of no meaning for a single row)."""
     return max(t.stride(0), t.shape[1]) if t.shape[0] > 1 else t.shape[1]
@@ -808,7 +815,8 @@ class Head:
     adapter_scale [G] (float32); all device tensors.  The memory they have now is
     kept and read by every call: weights changed in place are the ones the next
     call uses; a parameter that is given other memory later (module.to, .half,
-    p.data = ...) needs a new Head."""
+    p.data = ...) needs a new Head.  There is no backward pass: the weights are
+    taken detached, and rows that require a gradient are refused."""
 
     def __init__(self, weight, bias=None, adapter_a=None, adapter_b=None, adapter_scale=None):
         torch = _torch()
@@ -846,6 +854,7 @@ class Head:
         current stream."""
         torch = _torch()
         _matrix(x, (self.dtype,), self.device, "x")
+        _no_gradient(torch, "project", x, out)
         N = x.shape[0]
         if x.shape[1] != self.D:
             raise ValueError(f"x must be N x {self.D}")
@@ -887,12 +896,14 @@ def loglikes(logits, *, normalize: bool = True, scale: float = 1.0, log_prior=No
     out, out_row    rows of V float32 to write into, and int32 [N], the row of
                     each result (default: row n), e.g. Stream.frames viewed as rows
 
-    Returns `out`.  Enqueued on the current stream."""
+    Returns `out`.  Enqueued on the current stream.  There is no backward pass:
+    tensors that require a gradient are refused."""
     torch = _torch()
     f32, i32, i64 = torch.float32, torch.int32, torch.int64
     types = _types(torch)
     dev = logits.device
     _matrix(logits, types, dev, "logits")
+    _no_gradient(torch, "loglikes", logits, log_prior, repetition, presence, frequency, out)
     N, V = logits.shape
     p_prior = _vector(log_prior, f32, dev, V, "log_prior")
     p_request, p_mask_of = _vector(request, i32, dev, N, "request"), _vector(mask_of, i32, dev, N, "mask_of")
@@ -909,6 +920,7 @@ def loglikes(logits, *, normalize: bool = True, scale: float = 1.0, log_prior=No
         raise ValueError("penalties need a history")
     if bias is not None:
         off, ids, values = bias
+        _no_gradient(torch, "loglikes", values)
         if history is None:
             Q = off.numel() - 1
         n_bias = ids.numel()

@@ -325,3 +325,18 @@ def test_more_rows_than_a_launch_takes(wf, dtype):
             plain.close(y[n0:n0 + 4096], want[:N - n0], bound[:N - n0])
     assert torch.equal(y[4096:1 << 27].view(-1, 4096, P), y[:4096].expand((1 << 27) // 4096 - 1, 4096, P))
     assert torch.equal(y[1 << 27:1 << 28].view(-1, 4096, P), y[:4096].expand((1 << 27) // 4096, 4096, P))
+
+
+def test_gradients_are_refused_not_lost(wf):
+    d = make(8, 64, 32, 3, 8, BF16)
+    head, x = head_of(wf, d), d["x"].to(DEV)
+    y = head.project(x)
+    p = torch.nn.Parameter(x.clone())
+    for call in (lambda: head.project(p), lambda: head.project(p * 2), lambda: head.project(x, out=torch.nn.Parameter(y.clone()))):
+        with pytest.raises(ValueError, match="no backward"):
+            call()
+    with torch.no_grad():
+        assert torch.equal(head.project(p), y)
+    assert torch.equal(head.project(p.detach()), y)
+    # (weights are taken detached)
+    assert torch.equal(wf.Head(torch.nn.Parameter(d["weight"].to(DEV)), d["bias"].to(DEV)).project(x), y)

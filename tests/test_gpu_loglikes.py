@@ -275,3 +275,16 @@ def test_more_rows_than_a_launch_takes(wf):
     want = 0.5 * (torch.log_softmax(z.double(), 1) - prior.double())
     # (three roundings of values below 16, those of the sum and the logarithm, halved)
     assert float((y.double() - want).abs().max()) <= 64 * 2.0 ** -24
+
+
+def test_gradients_are_refused_not_lost(wf):
+    d = make(5, 64, F32, Q=3, history=10, biases=10, prior=True)
+    on = {k: tuple(t.to(DEV) for t in v) if isinstance(v, tuple) else v.to(DEV) for k, v in d.items()}
+    want = wf.loglikes(**on)
+    for k in ("logits", "log_prior", "repetition", "presence", "frequency"):
+        with pytest.raises(ValueError, match="no backward"):
+            wf.loglikes(**dict(on, **{k: on[k].clone().requires_grad_()}))
+    with pytest.raises(ValueError, match="no backward"):
+        wf.loglikes(**dict(on, bias=(*on["bias"][:2], on["bias"][2].clone().requires_grad_())))
+    with torch.no_grad():
+        assert torch.equal(wf.loglikes(**dict(on, logits=on["logits"].clone().requires_grad_())), want)
