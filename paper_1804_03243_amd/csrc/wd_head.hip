@@ -900,8 +900,9 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
     if (kinds > 0) {
       one = kinds == 1 && __all(least == 0);
       mixed = kinds > kKinds || !__all(fits);
-      if (!mixed && !one) {
-        // zeros times an infinite weight would be a NaN in another adapter's row
+      if (!mixed) {
+        // zeros times an infinite weight would be a NaN: in another adapter's row, and in
+        // the adapter's own, whose later terms may be zero
         __syncthreads();
         const int per = a.rp / 8;
         bool bad = false;

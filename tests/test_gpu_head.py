@@ -340,3 +340,20 @@ def test_gradients_are_refused_not_lost(wf):
     assert torch.equal(head.project(p.detach()), y)
     # (weights are taken detached)
     assert torch.equal(wf.Head(torch.nn.Parameter(d["weight"].to(DEV)), d["bias"].to(DEV)).project(x), y)
+
+
+@pytest.mark.parametrize("dtype,same", [(BF16, False), (F16, False), (BF16, True)])
+@pytest.mark.parametrize("N,D,P,R,run", [(3, 64, 80, 8, 1), (10, 64, 80, 12, 3), (60, 72, 130, 40, 20), (200, 64, 96, 8, 200), (200, 64, 96, 40, 64),
+                                         (300, 333, 70, 5, 300), (700, 64, 1000, 16, 256), (700, 64, 1000, 9, 30), (700, 64, 1000, 96, 100),
+                                         (8300, 72, 2100, 16, 1000), (8300, 72, 2100, 70, 1000), (1300, 77, 2100, 12, 700)])
+def test_own_adapters_infinities(wf, dtype, same, N, D, P, R, run):
+    """Infinite weights of a row's own adapter: the formula's infinities, not NaN."""
+    G = 4
+    d = make(N, D, P, G, R, dtype, seed=N + R, adapters="runs")
+    d["adapter"] = ((torch.arange(N) // run) % (G + 1)).to(torch.int32)
+    gen = torch.Generator().manual_seed(N)
+    for k, v in enumerate([float("inf"), float("-inf"), float("inf")]):
+        at = torch.randint(0, G, (5,), generator=gen), torch.randint(0, P, (5,), generator=gen), torch.randint(0, R, (5,), generator=gen)
+        d["b"][at] = v
+    d["b"][0, P // 2, R - 1] = float("inf")
+    check(wf, d, dtype if same else F32)
