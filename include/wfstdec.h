@@ -374,9 +374,11 @@ typedef struct {
  * of rows; outside 0..G-1, or adapter NULL: the shared layer alone), n < N.
  * x: N rows of h->type, x_ld >= D.  out: N rows of out_type (WD_F32 or
  * h->type), out_ld >= P, no overlap with the inputs.  Products are exact, sums
- * are kept in 32 bits, A_g x in 16 bits of mantissa or more; one rounding to
- * out_type at the end.  A row never sees another row's adapter (its infinities
- * and NaNs included).  ws: device, ws_bytes >= wd_project_workspace_bytes(h, N),
+ * are kept in 32 bits.  A_g x is held to 2^-16 of itself or, where that is more,
+ * to 2^-22 of the magnitudes that its sum adds up or 2^-38 of the row's largest
+ * (in 32 bits for calls of up to four rows).  One rounding to out_type at the
+ * end.  A row never sees another row's adapter (its infinities and NaNs
+ * included).  ws: device, ws_bytes >= wd_project_workspace_bytes(h, N),
  * 256-byte aligned, in use until the enqueued work has run. */
 wd_status wd_project_workspace_bytes(const wd_head* h, int64_t N, size_t* bytes);
 wd_status wd_project(const wd_head* h, const void* x, int64_t x_ld, int64_t N, const int32_t* adapter, void* out,

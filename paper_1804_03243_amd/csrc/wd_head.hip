@@ -4,8 +4,8 @@
 // has the mantissa the output needs, so that B_g u runs on the matrix
 // instructions too: u = u_0 + u_1 (+ u_2), each the rounding of what the ones
 // before left.  bfloat16 takes three terms (24 bits) for a 32-bit output and two
-// for its own; half precision takes two (22 bits), of u divided by a power of two
-// per row that puts the row's largest u in [1, 2).
+// for its own; half precision takes two (22 bits), where they do not hold a row as it
+// is (terms_hold) of u divided by a power of two per row.
 //
 // Then W x in tiles of matrix instructions; the adapters' part, the bias and the
 // rounding to the output's type are added as a tile is stored.  W is the
@@ -141,23 +141,39 @@ __device__ __forceinline__ void store_u(const HeadArgs& a, int64_t n, int r, flo
   for (int k = 0; k < TERMS; ++k) a.u[n * a.ul + k * a.rp + r] = t[k].u;
 }
 
-// The power of two that a row's u are divided by: 1 for bfloat16, which has the
-// range of 32 bits, and where half precision's two terms hold the row as it is
-// (its largest value to 21 bits).
+// Whether half precision's two terms hold u as it is: to 2^-16 of itself or 2^-22 of
+// `parts`, the magnitudes of what its sum adds up (which 32-bit sums are off by as much
+// for).  Their first is good to 11 bits and so is the second, but for its
+// least place of 2^-24: a rank whose A x is small beside the row's others needs more.
 template <class T>
-__device__ __forceinline__ float row_power(float largest) {
+__device__ __forceinline__ bool terms_hold(float u, float parts) {
+  if constexpr (__is_same(T, Bf16)) {
+    return true;
+  } else {
+    const float r = u - T::of(u).f(), e = r - T::of(r).f();
+    return !(fabsf(e) > fmaxf(0x1p-16f * fabsf(u), 0x1p-22f * parts));  // (one that is not finite is its first term)
+  }
+}
+
+// The power of two that a row's u are divided by: 1 for bfloat16, which has the
+// range of 32 bits, and where half precision's two terms `hold` every u of the row.  Else
+// one that puts the largest in [2^14, 2^15), so that what the terms leave of any is at
+// most 2^-39 of the largest.
+template <class T>
+__device__ __forceinline__ float row_power(float largest, bool hold) {
   if constexpr (__is_same(T, Bf16)) {
     return 1.0f;
   } else {
     const uint32_t e = __float_as_uint(largest) & 0x7f800000u;
-    if (e == 0 || (largest >= 0x1p-4f && largest < 0x1p15f)) return 1.0f;
-    return fminf(fmaxf(__uint_as_float(e), 0x1p-60f), 0x1p126f);
+    if (e == 0 || (hold && largest < 0x1p15f)) return 1.0f;
+    return fmaxf(__uint_as_float(e) * 0x1p-14f, 0x1p-70f);
   }
 }
 
 __device__ __forceinline__ float finite_abs(float u) { return fabsf(u) < INFINITY ? fabsf(u) : 0.0f; }
 
-// The products of a row of n elements with two others, by a wavefront.
+// The products of a row of n elements with two others, by a wavefront: each sum in two
+// parts, in the lanes of even and of odd number.
 template <class T>
 __device__ __forceinline__ void row_products(const T* x, const T* sx, const T* w0, const T* w1, const T* sw, int n,
                                              float& s0, float& s1) {
@@ -180,7 +196,7 @@ __device__ __forceinline__ void row_products(const T* x, const T* sx, const T* w
       s1 = fmaf(xe[i].f(), e1[i].f(), s1);
     }
   }
-  for (int o = 32; o > 0; o >>= 1) {
+  for (int o = 32; o > 1; o >>= 1) {
     s0 += __shfl_xor(s0, o);
     s1 += __shfl_xor(s1, o);
   }
@@ -190,7 +206,7 @@ __device__ __forceinline__ void row_products(const T* x, const T* sx, const T* w
 // in flight together).
 template <class T, int TERMS>
 __global__ void __launch_bounds__(512) k_low_row(HeadArgs a) {
-  __shared__ float us[WD_MAX_RANK];
+  __shared__ float us[WD_MAX_RANK], parts[WD_MAX_RANK];
   const int64_t n = blockIdx.x;
   const int g = adapter_of(a, n), D = a.h.D, R = a.h.rank;
   if (g < 0) {
@@ -205,13 +221,21 @@ __global__ void __launch_bounds__(512) k_low_row(HeadArgs a) {
   for (int r = wave * 2; r < R; r += 16) {
     float s0, s1;
     row_products(x, last_x<T>(a), w + (int64_t)r * D, w + (int64_t)min(r + 1, R - 1) * D, last_a<T>(a), D, s0, s1);
-    if (lane < 2 && r + lane < R) us[r + lane] = (lane ? s1 : s0) * sc;
+    const float t0 = __shfl_xor(s0, 1), t1 = __shfl_xor(s1, 1);
+    if (lane < 2 && r + lane < R) {
+      us[r + lane] = (lane ? s1 + t1 : s0 + t0) * sc;
+      parts[r + lane] = (lane ? fabsf(s1) + fabsf(t1) : fabsf(s0) + fabsf(t0)) * fabsf(sc);
+    }
   }
   __syncthreads();
   float top = 0.0f;
-  for (int r = lane; r < R; r += 64) top = fmaxf(top, finite_abs(us[r]));
+  bool hold = true;
+  for (int r = lane; r < R; r += 64) {
+    top = fmaxf(top, finite_abs(us[r]));
+    hold &= terms_hold<T>(us[r], parts[r]);
+  }
   for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
-  const float p = row_power<T>(top);
+  const float p = row_power<T>(top, __all(hold));
   if (threadIdx.x == 0) a.us[n] = p;
   if ((int)threadIdx.x < a.rp) store_u<T, TERMS>(a, n, threadIdx.x, (int)threadIdx.x < R ? us[threadIdx.x] / p : 0.0f);
   if (a.uk + (int)threadIdx.x < a.ul) a.u[n * a.ul + a.uk + threadIdx.x] = 0;
@@ -304,8 +328,8 @@ __global__ void __launch_bounds__(256) k_low_tile(HeadArgs a) {
       for (int r = 0; r < R; r += 2) {
         float s0, s1;
         row_products(x, last_x<T>(a), w + (int64_t)r * D, w + (int64_t)min(r + 1, R - 1) * D, last_a<T>(a), D, s0, s1);
-        // (the other wavefronts' parts of these sums are zero)
-        if (lane < 8 && r + (lane >> 2) < R) sums[lane & 3][i][r + (lane >> 2)] = lane == 0 ? s0 : lane == 4 ? s1 : 0.0f;
+        // (two parts, and zeros for the other two wavefronts')
+        if (lane < 8 && r + (lane >> 2) < R) sums[lane & 3][i][r + (lane >> 2)] = lane & 2 ? 0.0f : lane & 4 ? s1 : s0;
       }
     }
   }
@@ -314,15 +338,21 @@ __global__ void __launch_bounds__(256) k_low_tile(HeadArgs a) {
   const int gi = adapter_of(a, n0 + i);
   const float sc = gi >= 0 && a.h.scale ? a.h.scale[gi] : 1.0f;
   float u[RB], top = 0.0f;
+  bool hold = true;
 #pragma unroll
   for (int b = 0; b < RB; ++b) {
     const int r = b * 16 + r0;
-    u[b] = r < R ? ((sums[0][i][r] + sums[1][i][r]) + (sums[2][i][r] + sums[3][i][r])) * sc : 0.0f;
+    float q[4];
+#pragma unroll
+    for (int w = 0; w < 4; ++w) q[w] = r < R ? sums[w][i][r] : 0.0f;
+    u[b] = ((q[0] + q[1]) + (q[2] + q[3])) * sc;
+    hold &= terms_hold<T>(u[b], (fabsf(q[0]) + fabsf(q[1]) + fabsf(q[2]) + fabsf(q[3])) * fabsf(sc));
     top = fmaxf(top, finite_abs(u[b]));
   }
   for (int o = 8; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  hold = (__ballot(!hold) >> (lane & 48) & 0xffff) == 0;  // (of the row's 16 lanes)
   if (n0 + i >= a.N) return;
-  const float p = gi < 0 ? 1.0f : row_power<T>(top);
+  const float p = gi < 0 ? 1.0f : row_power<T>(top, hold);
   if (r0 == 0) a.us[n0 + i] = p;
 #pragma unroll
   for (int b = 0; b < RB; ++b)
@@ -690,7 +720,8 @@ __global__ void __launch_bounds__(512) k_rows(HeadArgs a) {
       float s0, s1;
       row_products((const T*)a.x + n * a.x_ld, last_x<T>(a), w0, w0 + (r + 1 < R ? D : 0), last_a<T>(a), D, s0, s1);
       const float sc = a.h.scale ? a.h.scale[gn] : 1.0f;
-      if (lane < 2 && r + lane < R) low_u[n][r + lane] = (lane ? s1 : s0) * sc;
+      const float t0 = __shfl_xor(s0, 1), t1 = __shfl_xor(s1, 1);
+      if (lane < 2 && r + lane < R) low_u[n][r + lane] = (lane ? s1 + t1 : s0 + t0) * sc;
     }
     // (read behind the barrier below)
   } else if (g >= 0) {

@@ -357,3 +357,16 @@ def test_own_adapters_infinities(wf, dtype, same, N, D, P, R, run):
         d["b"][at] = v
     d["b"][0, P // 2, R - 1] = float("inf")
     check(wf, d, dtype if same else F32)
+
+
+@pytest.mark.parametrize("adapters", ["runs", "mixed"])
+@pytest.mark.parametrize("N,D,P,R", [(10, 16, 48, 8), (100, 16, 96, 12), (400, 24, 300, 8), (700, 16, 96, 8), (1300, 24, 1000, 20),
+                                     (8300, 16, 2100, 8)])
+def test_half_precision_ranks_far_below_the_others(wf, adapters, N, D, P, R):
+    """Single ranks of A scaled down and the same columns of B up: their A x is held
+    to 16 bits of its own, not of the row's largest."""
+    d = make(N, D, P, 3, R, F16, seed=N + D, adapters=adapters)
+    for r, by in ((1, 12), (4, 9), (R - 1, 13)):
+        d["a"][:, r] *= 2.0 ** -by
+        d["b"][:, :, r] *= 2.0 ** by
+    check(wf, d)
