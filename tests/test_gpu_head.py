@@ -370,3 +370,58 @@ def test_half_precision_ranks_far_below_the_others(wf, adapters, N, D, P, R):
         d["a"][:, r] *= 2.0 ** -by
         d["b"][:, :, r] *= 2.0 ** by
     check(wf, d)
+
+
+def check_on_gpu(wf, d, out_dtype=F32):
+    """As check(), in 64 bits on the GPU, for rows of sorted adapters."""
+    dev = {k: v.to(DEV) for k, v in d.items()}
+    y = head_of(wf, d).project(dev["x"], dev["adapter"], out_dtype=out_dtype)
+    X, W, R = dev["x"].double(), dev["weight"].double(), d["a"].shape[1]
+    rel, least = plain.rounding(out_dtype)
+    worst = 0.0
+    for g in range(-1, d["a"].shape[0]):
+        rows = torch.nonzero(dev["adapter"] == g)[:, 0]
+        for r in rows.split(4096) if len(rows) else ():
+            want = X[r] @ W.T + dev["bias"].double()
+            err = (X.shape[1] + 8) * plain.EPS * (X[r].abs() @ W.abs().T + dev["bias"].double().abs())
+            if g >= 0:
+                A, B, s = dev["a"][g].double(), dev["b"][g].double(), float(d["scale"][g])
+                u, um = s * (X[r] @ A.T), s * (X[r].abs() @ A.abs().T)
+                want += u @ B.T
+                err += ((X.shape[1] + 2 * R + 16) * plain.EPS * um + 2.0 ** -16 * u.abs()) @ B.abs().T
+            off = (y[r].double() - want).abs() - (err * (1 + rel) + rel * want.abs() + least)
+            worst = max(worst, float(off.max()))
+    assert worst <= 0.0
+    return y
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("run", [2000, 700, 41])
+@pytest.mark.parametrize("N,D,P,R", [(2000, 333, 1600, 11), (300, 333, 70, 5), (2000, 1027, 1601, 16), (150, 777, 500, 40)])
+def test_unaligned_rows_of_many_steps(wf, dtype, run, N, D, P, R):
+    """Widths that are no multiple of eight, in tiles of 64 and of 128: the rows of
+    later steps go through registers while earlier ones are multiplied."""
+    d = make(N, D, P, 3, R, dtype, seed=N + D, adapters="runs")
+    d["adapter"] = ((torch.arange(N) // run + 1) % 4 - 1).to(torch.int32)
+    check_on_gpu(wf, d)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("run", [5000, 900, 90, 7])
+@pytest.mark.parametrize("N,D,P,R", [(2500, 128, 1300, 65), (2500, 136, 1300, 100), (4500, 64, 4200, 128), (4500, 72, 4100, 81)])
+def test_ranks_above_64_in_large_tiles(wf, dtype, run, N, D, P, R):
+    d = make(N, D, P, 3, R, dtype, seed=N + R, adapters="runs")
+    d["adapter"] = ((torch.arange(N) // run + 1) % 4 - 1).to(torch.int32)
+    check_on_gpu(wf, d)
+
+
+@pytest.mark.parametrize("dtype,out", [(BF16, F32), (BF16, BF16), (F16, F32), (F16, F16)])
+@pytest.mark.parametrize("D", [72, 77])
+@pytest.mark.parametrize("P", [8001, 8004])
+def test_outputs_past_the_caches(wf, dtype, out, D, P):
+    """256 MB of outputs and more, rows that do not end at a whole store."""
+    N = 17003 if out is not F32 else 8503
+    d = make(N, D, P, 3, 8, dtype, seed=N + P, adapters="runs")
+    d["adapter"] = ((torch.arange(N) // 1500 + 1) % 4 - 1).to(torch.int32)
+    assert N * P * (4 if out is F32 else 2) >= 256 << 20
+    check_on_gpu(wf, d, out)

@@ -125,3 +125,21 @@ def test_more_rows_than_a_launch_takes(wf):
     bits = torch.from_numpy(plain.label_masks(g, P, np.arange(S + 1), np.arange(S))).to(DEV)  # of each state alone
     want = bits[states[:2 * N:2].long()] | bits[states[1:2 * N:2].long()]
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("S,A,P,hub", [(30_000, 90_000, 3000, 400), (30_000, 90_000, 120_000, 50), (30_000, 120_000, 500_000, 9)])
+@pytest.mark.parametrize("rows,most", [(2, 30_000), (1, 40_000), (5, 70_000)])
+def test_several_workgroups_a_row(wf, S, A, P, hub, rows, most):
+    """Sets of 8192 states and more on average: parts of a row joined in memory."""
+    g = wide_graph(S, A, P, S + P, hub)
+    graph = wf.Graph(g, P)
+    rng = np.random.default_rng([rows, most, P])
+    counts = rng.integers(most // 2, most + 1, rows)
+    offsets = np.concatenate([[0], np.cumsum(counts)]).astype(np.int64)
+    states = rng.integers(0, S // 3, int(offsets[-1])).astype(np.int32)  # (many labels of many states, others of none)
+    assert len(states) // rows >= 8192
+    wide = torch.full((rows, (P + 31) // 32 + 3), 7, dtype=torch.int32, device=DEV)
+    out = wide[:, :(P + 31) // 32]
+    graph.label_masks(torch.from_numpy(offsets).to(DEV), torch.from_numpy(states).to(DEV), out=out)
+    assert np.array_equal(out.cpu().numpy(), plain.label_masks(g, P, offsets, states))
+    assert bool((wide[:, (P + 31) // 32:] == 7).all())

@@ -288,3 +288,20 @@ def test_gradients_are_refused_not_lost(wf):
         wf.loglikes(**dict(on, bias=(*on["bias"][:2], on["bias"][2].clone().requires_grad_())))
     with torch.no_grad():
         assert torch.equal(wf.loglikes(**dict(on, logits=on["logits"].clone().requires_grad_())), want)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N,V", [(13500, 5001), (2000, 33555)])
+def test_outputs_past_the_caches(wf, dtype, N, V):
+    """256 MB of outputs and more, rows that do not end at a whole store."""
+    z = (torch.randn((N, V), generator=torch.Generator(DEV).manual_seed(31), device=DEV) * 3).to(dtype)
+    prior = torch.log_softmax(torch.randn(V, generator=torch.Generator(DEV).manual_seed(32), device=DEV), 0)
+    assert N * V * 4 >= 256 << 20
+    y = wf.loglikes(z, log_prior=prior, scale=0.9)
+    for n0 in range(0, N, 1000):
+        x = z[n0:n0 + 1000].double()
+        want = 0.9 * (torch.log_softmax(x, 1) - prior.double())
+        # |x - max|, the sum's logarithm and the prior are below 64 together, each rounded
+        # three times; the sum is of V terms over 64 lanes
+        bound = 0.9 * (64 * 4 + V / 64 + 128) * plain.EPS
+        assert float((y[n0:n0 + 1000].double() - want).abs().max()) <= bound
