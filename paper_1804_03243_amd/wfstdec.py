@@ -894,7 +894,9 @@ def loglikes(logits, *, normalize: bool = True, scale: float = 1.0, log_prior=No
     mask, mask_of   int32 words [M, >= ceil(V/32)] (Graph.label_masks) and
                     int32 [N], the rows' masks (default: row n has mask n)
     out, out_row    rows of V float32 to write into, and int32 [N], the row of
-                    each result (default: row n), e.g. Stream.frames viewed as rows
+                    each result, all different (default: row n), e.g. Stream.frames
+                    viewed as rows; out may be the logits themselves (float32,
+                    without out_row), else it shares no memory with them
 
     Returns `out`.  Enqueued on the current stream.  There is no backward pass:
     tensors that require a gradient are refused."""
@@ -926,8 +928,10 @@ def loglikes(logits, *, normalize: bool = True, scale: float = 1.0, log_prior=No
         n_bias = ids.numel()
         p_boff, p_bid = _vector(off, i64, dev, Q + 1, "bias's offsets"), _vector(ids, i32, dev, n_bias, "bias's labels")
         p_bval = _vector(values, f32, dev, n_bias, "bias's values")
-    if Q < 1 and (history is not None or bias is not None):
+    if Q < 0:
         raise ValueError("history and bias need offsets, one more than requests")
+    if Q == 0:  # (lists of no request)
+        p_hoff = p_boff = None
     p_mask, n_masks, mask_ld = None, 0, 0
     if mask is not None:
         _matrix(mask, (i32,), dev, "mask")

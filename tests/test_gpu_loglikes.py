@@ -305,3 +305,17 @@ def test_outputs_past_the_caches(wf, dtype, N, V):
         # three times; the sum is of V terms over 64 lanes
         bound = 0.9 * (64 * 4 + V / 64 + 128) * plain.EPS
         assert float((y[n0:n0 + 1000].double() - want).abs().max()) <= bound
+
+
+def test_lists_of_no_request(wf):
+    """Offsets of one entry are lists of no request: an empty batch's, and rows without one."""
+    d = make(4, 70, F32, seed=33, masks=2, prior=True)
+    none, ids = torch.zeros(1, dtype=torch.int64), torch.zeros(0, dtype=torch.int32)
+    lists_ = dict(history=(none, ids), bias=(none, ids, torch.zeros(0)), repetition=torch.zeros(0), presence=torch.zeros(0),
+                  frequency=torch.zeros(0))
+    check(wf, dict(d, **lists_))
+    empty = dict(d, logits=d["logits"][:0], request=d["request"][:0], mask_of=d["mask_of"][:0], **lists_)
+    assert tuple(call(wf, empty).shape) == (0, 70)
+    for bad in (dict(history=(none[:0], ids)), dict(bias=(none[:0], ids, torch.zeros(0)))):
+        with pytest.raises(ValueError):
+            call(wf, dict(d, **bad))
