@@ -21,7 +21,6 @@ namespace wd {
 
 struct ScoreArgs {
   wd_loglikes_args a;
-  int64_t n0;       // first row of this launch
   float2* part;     // [N][slices] maximum and sum of each slice of a row
   uint32_t slices;  // slices of a row
   bool stream;      // outputs past the caches
@@ -68,7 +67,7 @@ __global__ void __launch_bounds__(THREADS) k_loglikes(ScoreArgs args) {
   const wd_loglikes_args& a = args.a;
   extern __shared__ uint32_t table[];  // [kSlice], where there are histories or biases
   __shared__ float red[2][kWavesHere];
-  const int64_t n = args.n0 + (PHASE == kWhole ? blockIdx.x : blockIdx.x / args.slices);
+  const int64_t n = PHASE == kWhole ? blockIdx.x : blockIdx.x / args.slices;
   const int c0 = PHASE == kWhole ? 0 : (int)(blockIdx.x % args.slices) * kSlice;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int64_t to = n;
@@ -187,7 +186,7 @@ __global__ void __launch_bounds__(THREADS) k_loglikes(ScoreArgs args) {
 #pragma unroll
     for (int w = 1; w < kWavesHere; ++w) s += red[1][w];
     if (PHASE == kStats) {
-      if (threadIdx.x == 0) args.part[n * args.slices + blockIdx.x % args.slices] = make_float2(top, s);
+      if (threadIdx.x == 0) args.part[blockIdx.x] = make_float2(top, s);
       return;
     }
     lse = logf(s);
@@ -237,12 +236,42 @@ __global__ void __launch_bounds__(THREADS) k_loglikes(ScoreArgs args) {
 constexpr int kWholeLabels = 32768;
 constexpr int kSliceThreads = 512, kSliceEach = 16, kSliceLabels = kSliceThreads * kSliceEach;
 
+// The arguments without their first n rows.
+inline ScoreArgs rows_from(ScoreArgs args, int64_t n) {
+  wd_loglikes_args& a = args.a;
+  a.N -= n;
+  a.logits = (const char*)a.logits + n * a.ld * (a.type == WD_F32 ? 4 : 2);
+  args.part = args.part ? args.part + n * args.slices : nullptr;
+  if (a.out_row)
+    a.out_row += n;
+  else
+    a.out += n * a.out_ld;
+  if (a.request) {
+    a.request += n;
+  } else {  // (row n is request n)
+    a.n_requests = (int32_t)std::max<int64_t>(0, a.n_requests - n);
+    if (a.hist_off) a.hist_off += n;
+    if (a.bias_off) a.bias_off += n;
+    if (a.repetition) a.repetition += n;
+    if (a.presence) a.presence += n;
+    if (a.frequency) a.frequency += n;
+  }
+  if (a.mask_of) {
+    a.mask_of += n;
+  } else if (a.mask) {
+    a.n_masks = std::max<int64_t>(0, a.n_masks - n);
+    a.mask += n * a.mask_ld;
+  }
+  return args;
+}
+
 // (A launch has fewer than 2^32 threads: more rows than that take several.)
 template <class T, int THREADS, int EACH, ScorePhase PHASE>
-void launch_slices(ScoreArgs args, hipStream_t s) {
-  const int64_t most = (((int64_t)1 << 32) / THREADS - 1) / args.slices;
-  for (; args.n0 < args.a.N; args.n0 += most) {
-    const dim3 grid((uint32_t)(std::min(most, args.a.N - args.n0) * args.slices)), block(THREADS);
+void launch_slices(const ScoreArgs& all, hipStream_t s) {
+  const int64_t most = (((int64_t)1 << 32) / THREADS - 1) / all.slices;
+  for (int64_t n0 = 0; n0 < all.a.N; n0 += most) {
+    const ScoreArgs args = n0 ? rows_from(all, n0) : all;
+    const dim3 grid((uint32_t)(std::min(most, args.a.N) * args.slices)), block(THREADS);
     if (!args.a.hist_off && !args.a.bias_off) {
       hipLaunchKernelGGL((k_loglikes<T, THREADS, EACH, PHASE, false>), grid, block, 0, s, args);
       continue;
@@ -256,7 +285,7 @@ void launch_slices(ScoreArgs args, hipStream_t s) {
 
 template <class T>
 void launch_loglikes(const wd_loglikes_args* a, void* ws, hipStream_t s) {
-  ScoreArgs args{*a, 0, (float2*)ws, 1, (uint64_t)a->N * a->V * 4 >= (256u << 20)};
+  ScoreArgs args{*a, (float2*)ws, 1, (uint64_t)a->N * a->V * 4 >= (256u << 20)};
   if (a->V <= 2048)
     launch_slices<T, 256, 8, kWhole>(args, s);
   else if (a->V <= 4096)

@@ -319,3 +319,27 @@ def test_lists_of_no_request(wf):
     for bad in (dict(history=(none[:0], ids)), dict(bias=(none[:0], ids, torch.zeros(0)))):
         with pytest.raises(ValueError):
             call(wf, dict(d, **bad))
+
+
+@pytest.mark.parametrize("given", [True, False])
+def test_requests_and_masks_of_later_launches(wf, given):
+    """Rows beyond the first launch keep their own request, mask and output row."""
+    N, V, Q = (1 << 24) + 40, 3, (1 << 24) + 30  # (the last ten rows have no request and no mask of their own)
+    gen = torch.Generator(DEV).manual_seed(34)
+    z = torch.randn((N, V), generator=gen, device=DEV)
+    off = torch.arange(Q + 1, device=DEV)  # (a label each)
+    ids = torch.randint(0, V, (Q,), generator=gen, device=DEV, dtype=torch.int32)
+    presence, values = torch.rand(Q, generator=gen, device=DEV), torch.randn(Q, generator=gen, device=DEV)
+    mask = torch.randint(1, 8, (Q, 1), generator=gen, device=DEV, dtype=torch.int32)
+    kw = {}
+    if given:
+        kw = dict(request=torch.arange(N, device=DEV, dtype=torch.int32), mask_of=torch.arange(N, device=DEV, dtype=torch.int32),
+                  out_row=torch.arange(N - 1, -1, -1, device=DEV, dtype=torch.int32), out=torch.empty((N, V), device=DEV))
+    y = wf.loglikes(z, normalize=False, history=(off, ids), presence=presence, bias=(off, ids, values), mask=mask, **kw)
+    y = y.flip(0) if given else y
+    want = z.clone()  # (in 32 bits: the presence off, then the bias on, each rounded once)
+    at = ids.long()[:, None]
+    want[:Q] = want[:Q].scatter(1, at, (want[:Q].gather(1, at) - presence[:, None]) + values[:, None])
+    keep = (mask >> torch.arange(V, device=DEV)) & 1
+    want[:Q] = torch.where(keep == 1, want[:Q], torch.full((), -INF, device=DEV))
+    assert torch.equal(y, want)
