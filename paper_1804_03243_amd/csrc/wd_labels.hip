@@ -24,7 +24,6 @@ struct LabelArgs {
   const int32_t* ilabel;
   uint32_t S, words, parts;
   int64_t A, N, n_states, ld;
-  int64_t n0;  // first row of this launch
   const int64_t* row;
   const int32_t* states;
   uint32_t* mask;
@@ -122,7 +121,7 @@ __global__ void __launch_bounds__(1024) k_label_sets(LabelArgs a) {
   extern __shared__ uint32_t lds[];
   __shared__ uint2 deals[16][64];
   const uint32_t wave = wave_id(), lane = lane_id();
-  const int64_t n = a.n0 + blockIdx.x / a.parts;
+  const int64_t n = blockIdx.x / a.parts;
   const uint32_t part = blockIdx.x % a.parts;
   uint32_t* out = a.mask + n * a.ld;
   uint32_t* bits = LDS ? lds : out;
@@ -165,7 +164,7 @@ extern "C" wd_status wd_label_masks(const wd_graph* g, int64_t N, const int64_t*
   if ((uintptr_t)off & 7 || (uintptr_t)states & 3 || (uintptr_t)mask & 3)
     return fail(WD_EINVAL, "label_masks: misaligned array");
   if (N > INT32_MAX / 64) return fail(WD_EINVAL, "label_masks: too many rows for one call");
-  LabelArgs a{g->dg.off, g->dg.ilabel_id, g->dg.S, words, 1, g->A, N, n_states, mask_ld, 0, off, states, mask};
+  LabelArgs a{g->dg.off, g->dg.ilabel_id, g->dg.S, words, 1, g->A, N, n_states, mask_ld, off, states, mask};
   hipStream_t s = (hipStream_t)stream;
   // (the rows' own lengths are on the device: the average decides)
   const int64_t mean = n_states / N;
@@ -182,8 +181,9 @@ extern "C" wd_status wd_label_masks(const wd_graph* g, int64_t N, const int64_t*
     hipLaunchKernelGGL(k_label_zero, dim3((uint32_t)std::min<uint64_t>((all + 255) / 256, 4096)), dim3(256), 0, s, a);
   }
   // (a launch has fewer than 2^32 threads: more rows than that take several)
-  for (const int64_t most = ((1 << 22) - 1) / a.parts; a.n0 < N; a.n0 += most) {
-    const dim3 grid((uint32_t)(std::min(most, N - a.n0) * a.parts));
+  const int64_t most = ((1 << 22) - 1) / a.parts;
+  for (; a.N > 0; a.N -= most, a.row += most, a.mask += most * mask_ld) {
+    const dim3 grid((uint32_t)(std::min(most, a.N) * a.parts));
     if (words <= kLdsWords)
       hipLaunchKernelGGL(k_label_sets<true>, grid, dim3(1024), words * 4, s, a);
     else
