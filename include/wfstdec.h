@@ -411,7 +411,7 @@ typedef struct {
   const int64_t* hist_off;   /* [Q+1] into hist; NULL: no histories.  Clamped to 0..n_hist */
   const int32_t* hist;       /* labels; those outside 0..V-1 are left out */
   int64_t n_hist;
-  const float* repetition;   /* [Q], > 0; NULL: 1 */
+  const float* repetition;   /* [Q], > 0, with a normal reciprocal; NULL: 1 */
   const float* presence;     /* [Q]; NULL: 0 */
   const float* frequency;    /* [Q]; NULL: 0 */
   const int64_t* bias_off;   /* [Q+1] into bias_id, bias_val; NULL: no biases.  Clamped to 0..n_bias */

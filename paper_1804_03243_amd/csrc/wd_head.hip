@@ -7,8 +7,9 @@
 // for its own; half precision takes two (22 bits), where they do not hold a row as it
 // is (terms_hold) of u divided by a power of two per row.
 //
-// Then W x in tiles of matrix instructions; the adapters' part, the bias and the
-// rounding to the output's type are added as a tile is stored.  W is the
+// Then W x in tiles of matrix instructions.  B_g u of a tile's one or two adapters are
+// further steps of its product; of more it is added behind the product, as the bias
+// is, and the rounding to the output's type comes as a tile is stored.  W is the
 // matrix instruction's first operand and x its second, so that a lane holds
 // consecutive outputs of one row.
 #include <algorithm>
@@ -247,7 +248,10 @@ __global__ void __launch_bounds__(512) k_low_row(HeadArgs a) {
 // 32 consecutive bytes of their row, 128 of a row between them (the order of
 // the columns in a sum of products is free).  The adapters of the 16 rows are
 // taken one after another, each row keeping its own.  Rows of many adapters
-// (kLowMix) go one by one on the vector ALU instead.
+// (more than kLowMix among 16) go one by one on the vector ALU instead.  (1024 rows of
+// 1024 columns to 3000 outputs at rank 16, whole call: runs of 8 rows 41 us by matrix
+// instructions and 63 one by one, an adapter per row 79 and 80.  In between the
+// bound is low: runs of 4 rows would take 59 for 80, of 2 rows 60 for 74.)
 constexpr int kLowMix = 3;
 
 template <class T, int TERMS, int RB>
@@ -361,7 +365,11 @@ __global__ void __launch_bounds__(256) k_low_tile(HeadArgs a) {
 }
 
 // A workgroup per row spreads few rows over the chip; from kLowRows on the rows
-// share the reads of their adapter instead.
+// share the reads of their adapter instead.  (1024 columns to 3000 outputs, rows in
+// runs of 32, whole call: at rank 16 400 rows 17.0 us a workgroup each and 18.0 in
+// tiles, 700 22.5 and 20.6, 2048 40 and 34; at rank 64 256 rows 22.3 and 24.2, 512 29.1
+// and 29.3, 2048 76 and 58.  Rows of an adapter each stay faster by themselves: 2048 118
+// and 141.)
 constexpr int64_t kLowRows = 512;
 
 template <class T, int TERMS>
@@ -436,6 +444,9 @@ __device__ __forceinline__ bool not_finite(uint4 v) {
 
 // A wavefront's rows of more adapters than this take the vector ALU, whose lanes
 // each read their own row's B; the matrix instructions take the adapters in turn.
+// (16384 rows of 1024 columns to 6000 outputs at rank 16, 128 rows a wavefront, whole
+// call: 8 adapters among them 439 us in turn and 585 row by row, 16 653 and 612, 32 1092
+// and 670.)
 constexpr int kWaveMix = 16;
 
 // B_g u for the wavefront's rows n0.., added to acc; prow(j, i) is the output of
@@ -1106,7 +1117,9 @@ void launch_project(HeadArgs a, hipStream_t s) {
   // are one per compute unit at most: 128 rows of as many adapters, 512 -> 3000, take
   // 13.0 us and in tiles 18.8, 256 of 300 -> 1500 13.3 and 20.5; past that the tiles
   // are ahead (256 of 1024 -> 6000 33 us for 41), and for rows of one adapter throughout
-  // (128 of 1133 -> 1516 24 us for 30).
+  // (128 of 1133 -> 1516 24 us for 30).  Which adapters the rows use is known on the
+  // device only: the rule counts those that the head holds, so that 128 rows of one
+  // adapter take 24.0 us with a head of 20 adapters or 1000 and 20.5 with one of four.
   const bool many = a.adapter && (int64_t)a.h.n_adapters * 16 > a.N;
   const int64_t blocks64 = (a.N + 63) / 64;
   if (a.N <= 16)

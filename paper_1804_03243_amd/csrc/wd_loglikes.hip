@@ -8,9 +8,9 @@
 // count by additions in the lower ones (integer atomics: the order of the entries
 // does not matter; longer lists take the table in turn).  Then m = max z and s = sum
 // of exp(z - m) over the workgroup, in 32 bits, and y = (z - m) - log s.  Bound by
-// memory where rows are many (48 thousand rows of 6000 labels of 32 bits: 600 us, 5.1
-// TB/s, what a copy reaches), by the chain of reads request, offsets, list where they
-// are few.
+// memory where rows are many (67 thousand rows of 6000 labels of 32 bits: 590 us, 5.5
+// TB/s, a little more than a copy reaches), by the chain of reads request, offsets, list
+// where they are few.
 #include <algorithm>
 #include <cmath>
 
@@ -107,6 +107,8 @@ __global__ void __launch_bounds__(THREADS) k_loglikes(ScoreArgs args) {
   for (int j = 0; j < EACH; ++j) z[j] = raw[j / 4].v[j & 3].f();
   const bool has_hist = hist.b < hist.e, has_bias = bias.b < bias.e;  // (the same for the whole workgroup)
   if (LISTS && (has_hist || has_bias)) {
+    // (a product with the rounded reciprocal is off by up to 1.5 units of the last place,
+    // a quotient by half a one: one instruction a label for about ten)
     const float rho = has_hist && a.repetition ? a.repetition[q] : 1.0f, inv_rho = 1.0f / rho;
     const float pres = has_hist && a.presence ? a.presence[q] : 0.0f, freq = has_hist && a.frequency ? a.frequency[q] : 0.0f;
     const auto clear = [&]() {
@@ -230,9 +232,13 @@ __global__ void __launch_bounds__(THREADS) k_loglikes(ScoreArgs args) {
 
 // Rows of up to kWholeLabels labels are one slice: they are read once and their
 // lists are scattered once (400 rows of 30000 labels of 16 bits with histories and
-// biases: 39 us, in slices 73; 8 rows: 23 and 27 with the launch).  Longer ones go
-// in slices, twice (400 rows of 100000 labels: 155 us in slices of 8192 labels, 171
-// of 16384, 190 of 32768: more workgroups hide each other's waits for the lists).
+// biases, whole call: 33 us, in slices 48; 8 rows 13.6 and 16.7).  Longer ones go
+// in slices, twice (400 rows of 100000 labels: 109 us in slices of 8192 labels, 153
+// of 16384, 173 of 32768: more workgroups hide each other's waits for the lists).
+// A row's workgroup is the smallest that holds it (4000 rows of 16 bits with lists of
+// 500: 2048 labels 24 us by 256 threads of 8 and 27 of 16; 4096 35 by 256 of 16, 51 of 32;
+// 8192 72 by 256 of 32 and 98 by 1024 of 8 - 63 by 512 of 16 -; 16384 190 by 1024 of 16,
+// 231 of 32).  One row or 64 take the same time either way, to 1 us.
 constexpr int kWholeLabels = 32768;
 constexpr int kSliceThreads = 512, kSliceEach = 16, kSliceLabels = kSliceThreads * kSliceEach;
 

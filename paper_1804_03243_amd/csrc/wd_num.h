@@ -1,5 +1,5 @@
-// Device-side helpers of the operators that make log-likelihoods: 16-bit
-// types, loads and stores of any alignment, workgroup reductions.
+// Device-side helpers of the operators that make log-likelihoods: element types,
+// loads and stores of the alignment of one element.
 #pragma once
 
 #include "wd_block.h"
