@@ -905,7 +905,7 @@ def loglikes(logits, *, normalize: bool = True, scale: float = 1.0, log_prior=No
     types = _types(torch)
     dev = logits.device
     _matrix(logits, types, dev, "logits")
-    _no_gradient(torch, "loglikes", logits, log_prior, repetition, presence, frequency, out)
+    _no_gradient(torch, "loglikes", logits, log_prior, out)
     N, V = logits.shape
     p_prior = _vector(log_prior, f32, dev, V, "log_prior")
     p_request, p_mask_of = _vector(request, i32, dev, N, "request"), _vector(mask_of, i32, dev, N, "mask_of")
@@ -914,6 +914,7 @@ def loglikes(logits, *, normalize: bool = True, scale: float = 1.0, log_prior=No
     p_hoff = p_hist = p_rep = p_pres = p_freq = p_boff = p_bid = p_bval = None
     if history is not None:
         off, ids = history
+        _no_gradient(torch, "loglikes", repetition, presence, frequency)
         Q, n_hist = off.numel() - 1, ids.numel()
         p_hoff, p_hist = _vector(off, i64, dev, Q + 1, "history's offsets"), _vector(ids, i32, dev, n_hist, "history's labels")
         p_rep, p_pres = _vector(repetition, f32, dev, Q, "repetition"), _vector(presence, f32, dev, Q, "presence")
