@@ -444,6 +444,100 @@ wd_status wd_loglikes(const wd_loglikes_args* a, void* ws, size_t ws_bytes, void
 wd_status wd_label_masks(const wd_graph* g, int64_t N, const int64_t* off, const int32_t* states, int64_t n_states,
                          uint32_t* mask, int64_t mask_ld, void* stream);
 
+/* ---- fitting the output layer, and holding it in four bits ------------- */
+
+/* What a program needs to fit the output layer W x + b to labels (the first pass's
+ * alignments, words) and to hold it in a quarter of the memory.  The conventions of the
+ * section above hold. */
+
+/* Cross entropy of N rows against their labels, z = W x[n] + b:
+ *   loss[n] = log(sum over p of exp z_p) - z_t, t = target[n]
+ * and for the gradient g[n] of each loss
+ *   dz = g[n] (softmax z - 1 at t), dx[n] = dz W, dweight = sum_n dz x[n], dbias = sum_n dz.
+ * A row whose target is outside 0..P-1 has loss 0 and no part in any gradient, nor has a
+ * row with g[n] = 0 or without a logit above -inf (its loss is +inf): whatever such a
+ * row holds, its dx is 0.  NaNs and +inf among a row's logits make its loss NaN.
+ * Products are exact and sums are kept in 32 bits; for the gradients of x and W, dz is
+ * rounded once to `type` (half precision: times a power of two common to the call, so
+ * that values down to 2^-29 of the largest |g| keep their bits), and each gradient
+ * once to its own. */
+typedef struct {
+  int64_t N;
+  int32_t D, P;            /* 1 <= D < 2^22, 1 <= P < 2^24 */
+  int32_t type;            /* wd_dtype of x, weight, dx and dweight: WD_F16 or WD_BF16 */
+  const void* x;           /* [N][x_ld], x_ld >= D */
+  int64_t x_ld;
+  const void* weight;      /* [P][weight_ld], weight_ld >= D */
+  int64_t weight_ld;
+  const float* bias;       /* [P]; NULL: 0 */
+  const int32_t* target;   /* [N] */
+  float* loss;             /* wd_cross_entropy writes [N]; NULL: not wanted */
+  float* stats;            /* [N][2], 8-byte aligned: a row's largest logit, and the sum of exp(z - largest).
+                              wd_cross_entropy writes them (NULL: not wanted), wd_cross_entropy_grads reads them */
+  const float* grad;       /* g [N]; NULL: 1 */
+  void* dx;                /* [N][dx_ld], dx_ld >= D; NULL: not wanted */
+  int64_t dx_ld;
+  void* dweight;           /* [P][dweight_ld], dweight_ld >= D; NULL: not wanted */
+  int64_t dweight_ld;
+  float* dbias;            /* [P]; NULL: not wanted */
+} wd_loss_args;
+/* wd_cross_entropy_grads: after wd_cross_entropy of the same x, weight, bias and target;
+ * at least one gradient is wanted, and they overlap nothing else.  N = 0: dweight and
+ * dbias are zeros.  At most 2^19 rows or labels (one of the two may be more).
+ * ws as for wd_project (the sizes depend on which gradients are wanted). */
+wd_status wd_cross_entropy_workspace_bytes(const wd_loss_args* a, size_t* bytes);
+wd_status wd_cross_entropy(const wd_loss_args* a, void* ws, size_t ws_bytes, void* stream);
+wd_status wd_cross_entropy_grads_workspace_bytes(const wd_loss_args* a, size_t* bytes);
+wd_status wd_cross_entropy_grads(const wd_loss_args* a, void* ws, size_t ws_bytes, void* stream);
+
+/* The norm over n_tensors gradients, sqrt of the sum of every value's square (formed in
+ * 64 bits, written in 32), and the gradients times min(1, max_norm / norm): in place, or
+ * into tensors of another type.  A norm that is not above max_norm leaves gradients in
+ * place as they are (outputs apart are copies), and so does one that is not finite:
+ * `norm` says so.  max_norm >= 0; infinity: the norm alone.
+ * g: host memory, not needed after the call.  Tensors are contiguous; nothing that is
+ * written overlaps another tensor (one that stands twice in the list does).
+ * ws as for wd_project. */
+typedef struct {
+  void* data;              /* [n] */
+  int64_t n;               /* 0: left out */
+  void* out;               /* [n]; NULL: in place */
+  int32_t type, out_type;  /* wd_dtype */
+} wd_gradient;
+wd_status wd_clip_workspace_bytes(int64_t n_tensors, size_t* bytes);
+wd_status wd_clip_gradients(const wd_gradient* g, int64_t n_tensors, double max_norm, float* norm, void* ws, size_t ws_bytes,
+                            void* stream);
+
+/* A matrix in microscaled 4-bit floating point.  A row's values stand in blocks of 32
+ * that share a power of two 2^(s - 127), s = floor(log2 of the largest magnitude) + 125
+ * (at least 0); each is 0, 0.5, 1, 1.5, 2, 3, 4 or 6 times it, with a sign: the nearest,
+ * ties to the even code, magnitudes above 6 to 6.  A block with an infinity or NaN is
+ * NaN as a whole (s = 255).
+ * codes: [rows][ceil(D/32)][16] bytes, two values a byte, the first in the lower bits;
+ * columns past D are zeros.  scales: [rows][16 ceil(D/512)] bytes; of each 512 columns,
+ * the s of block 4h + q (h, q = 0..3) is byte 4q + h; past the last block 0.
+ * Device memory, 16-byte aligned, of wd_micro_bytes. */
+typedef struct {
+  int64_t rows;
+  int32_t D;               /* 1 <= D < 2^22 */
+  void* codes;
+  void* scales;
+} wd_micro;
+wd_status wd_micro_bytes(int64_t rows, int32_t D, size_t* codes, size_t* scales);
+/* out's rows from x: out->rows rows of type (any wd_dtype), x_ld >= D. */
+wd_status wd_micro_quantize(const void* x, int32_t type, int64_t x_ld, const wd_micro* out, void* stream);
+/* The values that m stands for, exact in WD_F32 and WD_BF16: out_ld >= D. */
+wd_status wd_micro_values(const wd_micro* m, void* out, int32_t type, int64_t out_ld, void* stream);
+/* out[n] = W q(x[n]) + bias: w holds the weights (P = w->rows outputs, 1 <= P < 2^24), q
+ * is wd_micro_quantize of the row.  x: N rows of type, x_ld >= D.  bias [P] or NULL.
+ * out: N rows of out_type (any wd_dtype), out_ld >= P, no overlap with the inputs.
+ * Products are exact, sums are kept in 32 bits; one rounding to out_type.  A row with a
+ * block that is not a number is NaN throughout, so is the output of such a weight row.
+ * ws as for wd_project. */
+wd_status wd_micro_project_workspace_bytes(const wd_micro* w, int64_t N, size_t* bytes);
+wd_status wd_micro_project(const wd_micro* w, const float* bias, const void* x, int32_t type, int64_t x_ld, int64_t N, void* out,
+                           int32_t out_type, int64_t out_ld, void* ws, size_t ws_bytes, void* stream);
+
 /* ---- lattice determinisation (host) ----------------------------------- */
 
 /* The compact "exact lattice" (Sec. 3.4, after Povey et al. 2012) of a pruned

@@ -5,4 +5,5 @@ include/wfstdec.h); `wfstdec` is its ctypes binding.  Importing the package
 does not load the library; the first call does, and raises if it is missing.
 """
 from . import wfstdec  # noqa: F401
-from .wfstdec import Graph, Head, WdError, decode, decode_batch, loglikes  # noqa: F401
+from .wfstdec import (Graph, Head, Micro, MicroHead, WdError, clip_gradients, cross_entropy,  # noqa: F401
+                      cross_entropy_grads, decode, decode_batch, loglikes, micro)

@@ -1,0 +1,236 @@
+// The norm over many tensors' gradients, and the gradients times
+// min(1, max_norm / norm).
+//
+// Two passes, since the factor needs every value: sums of squares, a workgroup each a
+// number of chunks, in 64 bits (squares of 32-bit values neither overflow nor vanish, and
+// 64-bit multiply-adds are faster than memory brings values); then every workgroup
+// scales its chunks.  Bound by memory: all values are read twice and written once.
+// The tensors' addresses come as kernel arguments, kTensors at a launch, so that a call
+// copies nothing and can be captured.
+#include <algorithm>
+
+#include "wd_host.h"
+#include "wd_num.h"
+
+namespace wd {
+
+constexpr int kTensors = 64;       // of a launch
+constexpr int kChunk = 16384;      // values
+constexpr int kClipGroups = 2048;  // workgroups of a launch at most
+constexpr int kClipThreads = 256;
+
+struct ClipArgs {
+  const void* data[kTensors];
+  void* out[kTensors];
+  int64_t n[kTensors];
+  uint32_t first[kTensors + 1];  // chunk of the launch that a tensor begins with
+  uint8_t type[kTensors], out_type[kTensors];
+  int32_t tensors;
+};
+
+// The tensor of chunk c.
+__device__ __forceinline__ int tensor_of(const ClipArgs& a, uint32_t c) {
+  int lo = 0, hi = a.tensors - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (a.first[mid] <= c)
+      lo = mid;
+    else
+      hi = mid - 1;
+  }
+  return lo;
+}
+
+__device__ __forceinline__ double wave_sum(double v) {
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+  return v;
+}
+// In every thread; the same bits every time.
+__device__ __forceinline__ double block_sum(double v, double* lds) {
+  v = wave_sum(v);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = lds[0];
+#pragma unroll
+  for (int k = 1; k < kClipThreads / 64; ++k) v += lds[k];
+  return v;
+}
+
+template <class T>
+__device__ __forceinline__ double chunk_squares(const T* p, int n) {
+  constexpr int kEach = 16 / sizeof(T);
+  double s = 0.0;
+  int i = threadIdx.x * kEach;
+#pragma unroll 4
+  for (; i + kEach <= n; i += kClipThreads * kEach) {
+    const Few<T, kEach> v = *(const Few<T, kEach>*)(p + i);
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) s = __builtin_fma((double)v.v[e].f(), (double)v.v[e].f(), s);
+  }
+  for (; i < n; ++i) s = __builtin_fma((double)p[i].f(), (double)p[i].f(), s);
+  return s;
+}
+
+__global__ void __launch_bounds__(kClipThreads) k_clip_squares(ClipArgs a, double* part) {
+  __shared__ double lds[kClipThreads / 64];
+  double s = 0.0;
+  for (uint32_t c = blockIdx.x; c < a.first[a.tensors]; c += gridDim.x) {
+    const int t = tensor_of(a, c);
+    const int64_t at = (int64_t)(c - a.first[t]) * kChunk;
+    const int n = (int)min<int64_t>(kChunk, a.n[t] - at);
+    if (a.type[t] == WD_F32)
+      s += chunk_squares((const F32*)a.data[t] + at, n);
+    else if (a.type[t] == WD_F16)
+      s += chunk_squares((const Half*)a.data[t] + at, n);
+    else
+      s += chunk_squares((const Bf16*)a.data[t] + at, n);
+  }
+  s = block_sum(s, lds);
+  if (threadIdx.x == 0) part[blockIdx.x] = s;
+}
+
+// The norm from the launches' sums, and the factor: 1 where the norm is not above
+// max_norm, and where it is not finite (nothing is scaled then).
+__global__ void __launch_bounds__(kClipThreads) k_clip_norm(const double* part, int64_t parts, double max_norm, float* norm, float* factor) {
+  __shared__ double lds[kClipThreads / 64];
+  double s = 0.0;
+  for (int64_t i = threadIdx.x; i < parts; i += kClipThreads) s += part[i];
+  s = sqrt(block_sum(s, lds));
+  if (threadIdx.x != 0) return;
+  *norm = (float)s;
+  *factor = s > max_norm && s < INFINITY ? (float)(max_norm / s) : 1.0f;
+}
+
+template <class T, class O>
+__device__ __forceinline__ void chunk_scaled(const T* p, O* o, int n, float by) {
+  constexpr int kEach = 16 / (sizeof(T) > sizeof(O) ? sizeof(T) : sizeof(O));
+  int i = threadIdx.x * kEach;
+#pragma unroll 4
+  for (; i + kEach <= n; i += kClipThreads * kEach) {
+    const Few<T, kEach> v = *(const Few<T, kEach>*)(p + i);
+    Few<O, kEach> w;
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) w.v[e] = O::of(v.v[e].f() * by);
+    *(Few<O, kEach>*)(o + i) = w;
+  }
+  for (; i < n; ++i) o[i] = O::of(p[i].f() * by);
+}
+
+template <class T>
+__device__ __forceinline__ void chunk_to(const T* p, void* out, int out_type, int64_t at, int n, float by) {
+  if (out_type == WD_F32)
+    chunk_scaled(p + at, (F32*)out + at, n, by);
+  else if (out_type == WD_F16)
+    chunk_scaled(p + at, (Half*)out + at, n, by);
+  else
+    chunk_scaled(p + at, (Bf16*)out + at, n, by);
+}
+
+__global__ void __launch_bounds__(kClipThreads) k_clip_scale(ClipArgs a, const float* factor) {
+  const float by = *factor;
+  // the chunks that were read last first: they may still be in the caches
+  const uint32_t chunks = a.first[a.tensors];
+  for (uint32_t i = blockIdx.x; i < chunks; i += gridDim.x) {
+    const uint32_t c = chunks - 1 - i;
+    const int t = tensor_of(a, c);
+    if (by == 1.0f && a.out[t] == a.data[t]) continue;
+    const int64_t at = (int64_t)(c - a.first[t]) * kChunk;
+    const int n = (int)min<int64_t>(kChunk, a.n[t] - at);
+    if (a.type[t] == WD_F32)
+      chunk_to((const F32*)a.data[t], a.out[t], a.out_type[t], at, n, by);
+    else if (a.type[t] == WD_F16)
+      chunk_to((const Half*)a.data[t], a.out[t], a.out_type[t], at, n, by);
+    else
+      chunk_to((const Bf16*)a.data[t], a.out[t], a.out_type[t], at, n, by);
+  }
+}
+
+}  // namespace wd
+
+using namespace wd;
+
+static size_t type_bytes(int32_t type) { return type == WD_F32 ? 4 : 2; }
+// A launch more may begin in the middle of a long list, where its tensors have too many chunks together.
+static int64_t clip_launches(int64_t tensors) { return (tensors + kTensors - 1) / kTensors; }
+
+extern "C" wd_status wd_clip_workspace_bytes(int64_t n_tensors, size_t* bytes) {
+  if (!bytes) return fail(WD_EINVAL, "clip_workspace_bytes: null output");
+  if (n_tensors < 0 || n_tensors > (1 << 24)) return fail(WD_EINVAL, "clip: n_tensors out of range");
+  *bytes = 256 + (size_t)clip_launches(n_tensors) * kClipGroups * sizeof(double);
+  return WD_OK;
+}
+
+extern "C" wd_status wd_clip_gradients(const wd_gradient* g, int64_t n_tensors, double max_norm, float* norm, void* ws, size_t ws_bytes, void* stream) try {
+  if (n_tensors < 0 || n_tensors > (1 << 24)) return fail(WD_EINVAL, "clip: n_tensors out of range");
+  if (!g && n_tensors > 0) return fail(WD_EINVAL, "clip: null gradients");
+  if (!(max_norm >= 0.0)) return fail(WD_EINVAL, "clip: max_norm must be >= 0");
+  if (!norm || (uintptr_t)norm & 3) return fail(WD_EINVAL, "clip: null or misaligned norm");
+  struct Range {
+    uintptr_t from, to;
+    int64_t i;  // of a tensor that is written there, else -1 - tensor
+  };
+  std::vector<Range> ranges;
+  ranges.reserve((size_t)n_tensors * 2 + 1);
+  ranges.push_back({(uintptr_t)norm, (uintptr_t)norm + 4, n_tensors});
+  bool apart = false;  // tensors with an output of their own
+  for (int64_t i = 0; i < n_tensors; ++i) {
+    const wd_gradient& t = g[i];
+    if (t.n < 0 || t.n > (1ll << 40)) return fail(WD_EINVAL, "clip: size of a tensor out of range");
+    if (t.type < WD_F32 || t.type > WD_BF16 || (t.out && (t.out_type < WD_F32 || t.out_type > WD_BF16))) return fail(WD_EINVAL, "clip: unknown type");
+    if (t.n == 0) continue;
+    if (!t.data) return fail(WD_EINVAL, "clip: null tensor");
+    if ((uintptr_t)t.data % type_bytes(t.type) || (t.out && (uintptr_t)t.out % type_bytes(t.out_type))) return fail(WD_EINVAL, "clip: misaligned tensor");
+    const uintptr_t p = (uintptr_t)t.data;
+    const bool in_place = !t.out || (t.out == t.data && t.out_type == t.type);
+    ranges.push_back({p, p + (uint64_t)t.n * type_bytes(t.type), in_place ? i : -1 - i});
+    if (!in_place) ranges.push_back({(uintptr_t)t.out, (uintptr_t)t.out + (uint64_t)t.n * type_bytes(t.out_type), i}), apart = true;
+  }
+  // A value that is written is nobody else's (a tensor that stands twice would be scaled twice).
+  std::sort(ranges.begin(), ranges.end(), [](const Range& a, const Range& b) { return a.from < b.from; });
+  uintptr_t any = 0, written = 0;  // where the ranges so far end
+  for (const Range& r : ranges) {
+    if (r.from < written || (r.i >= 0 && r.from < any)) return fail(WD_EINVAL, "clip: tensors overlap");
+    any = std::max(any, r.to);
+    if (r.i >= 0) written = std::max(written, r.to);
+  }
+  size_t need = 0;
+  wd_clip_workspace_bytes(n_tensors, &need);
+  if (!ws || ws_bytes < need || (uintptr_t)ws & 255) return fail(WD_EINVAL, "clip: workspace missing, too small or not 256-byte aligned");
+  hipStream_t s = (hipStream_t)stream;
+  float* factor = (float*)ws;
+  double* part = (double*)((char*)ws + 256);
+  int64_t parts = 0;
+  const auto each = [&](auto&& launch) -> wd_status {
+    for (int64_t i0 = 0; i0 < n_tensors; i0 += kTensors) {
+      ClipArgs a;
+      a.tensors = 0;
+      uint64_t chunks = 0;
+      for (int64_t i = i0; i < std::min(i0 + kTensors, n_tensors); ++i) {
+        const wd_gradient& t = g[i];
+        if (t.n == 0) continue;
+        const int k = a.tensors++;
+        a.data[k] = t.data, a.out[k] = t.out ? t.out : (void*)t.data, a.n[k] = t.n;
+        a.type[k] = (uint8_t)t.type, a.out_type[k] = (uint8_t)(t.out ? t.out_type : t.type);
+        a.first[k] = (uint32_t)chunks;
+        chunks += (uint64_t)(t.n + kChunk - 1) / kChunk;
+        if (chunks > UINT32_MAX - kClipGroups) return fail(WD_EINVAL, "clip: too many values for one call");
+      }
+      if (a.tensors == 0) continue;
+      a.first[a.tensors] = (uint32_t)chunks;
+      launch(a, (uint32_t)std::min<uint64_t>(chunks, kClipGroups));
+    }
+    return WD_OK;
+  };
+  wd_status st = each([&](const ClipArgs& a, uint32_t groups) {
+    hipLaunchKernelGGL(k_clip_squares, dim3(groups), dim3(kClipThreads), 0, s, a, part + parts);
+    parts += groups;
+  });
+  if (st != WD_OK) return st;
+  hipLaunchKernelGGL(k_clip_norm, dim3(1), dim3(kClipThreads), 0, s, part, parts, max_norm, norm, factor);
+  if (max_norm < INFINITY || apart)
+    st = each([&](const ClipArgs& a, uint32_t groups) { hipLaunchKernelGGL(k_clip_scale, dim3(groups), dim3(kClipThreads), 0, s, a, factor); });
+  return st != WD_OK ? st : hip_check(hipGetLastError(), "clip");
+} catch (const std::bad_alloc&) {
+  return fail(WD_EINVAL, "clip: out of host memory");
+}

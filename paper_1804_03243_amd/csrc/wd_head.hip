@@ -17,20 +17,9 @@
 #include "wd_host.h"
 #include "wd_num.h"
 #include "wd_rows.h"
+#include "wd_tile.h"
 
 namespace wd {
-
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
-typedef __attribute__((ext_vector_type(4))) float f32x4;
-typedef f32x4 __attribute__((aligned(2))) f32x4_any;
-
-__device__ __forceinline__ f32x4 mfma16(uint4 a, uint4 b, f32x4 c, Bf16) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
-}
-__device__ __forceinline__ f32x4 mfma16(uint4 a, uint4 b, f32x4 c, Half) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-}
 
 struct HeadArgs {
   wd_head h;
@@ -592,18 +581,6 @@ __device__ __forceinline__ void add_low(const HeadArgs& a, int64_t n0, const int
   }
 }
 
-// N consecutive outputs of a row, those from n on left out.
-template <class O, int N>
-__device__ __forceinline__ void store_out(O* out, const Few<O, N>& v, int n) {
-  if (n >= N) {
-    *(Few<O, N>*)out = v;
-  } else {
-#pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (i < n) out[i] = v.v[i];
-  }
-}
-
 // The adapters' part and the bias, the rounding, and the store: a block of 16
 // rows at a time through LDS (`mine`, the wavefront's own), so that a store
 // instruction writes whole lines of a row.  In the accumulators' layout it writes
@@ -649,28 +626,6 @@ __device__ __forceinline__ void finish_tile(const HeadArgs& a, int64_t n0, int p
       }
     }
   }
-}
-
-// 16 bytes per lane from `base` (the same in every lane) + the lane's offset
-// straight to LDS at `to` + 16 * lane (the same `to` in every lane).  The compiler
-// does not see this load (its builtin makes every LDS read wait for all of them):
-// the data is there after loads_left() and a barrier.
-__device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t to) {
-  const uint64_t p = (uint64_t)base;  // (into scalar registers, where the compiler would not hold it there)
-  base = (const void*)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(p >> 32)) << 32 |
-                       (uint32_t)__builtin_amdgcn_readfirstlane((int)p));
-  // (m0 is a register that the compiler keeps to itself, and warns of here; it holds no
-  // value there across other code, and is named so that none of its uses is put around this)
-#pragma clang diagnostic push
-#pragma clang diagnostic ignored "-Winline-asm"
-  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(to)
-               : "memory", "m0");
-#pragma clang diagnostic pop
-}
-// Waits until at most N of this wavefront's loads are on their way (they arrive in order).
-template <int N>
-__device__ __forceinline__ void loads_left() {
-  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
 }
 
 // Few rows (16 * NB to a workgroup): what counts is that W streams through the chip once.
@@ -798,33 +753,11 @@ __global__ void __launch_bounds__(512) k_rows(HeadArgs a) {
   store_out((O*)a.out + fi * a.out_ld + fp, out, P - fp);
 }
 
-constexpr int kStepK = 64;  // columns of a step: 128 bytes of a row
-
-// Where chunk c (16 bytes) of tile row r lies in LDS: at c ^ swizzle, so that the
-// 16 rows of an operand read fall on different banks.
-__device__ __forceinline__ int swizzle(int row) { return (row >> 1) & 7; }
-
-// The tile of this workgroup.  Workgroups go round the eight XCDs, each with an
-// L2 of its own: an XCD takes a run of tiles, in groups of kGroup rows of tiles
-// column by column, so that its workgroups share rows of x and of W.
-constexpr uint32_t kGroup = 8;
-__device__ __forceinline__ void my_tile(uint32_t rows, uint32_t cols, uint32_t& row, uint32_t& col) {
-  const uint32_t all = rows * cols, xcd = blockIdx.x % 8, q = all / 8, r = all % 8;
-  const uint32_t at = xcd * q + min(xcd, r) + blockIdx.x / 8;
-  const uint32_t group = at / (kGroup * cols), first = group * kGroup, height = min(kGroup, rows - first);
-  const uint32_t in = at - first * cols;
-  col = in / height;
-  row = first + in % height;
-}
-
 // Adapters of a tile that are steps of its product.  A step more costs a tile of 256
 // rows 1.5 us, add_low about 2 per adapter with the first wait: 64 utterances of 1000 rows
 // 938 us with one adapter in the steps, 906 with two; rows in runs of 32 lose with
 // more (64000 rows: 1218 us by add_low, 1367 in up to eight steps).
 constexpr int kKinds = 2;
-
-// What a lane loads for the terms of another adapter's row.
-__device__ const uint4 k_zeros[kStepK / 8] = {};
 
 // BM rows and BN outputs per workgroup of WM x WN wavefronts.  Two steps of kStepK
 // columns are in LDS.  A step is two halves: while one is multiplied, the next

@@ -1,0 +1,693 @@
+// Cross entropy of hidden rows against their labels, straight from the rows and the
+// output layer's weights, and its gradients; the logits are never in memory.
+//
+//   z = W x[n] + b      loss[n] = log sum_p exp z_p - z_t, t = target[n]
+//   dz = g[n] (softmax z - 1 at t)      dx[n] = dz W      dW = sum_n dz x[n]      db = sum_n dz
+//
+// Loss: the product W x in tiles of matrix instructions; a tile leaves its largest
+// logit and its sum of exponentials for each of its rows (8 bytes per 256 logits), and
+// the logit of the row's label.  A second kernel joins the row's tiles.
+//
+// Gradients: the same tiles are formed again and turned into dz, rounded to the
+// inputs' 16-bit type (below) in a workspace that holds a piece of the rows or of the
+// labels; two more products, dz W and dz^T x, read it from there.  Forming the logits
+// twice costs 2 N D P operations of 8, keeping them would cost N P values of memory.
+//
+// What is rounded: dz to 16 bits, as matrix instructions take it; half a step of the
+// type, relative to each value, as large as the rounding of the gradients themselves,
+// whose sums run in 32 bits.  Half precision has dz times a power of two that takes the
+// largest |g| to [2^14, 2^15), so that what is 2^29 times smaller than the largest
+// keeps its bits.  db sums the 32-bit values.
+#include <algorithm>
+
+#include "wd_host.h"
+#include "wd_tile.h"
+
+namespace wd {
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
+// What the gradients need of a row: its largest logit, g / sum, g (both times the power
+// of two), its label (-1: the row has no part in the gradients).
+struct RowInfo {
+  float top, gs, g;
+  int32_t label;
+};
+
+struct LossArgs {
+  const void* x;      // rows of the launch, x_ld bytes apart
+  const void* w;      // outputs of the launch
+  int64_t x_ld, w_ld;
+  int64_t N;
+  int32_t P, K;       // outputs; shared columns, a multiple of eight
+  const float* bias;  // of the launch's outputs; NULL: 0
+  const int32_t* target;  // of the launch's rows
+  float2* part;       // loss: [column tile][N] largest logit, sum of exponentials
+  float* label_z;     // loss: [N] logit of the row's label
+  const RowInfo* info;    // gradients: of the launch's rows
+  int32_t p_first;    // gradients: the first output's label
+  void* dz;           // gradients: [N][dz_ld], zeros from P on
+  int64_t dz_ld;      // in elements, a multiple of 64
+  float* db_part;     // gradients: [row tile][P]; NULL: not wanted
+};
+
+// The sum of exponentials of two parts, for the larger of their largest logits.
+__device__ __forceinline__ float2 join(float2 a, float2 b) {
+  const float top = fmaxf(a.x, b.x), at = top > -INFINITY ? top : 0.0f;
+  return make_float2(top, a.y * __builtin_amdgcn_exp2f((a.x - at) * kLog2e) + b.y * __builtin_amdgcn_exp2f((b.x - at) * kLog2e));
+}
+
+// Rows and outputs of a tile; the logits of its rows are acc + bias, -inf past the last output.
+template <int TN>
+__device__ __forceinline__ void load_bias(const LossArgs& a, int p, float (&bias)[TN][4]) {
+  const int quad = (threadIdx.x & 63) >> 4;
+#pragma unroll
+  for (int j = 0; j < TN; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int at = p + j * 16 + quad * 4 + e;
+      bias[j][e] = at >= a.P ? -INFINITY : a.bias ? a.bias[at] : 0.0f;
+    }
+}
+
+template <class T, int BM, int BN, int WM, int WN>
+__global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2) k_loss(LossArgs a, uint32_t row_tiles, uint32_t col_tiles) {
+  using Tl = Tile<T, BM, BN, WM, WN, false, false>;
+  constexpr int TM = Tl::TM, TN = Tl::TN;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  uint32_t row_tile, col_tile;
+  my_tile(row_tiles, col_tiles, row_tile, col_tile);
+  const int64_t n0 = (int64_t)row_tile * BM;
+  const int p0 = (int)col_tile * BN;
+  f32x4 acc[TM][TN] = {};
+  Tl::multiply({(const char*)a.x + n0 * a.x_ld, a.x_ld, (int)min<int64_t>(BM, a.N - n0)},
+               {(const char*)a.w + (int64_t)p0 * a.w_ld, a.w_ld, min(BN, a.P - p0)}, a.K, lds, acc);
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
+  const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
+  float bias[TN][4];
+  load_bias<TN>(a, p0 + wn, bias);
+  __syncthreads();  // (every wavefront has read its last operands)
+  float2* sums = (float2*)lds;  // [WN][BM]
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int64_t n = n0 + wm + i * 16 + col;
+    const int t = n < a.N ? a.target[n] - p0 - wn : -1;
+    float top = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        acc[i][j][e] += bias[j][e];
+        top = fmaxf(top, acc[i][j][e]);
+      }
+    top = fmaxf(top, __shfl_xor(top, 16));
+    top = fmaxf(top, __shfl_xor(top, 32));
+    const float at = top > -INFINITY ? top : 0.0f;
+    float sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f((acc[i][j][e] - at) * kLog2e);
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if (quad == 0) sums[(wave % WN) * BM + wm + i * 16 + col] = make_float2(top, sum);
+    if (__any(t >= 0 && t < TN * 16)) {  // (few blocks hold a label)
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (t == j * 16 + quad * 4 + e && t + p0 + wn < a.P) a.label_z[n] = acc[i][j][e];
+    }
+  }
+  __syncthreads();
+  for (int r = threadIdx.x; r < BM; r += 64 * WM * WN) {
+    float2 v = sums[r];
+#pragma unroll
+    for (int k = 1; k < WN; ++k) v = join(v, sums[k * BM + r]);
+    if (n0 + r < a.N) a.part[(int64_t)col_tile * a.N + n0 + r] = v;
+  }
+}
+
+// A row's tiles: LANES lanes each take every LANES-th, then join theirs.
+template <int LANES>
+__global__ void __launch_bounds__(256) k_loss_join(const float2* part, int tiles, const float* label_z, const int32_t* target, int32_t P,
+                                                   int64_t N, float* loss, float2* stats) {
+  constexpr int kRows = 256 / LANES;
+  __shared__ float2 sums[LANES][kRows];
+  const int r = threadIdx.x % kRows, l = threadIdx.x / kRows;
+  const int64_t n = (int64_t)blockIdx.x * kRows + r;
+  float2 v = make_float2(-INFINITY, 0.0f);
+  if (n < N)
+    for (int t = l; t < tiles; t += LANES) v = join(v, part[(int64_t)t * N + n]);
+  sums[l][r] = v;
+  __syncthreads();
+  if (l != 0 || n >= N) return;
+#pragma unroll
+  for (int k = 1; k < LANES; ++k) v = join(v, sums[k][r]);
+  const int t = target[n];
+  if (stats) stats[n] = v;
+  if (loss) loss[n] = t < 0 || t >= P ? 0.0f : v.y == 0.0f ? INFINITY : (v.x - label_z[n]) + logf(v.y);
+}
+
+// The power of two of the gradients (half precision), and its reciprocal.
+__global__ void __launch_bounds__(1024) k_power(const float* g, int64_t N, float* power) {
+  __shared__ float tops[16];
+  float top = g ? 0.0f : 1.0f;
+  for (int64_t n = threadIdx.x; g && n < N; n += 1024) top = fmaxf(top, fabsf(g[n]) < INFINITY ? fabsf(g[n]) : 0.0f);
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
+  if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  for (int k = 1; k < 16; ++k) top = fmaxf(top, tops[k]);
+  const int e = max(-100, min(100, 14 - ((int)(__float_as_uint(top) >> 23) - 127)));
+  power[0] = __uint_as_float((uint32_t)(127 + (top > 0.0f ? e : 0)) << 23);
+  power[1] = 1.0f / power[0];
+}
+
+__global__ void __launch_bounds__(256) k_row_info(const float2* stats, const float* g, const int32_t* target, int32_t P, int64_t N,
+                                                  const float* power, RowInfo* info) {
+  const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (n >= N) return;
+  const float2 s = stats[n];
+  const int t = target[n];
+  const float gn = (g ? g[n] : 1.0f) * (power ? power[0] : 1.0f);
+  // (a row without a finite logit has no softmax)
+  const bool in = t >= 0 && t < P && gn != 0.0f && !(s.x == -INFINITY && s.y == 0.0f);
+  info[n] = in ? RowInfo{s.x, gn / s.y, gn, t} : RowInfo{0.0f, 0.0f, 0.0f, -1};
+}
+
+// Rows of D elements to rows of `to_ld` >= D with zeros behind them; rows without a part
+// in the gradients (info) are zeros, so that nothing of theirs reaches a sum.
+template <class T>
+__global__ void __launch_bounds__(256) k_lay(const T* from, int64_t ld, int64_t N, int D, const RowInfo* info, T* to, int64_t to_ld) {
+  const int64_t per = to_ld / 8;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < N * per; i += (int64_t)gridDim.x * 256) {
+    const int64_t n = i / per;
+    const int k = (int)(i % per) * 8;
+    Few<T, 8> v{};
+    if (!info || info[n].label >= 0) {
+      if (k + 8 <= D) {
+        v = *(const Few<T, 8>*)(from + n * ld + k);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (k + e < D) v.v[e] = from[n * ld + k + e];
+      }
+    }
+    *(uint4*)(to + n * to_ld + k) = __builtin_bit_cast(uint4, v);
+  }
+}
+
+// A tile's values to memory, a block of 16 rows at a time through LDS (`mine`, the
+// wavefront's own), so that a store instruction writes whole lines of a row.  value(i, j, e)
+// is the lane's value of row i * 16 + lane % 16, column j * 16 + lane / 16 * 4 + e.
+template <class O, int TM, int TN, class Value>
+__device__ __forceinline__ void store_tile(O* out, int64_t ld, int64_t rows, int64_t cols, char* mine, Value value) {
+  constexpr int kCols = TN * 16, kEach = 16 / sizeof(O);
+  constexpr int kLine = kCols + kEach;  // a row in LDS, padded against bank conflicts
+  constexpr int kLanes = kCols / kEach, kRows = 64 / kLanes;
+  const int lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
+  O* lines = (O*)mine;
+  const int c = (lane % kLanes) * kEach, r0 = lane / kLanes, left = (int)min<int64_t>(cols - c, kEach);
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      struct alignas(4 * sizeof(O)) Four {
+        O v[4];
+      } v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v.v[e] = O::of(value(i, j, e));
+      *(Four*)(lines + col * kLine + j * 16 + quad * 4) = v;
+    }
+#pragma unroll
+    for (int q = 0; q < 16; q += kRows) {
+      const uint4 v = *(const uint4*)(lines + (q + r0) * kLine + c);
+      const int64_t n = i * 16 + q + r0;
+      if (n < rows) store_out(out + n * ld + c, __builtin_bit_cast(Few<O, kEach>, v), left);
+    }
+  }
+}
+// Bytes of store_tile's LDS for each wavefront.
+template <class O, int TN>
+constexpr int kStoreBytes = 16 * (TN * 16 + 16 / (int)sizeof(O)) * (int)sizeof(O);
+
+template <class T, int BM, int BN, int WM, int WN>
+__global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2) k_loss_dz(LossArgs a, uint32_t row_tiles, uint32_t col_tiles) {
+  using Tl = Tile<T, BM, BN, WM, WN, false, false>;
+  constexpr int TM = Tl::TM, TN = Tl::TN;
+  static_assert(kStoreBytes<T, TN> * WM * WN + WM * BN * 4 <= Tl::kBytes, "");
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  uint32_t row_tile, col_tile;
+  my_tile(row_tiles, col_tiles, row_tile, col_tile);
+  const int64_t n0 = (int64_t)row_tile * BM;
+  const int p0 = (int)col_tile * BN;
+  f32x4 acc[TM][TN] = {};
+  Tl::multiply({(const char*)a.x + n0 * a.x_ld, a.x_ld, (int)min<int64_t>(BM, a.N - n0)},
+               {(const char*)a.w + (int64_t)p0 * a.w_ld, a.w_ld, min(BN, a.P - p0)}, a.K, lds, acc);
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
+  const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
+  float bias[TN][4], db[TN][4] = {};
+  load_bias<TN>(a, p0 + wn, bias);
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int64_t n = n0 + wm + i * 16 + col;
+    const RowInfo r = n < a.N ? a.info[n] : RowInfo{0.0f, 0.0f, 0.0f, -1};
+    const int t = r.label < 0 ? -1 : r.label - a.p_first - p0 - wn;
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float v = r.gs * __builtin_amdgcn_exp2f((acc[i][j][e] + bias[j][e] - r.top) * kLog2e);
+        acc[i][j][e] = r.label >= 0 ? v : 0.0f;  // (a row left out may have infinite logits)
+      }
+    if (__any(t >= 0 && t < TN * 16)) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          if (t == j * 16 + quad * 4 + e) acc[i][j][e] -= r.g;
+    }
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) db[j][e] += acc[i][j][e];
+  }
+  __syncthreads();  // (every wavefront has read its last operands)
+  store_tile<T, TM, TN>((T*)a.dz + (n0 + wm) * a.dz_ld + p0 + wn, a.dz_ld, a.N - n0 - wm, a.dz_ld - p0 - wn, lds + wave * kStoreBytes<T, TN>,
+                        [&](int i, int j, int e) { return acc[i][j][e]; });
+  if (!a.db_part) return;
+  float* sums = (float*)(lds + kStoreBytes<T, TN> * WM * WN);  // [WM][BN]
+#pragma unroll
+  for (int j = 0; j < TN; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      float s = db[j][e];
+      for (int o = 8; o > 0; o >>= 1) s += __shfl_xor(s, o);
+      if (col == 0) sums[(wave / WN) * BN + wn + j * 16 + quad * 4 + e] = s;
+    }
+  __syncthreads();
+  for (int p = threadIdx.x; p < BN; p += 64 * WM * WN) {
+    float s = sums[p];
+#pragma unroll
+    for (int k = 1; k < WM; ++k) s += sums[k * BN + p];
+    if (p0 + p < a.P) a.db_part[(int64_t)row_tile * a.P + p0 + p] = s;
+  }
+}
+
+// db of a piece: the row tiles' sums in their order.
+__global__ void __launch_bounds__(256) k_loss_db(const float* part, int tiles, int P, const float* power, bool add, float* db) {
+  const int p = blockIdx.x * 256 + threadIdx.x;
+  if (p >= P) return;
+  float s = 0.0f;
+#pragma unroll 8
+  for (int t = 0; t < tiles; ++t) s += part[(int64_t)t * P + p];
+  if (power) s *= power[1];
+  db[p] = add ? db[p] + s : s;
+}
+
+// out[m][c] = sum over k of x(m, k) w(c, k): dz W (x by rows, w by shared columns) and
+// dz^T x (both by shared columns).
+struct ProductArgs {
+  const void *x, *w;
+  int64_t x_ld, w_ld;  // bytes
+  int64_t M;           // rows of the output
+  int32_t C;           // its columns
+  int32_t K, k_each;   // shared columns, and those of a split (a multiple of kStepK)
+  void* out;           // in the inputs' type; NULL: into `part`
+  int64_t out_ld;
+  float* part;         // [split][M][part_ld]
+  int64_t part_ld;
+  const float* power;  // NULL: 1
+  const RowInfo* info; // rows without a part in the gradients are zeros; NULL: none
+};
+
+template <class T, int BM, int BN, int WM, int WN, bool XKR>
+__global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2) k_product(ProductArgs a, uint32_t row_tiles, uint32_t col_tiles) {
+  using Tl = Tile<T, BM, BN, WM, WN, XKR, true>;
+  constexpr int TM = Tl::TM, TN = Tl::TN;
+  static_assert(kStoreBytes<F32, TN> * WM * WN <= Tl::kBytes, "");
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  uint32_t row_tile, col_tile;
+  my_tile(row_tiles, col_tiles, row_tile, col_tile);
+  const int64_t m0 = (int64_t)row_tile * BM;
+  const int c0 = (int)col_tile * BN, k0 = (int)blockIdx.y * a.k_each;
+  f32x4 acc[TM][TN] = {};
+  const char* x = (const char*)a.x + (XKR ? m0 * 2 + (int64_t)k0 * a.x_ld : m0 * a.x_ld + (int64_t)k0 * 2);
+  Tl::multiply({x, a.x_ld, (int)min<int64_t>(BM, a.M - m0)}, {(const char*)a.w + (int64_t)k0 * a.w_ld + (int64_t)c0 * 2, a.w_ld, min(BN, a.C - c0)},
+               min(a.k_each, a.K - k0), lds, acc);
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15;
+  const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
+  __syncthreads();  // (every wavefront has read its last operands)
+  if (a.out) {
+    const float by = a.power ? a.power[1] : 1.0f;
+    bool in[TM];
+#pragma unroll
+    for (int i = 0; i < TM; ++i) in[i] = !a.info || a.info[min<int64_t>(m0 + wm + i * 16 + col, a.M - 1)].label >= 0;
+    store_tile<T, TM, TN>((T*)a.out + (m0 + wm) * a.out_ld + c0 + wn, a.out_ld, a.M - m0 - wm, a.C - c0 - wn, lds + wave * kStoreBytes<T, TN>,
+                          [&](int i, int j, int e) { return in[i] ? acc[i][j][e] * by : 0.0f; });
+  } else {
+    store_tile<F32, TM, TN>((F32*)a.part + ((int64_t)blockIdx.y * a.M + m0 + wm) * a.part_ld + c0 + wn, a.part_ld, a.M - m0 - wm, a.C - c0 - wn,
+                            lds + wave * kStoreBytes<F32, TN>, [&](int i, int j, int e) { return acc[i][j][e]; });
+  }
+}
+
+// The splits' sums in their order, behind those of earlier pieces (`sum`, in 32 bits), to
+// `sum`, or at the last piece to the output.  No splits: zeros.
+template <class T>
+__global__ void __launch_bounds__(256) k_product_join(ProductArgs a, int splits, const float* before, float* sum) {
+  const int64_t per = (a.C + 3) / 4;
+  const float by = a.power ? a.power[1] : 1.0f;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < a.M * per; i += (int64_t)gridDim.x * 256) {
+    const int64_t m = i / per;
+    const int c = (int)(i % per) * 4;
+    f32x4 s = {0, 0, 0, 0};
+    if (before) s = *(const f32x4*)(before + m * a.part_ld + c);
+    for (int k = 0; k < splits; ++k) s += *(const f32x4*)(a.part + ((int64_t)k * a.M + m) * a.part_ld + c);
+    if (a.out) {
+      const bool in = !a.info || a.info[m].label >= 0;
+      Few<T, 4> v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v.v[e] = T::of(in ? s[e] * by : 0.0f);
+      store_out((T*)a.out + m * a.out_ld + c, v, min(4, a.C - c));
+    } else {
+      *(f32x4*)(sum + m * a.part_ld + c) = s;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ host
+
+// Tiles: the largest that gives every compute unit one (256, 192 of the middle ones).
+enum TileSize { kSmall = 64, kMiddle = 128, kLarge = 256 };
+static int64_t tiles_of(int64_t M, int64_t C, int size) { return ((M + size - 1) / size) * ((C + size - 1) / size); }
+static TileSize tile_size(int64_t M, int64_t C) {
+  return tiles_of(M, C, 256) >= 256 ? kLarge : tiles_of(M, C, 128) >= 192 ? kMiddle : kSmall;
+}
+
+template <class K, class A>
+static void launch_tile(K* kernel, int bytes, std::atomic<uint64_t>& done, int threads, int size, int64_t M, int64_t C, int splits, hipStream_t s,
+                        const A& args) {
+  allow_lds((const void*)kernel, bytes, done);
+  const uint32_t rows = (uint32_t)((M + size - 1) / size), cols = (uint32_t)((C + size - 1) / size);
+  hipLaunchKernelGGL(kernel, dim3(rows * cols, (uint32_t)splits), dim3(threads), bytes, s, args, rows, cols);
+}
+
+#define WD_TILES(size, CALL) \
+  if ((size) == kLarge) {    \
+    CALL(256, 2, 4);         \
+  } else if ((size) == kMiddle) { \
+    CALL(128, 2, 2);         \
+  } else {                   \
+    CALL(64, 2, 2);          \
+  }
+
+template <class T>
+static void launch_loss(const LossArgs& a, int size, hipStream_t s) {
+#define WD_CALL(B, WM, WN)                                                                                                      \
+  static std::atomic<uint64_t> done{0};                                                                                         \
+  launch_tile(k_loss<T, B, B, WM, WN>, Tile<T, B, B, WM, WN, false, false>::kBytes, done, 64 * WM * WN, B, a.N, a.P, 1, s, a)
+  WD_TILES(size, WD_CALL)
+#undef WD_CALL
+}
+template <class T>
+static void launch_dz(const LossArgs& a, int size, hipStream_t s) {
+#define WD_CALL(B, WM, WN)                                                                                                      \
+  static std::atomic<uint64_t> done{0};                                                                                         \
+  launch_tile(k_loss_dz<T, B, B, WM, WN>, Tile<T, B, B, WM, WN, false, false>::kBytes, done, 64 * WM * WN, B, a.N, a.dz_ld, 1, s, a)
+  WD_TILES(size, WD_CALL)
+#undef WD_CALL
+}
+template <class T, bool XKR>
+static void launch_product(const ProductArgs& a, int size, int splits, hipStream_t s) {
+#define WD_CALL(B, WM, WN)                                                                                                      \
+  static std::atomic<uint64_t> done{0};                                                                                         \
+  launch_tile(k_product<T, B, B, WM, WN, XKR>, Tile<T, B, B, WM, WN, XKR, true>::kBytes, done, 64 * WM * WN, B, a.M, a.C, splits, s, a)
+  WD_TILES(size, WD_CALL)
+#undef WD_CALL
+}
+
+// How a product is cut: tiles, and splits of its shared columns so that there are enough
+// workgroups (at least eight steps each).
+struct Cut {
+  int size, splits, k_each;
+};
+static Cut cut_product(int64_t M, int64_t C, int64_t K) {
+  Cut c;
+  const int64_t steps = (K + kStepK - 1) / kStepK;
+  c.size = tile_size(M, C);
+  int64_t splits = 1;
+  if (c.size == kSmall) {  // a small output: larger tiles whose columns are split
+    for (int size : {256, 128, 64}) {
+      const int64_t tiles = tiles_of(M, C, size), want = (256 + tiles - 1) / tiles;
+      if (size == 64 || steps / want >= 8) {
+        c.size = size;
+        splits = std::max<int64_t>(1, std::min(want, steps / 8));
+        break;
+      }
+    }
+  }
+  c.k_each = (int)((steps + splits - 1) / splits) * kStepK;
+  c.splits = (int)((K + c.k_each - 1) / c.k_each);
+  return c;
+}
+
+// The plan of a call: what it copies, its pieces, and where things lie in the workspace.
+struct LossPlan {
+  int64_t Dp;                // columns of the copies
+  bool copy_x, copy_w;       // (for the product W x)
+  int64_t block;             // loss: rows of a launch
+  int64_t rows, cols;        // gradients: rows and labels of a piece
+  size_t w, x, part, label_z, info, power, dz, db, sum, split, end;
+};
+
+constexpr int64_t kPieceBytes = 256ll << 20;  // of dz
+
+static bool rows_fit(const void* p, int64_t ld, int64_t rows) { return !((uintptr_t)p & 15) && (ld % 8 == 0 || rows == 1) && ld < (1 << 22); }
+
+static LossPlan plan_loss(const wd_loss_args* a, bool grads) {
+  LossPlan p{};
+  const int64_t N = a->N, D = a->D, P = a->P;
+  p.Dp = align_up(D, 8);
+  p.copy_w = D % 8 != 0 || !rows_fit(a->weight, a->weight_ld, P);
+  p.copy_x = grads || D % 8 != 0 || !rows_fit(a->x, a->x_ld, N);
+  size_t at = 0;
+  const auto take = [&](uint64_t bytes) {
+    const size_t here = at;
+    at += align_up(bytes, 256);
+    return here;
+  };
+  if (p.copy_w) p.w = take((uint64_t)P * p.Dp * 2);
+  if (!grads) {
+    const int64_t cols = (P + 255) / 256;
+    p.block = std::min(N, std::max<int64_t>(16, 8192 / cols) * 256);
+    const int64_t tiles = (P + tile_size(p.block, P) - 1) / tile_size(p.block, P);
+    if (p.copy_x) p.x = take((uint64_t)p.block * p.Dp * 2);
+    p.part = take((uint64_t)p.block * tiles * sizeof(float2));
+    p.label_z = take((uint64_t)p.block * 4);
+  } else {
+    p.rows = N;
+    p.cols = P;
+    const int64_t most = kPieceBytes / 2;
+    if ((uint64_t)N * align_up(P, 64) > (uint64_t)most) {
+      if (N > P)
+        p.rows = std::max<int64_t>(1, most / (int64_t)align_up(P, 64) / 256) * 256;
+      else
+        p.cols = std::max<int64_t>(1, most / N / 256) * 256;
+      // pieces of one size
+      p.rows = std::min<int64_t>(N, align_up((N + (N + p.rows - 1) / p.rows - 1) / ((N + p.rows - 1) / p.rows), 256));
+      p.cols = std::min<int64_t>(P, align_up((P + (P + p.cols - 1) / p.cols - 1) / ((P + p.cols - 1) / p.cols), 256));
+    }
+    p.x = take((uint64_t)p.rows * p.Dp * 2);
+    p.info = take((uint64_t)N * sizeof(RowInfo));
+    p.power = take(8);
+    p.dz = take((uint64_t)p.rows * align_up(p.cols, 64) * 2);
+    if (p.rows < N) p.sum = take((uint64_t)P * p.Dp * 4);
+    if (p.cols < P) p.sum = take((uint64_t)N * p.Dp * 4);
+    uint64_t db = 0, split = 0;  // (the last piece may be cut otherwise)
+    for (int64_t n : {p.rows, (N - 1) % p.rows + 1})
+      for (int64_t c : {p.cols, (P - 1) % p.cols + 1}) {
+        const int size = tile_size(n, align_up(c, 64));
+        db = std::max(db, (uint64_t)((n + size - 1) / size) * c * 4);
+        const Cut cx = cut_product(n, D, c), cw = cut_product(c, D, n);
+        if (a->dx && (cx.splits > 1 || p.cols < P)) split = std::max(split, (uint64_t)cx.splits * n * p.Dp * 4);
+        if (a->dweight && (cw.splits > 1 || p.rows < N)) split = std::max(split, (uint64_t)cw.splits * c * p.Dp * 4);
+      }
+    p.db = take(db);
+    p.split = take(split);
+  }
+  p.end = at;
+  return p;
+}
+
+template <class T>
+static void lay(const void* from, int64_t ld, int64_t N, int D, const RowInfo* info, void* to, int64_t to_ld, hipStream_t s) {
+  const uint64_t blocks = ((uint64_t)N * (to_ld / 8) + 255) / 256;
+  hipLaunchKernelGGL((k_lay<T>), dim3((uint32_t)std::min<uint64_t>(blocks, 1 << 16)), dim3(256), 0, s, (const T*)from, ld, N, D, info, (T*)to, to_ld);
+}
+
+template <class T>
+static void run_loss(const wd_loss_args* a, const LossPlan& p, char* ws, hipStream_t s) {
+  const void* w = a->weight;
+  int64_t w_ld = a->weight_ld * 2;
+  if (p.copy_w) {
+    lay<T>(a->weight, a->weight_ld, a->P, a->D, nullptr, ws + p.w, p.Dp, s);
+    w = ws + p.w, w_ld = p.Dp * 2;
+  }
+  const int size = tile_size(p.block, a->P), tiles = (a->P + size - 1) / size;
+  for (int64_t n0 = 0; n0 < a->N; n0 += p.block) {
+    const int64_t n = std::min(p.block, a->N - n0);
+    const void* x = (const T*)a->x + n0 * a->x_ld;
+    int64_t x_ld = a->x_ld * 2;
+    if (p.copy_x) {
+      lay<T>(x, a->x_ld, n, a->D, nullptr, ws + p.x, p.Dp, s);
+      x = ws + p.x, x_ld = p.Dp * 2;
+    }
+    LossArgs l{};
+    l.x = x, l.w = w, l.x_ld = x_ld, l.w_ld = w_ld, l.N = n, l.P = a->P, l.K = (int)p.Dp, l.bias = a->bias;
+    l.target = a->target + n0, l.part = (float2*)(ws + p.part), l.label_z = (float*)(ws + p.label_z);
+    launch_loss<T>(l, size, s);
+    float* loss = a->loss ? a->loss + n0 : nullptr;
+    float2* stats = a->stats ? (float2*)a->stats + n0 : nullptr;
+    if (tiles <= 64)
+      hipLaunchKernelGGL((k_loss_join<4>), dim3((uint32_t)((n + 63) / 64)), dim3(256), 0, s, l.part, tiles, l.label_z, l.target, l.P, n, loss, stats);
+    else
+      hipLaunchKernelGGL((k_loss_join<64>), dim3((uint32_t)((n + 3) / 4)), dim3(256), 0, s, l.part, tiles, l.label_z, l.target, l.P, n, loss, stats);
+  }
+}
+
+template <class T>
+static void run_grads(const wd_loss_args* a, const LossPlan& p, char* ws, hipStream_t s) {
+  const int64_t N = a->N, P = a->P, D = a->D;
+  const void* w = a->weight;
+  int64_t w_ld = a->weight_ld * 2;
+  const float* power = nullptr;
+  RowInfo* info = (RowInfo*)(ws + p.info);
+  const auto join = [&](ProductArgs q, int splits, const float* before, float* sum) {
+    const uint64_t blocks = ((uint64_t)q.M * ((q.C + 3) / 4) + 255) / 256;
+    hipLaunchKernelGGL((k_product_join<T>), dim3((uint32_t)std::min<uint64_t>(blocks, 1 << 14)), dim3(256), 0, s, q, splits, before, sum);
+  };
+  if (N == 0) {  // sums of nothing
+    ProductArgs q{};
+    q.M = P, q.C = (int)D, q.out = a->dweight, q.out_ld = a->dweight_ld;
+    if (a->dweight) join(q, 0, nullptr, nullptr);
+    if (a->dbias) hipLaunchKernelGGL(k_loss_db, dim3((uint32_t)((P + 255) / 256)), dim3(256), 0, s, nullptr, 0, (int)P, nullptr, false, a->dbias);
+    return;
+  }
+  if (p.copy_w) {
+    lay<T>(a->weight, a->weight_ld, P, (int)D, nullptr, ws + p.w, p.Dp, s);
+    w = ws + p.w, w_ld = p.Dp * 2;
+  }
+  if (__is_same(T, Half)) {
+    power = (const float*)(ws + p.power);
+    hipLaunchKernelGGL(k_power, dim3(1), dim3(1024), 0, s, a->grad, N, (float*)(ws + p.power));
+  }
+  hipLaunchKernelGGL(k_row_info, dim3((uint32_t)((N + 255) / 256)), dim3(256), 0, s, (const float2*)a->stats, a->grad, a->target, (int32_t)P, N, power, info);
+  float* sum = (float*)(ws + p.sum);
+  for (int64_t n0 = 0; n0 < N; n0 += p.rows) {
+    const int64_t n = std::min(p.rows, N - n0);
+    lay<T>((const T*)a->x + n0 * a->x_ld, a->x_ld, n, (int)D, info + n0, ws + p.x, p.Dp, s);
+    for (int64_t c0 = 0; c0 < P; c0 += p.cols) {
+      const int64_t c = std::min(p.cols, P - c0);
+      LossArgs l{};
+      l.x = ws + p.x, l.w = (const char*)w + c0 * w_ld, l.x_ld = p.Dp * 2, l.w_ld = w_ld, l.N = n, l.P = (int)c, l.K = (int)p.Dp;
+      l.bias = a->bias ? a->bias + c0 : nullptr, l.info = info + n0, l.p_first = (int)c0, l.dz = ws + p.dz, l.dz_ld = align_up(c, 64);
+      l.db_part = a->dbias ? (float*)(ws + p.db) : nullptr;
+      const int size = tile_size(n, l.dz_ld);
+      launch_dz<T>(l, size, s);
+      if (a->dbias)
+        hipLaunchKernelGGL(k_loss_db, dim3((uint32_t)((c + 255) / 256)), dim3(256), 0, s, l.db_part, (int)((n + size - 1) / size), (int)c, power, n0 > 0,
+                           a->dbias + c0);
+      if (a->dweight) {
+        const Cut cut = cut_product(c, D, n);
+        ProductArgs q{};
+        q.x = l.dz, q.x_ld = l.dz_ld * 2, q.w = ws + p.x, q.w_ld = p.Dp * 2, q.M = c, q.C = (int)D, q.K = (int)n, q.k_each = cut.k_each;
+        q.part = (float*)(ws + p.split), q.part_ld = p.Dp, q.power = power, q.out_ld = a->dweight_ld;
+        void* out = (T*)a->dweight + c0 * a->dweight_ld;
+        const bool pieces = p.rows < N, last = n0 + p.rows >= N;
+        q.out = !pieces && cut.splits == 1 ? out : nullptr;
+        launch_product<T, true>(q, cut.size, cut.splits, s);
+        if (!q.out) {
+          q.out = last ? out : nullptr;
+          join(q, cut.splits, n0 > 0 ? sum : nullptr, sum);
+        }
+      }
+      if (a->dx) {
+        const Cut cut = cut_product(n, D, c);
+        ProductArgs q{};
+        q.x = l.dz, q.x_ld = l.dz_ld * 2, q.w = l.w, q.w_ld = w_ld, q.M = n, q.C = (int)D, q.K = (int)c, q.k_each = cut.k_each;
+        q.part = (float*)(ws + p.split), q.part_ld = p.Dp, q.power = power, q.info = info + n0, q.out_ld = a->dx_ld;
+        void* out = (T*)a->dx + n0 * a->dx_ld;
+        const bool pieces = p.cols < P, last = c0 + p.cols >= P;
+        q.out = !pieces && cut.splits == 1 ? out : nullptr;
+        launch_product<T, false>(q, cut.size, cut.splits, s);
+        if (!q.out) {
+          q.out = last ? out : nullptr;
+          join(q, cut.splits, c0 > 0 ? sum : nullptr, sum);
+        }
+      }
+    }
+  }
+}
+
+}  // namespace wd
+
+using namespace wd;
+
+static wd_status check_loss(const wd_loss_args* a, bool grads) {
+  if (!a) return fail(WD_EINVAL, "cross_entropy: null arguments");
+  if (a->N < 0 || a->N > INT32_MAX) return fail(WD_EINVAL, "cross_entropy: N out of range");
+  if (a->D < 1 || a->D >= (1 << 22)) return fail(WD_EINVAL, "cross_entropy: D out of range");
+  if (a->P < 1 || a->P >= (1 << 24)) return fail(WD_EINVAL, "cross_entropy: P out of range");
+  if (a->type != WD_F16 && a->type != WD_BF16) return fail(WD_EINVAL, "cross_entropy: type must be WD_F16 or WD_BF16");
+  if (a->x_ld < a->D || a->weight_ld < a->D) return fail(WD_EINVAL, "cross_entropy: row stride too small");
+  if (grads && a->N > (1 << 19) && a->P > (1 << 19)) return fail(WD_EINVAL, "cross_entropy: too many rows and labels for one call");
+  if (grads && ((a->dx && a->dx_ld < a->D) || (a->dweight && a->dweight_ld < a->D)))
+    return fail(WD_EINVAL, "cross_entropy: row stride of a gradient too small");
+  if (!a->weight || (a->N > 0 && (!a->x || !a->target))) return fail(WD_EINVAL, "cross_entropy: null rows, weight or targets");
+  if ((uintptr_t)a->x & 1 || (uintptr_t)a->weight & 1 || (uintptr_t)a->bias & 3 || (uintptr_t)a->target & 3 || (uintptr_t)a->loss & 3 ||
+      (uintptr_t)a->stats & 7)
+    return fail(WD_EINVAL, "cross_entropy: misaligned array");
+  if (!grads) {
+    if (a->N > 0 && !a->loss && !a->stats) return fail(WD_EINVAL, "cross_entropy: null loss and stats");
+    return WD_OK;
+  }
+  if (a->N > 0 && !a->stats) return fail(WD_EINVAL, "cross_entropy: the gradients need stats");
+  if (!a->dx && !a->dweight && !a->dbias) return fail(WD_EINVAL, "cross_entropy: no gradient wanted");
+  if ((uintptr_t)a->grad & 3 || (uintptr_t)a->dx & 1 || (uintptr_t)a->dweight & 1 || (uintptr_t)a->dbias & 3)
+    return fail(WD_EINVAL, "cross_entropy: misaligned gradient");
+  return WD_OK;
+}
+
+static wd_status loss_bytes(const wd_loss_args* a, bool grads, size_t* bytes) {
+  if (!bytes) return fail(WD_EINVAL, "cross_entropy: null output");
+  const wd_status st = check_loss(a, grads);
+  if (st != WD_OK) return st;
+  *bytes = a->N == 0 ? 0 : plan_loss(a, grads).end;
+  return WD_OK;
+}
+
+static wd_status loss_call(const wd_loss_args* a, bool grads, void* ws, size_t ws_bytes, void* stream) {
+  const wd_status st = check_loss(a, grads);
+  if (st != WD_OK) return st;
+  hipStream_t s = (hipStream_t)stream;
+  if (a->N == 0) {
+    if (!grads) return WD_OK;
+    a->type == WD_F16 ? run_grads<Half>(a, LossPlan{}, nullptr, s) : run_grads<Bf16>(a, LossPlan{}, nullptr, s);
+    return hip_check(hipGetLastError(), "cross_entropy");
+  }
+  const LossPlan p = plan_loss(a, grads);
+  if (!ws || ws_bytes < p.end || (uintptr_t)ws & 255) return fail(WD_EINVAL, "cross_entropy: workspace missing, too small or not 256-byte aligned");
+  if (grads)
+    a->type == WD_F16 ? run_grads<Half>(a, p, (char*)ws, s) : run_grads<Bf16>(a, p, (char*)ws, s);
+  else
+    a->type == WD_F16 ? run_loss<Half>(a, p, (char*)ws, s) : run_loss<Bf16>(a, p, (char*)ws, s);
+  return hip_check(hipGetLastError(), "cross_entropy");
+}
+
+extern "C" wd_status wd_cross_entropy_workspace_bytes(const wd_loss_args* a, size_t* bytes) { return loss_bytes(a, false, bytes); }
+extern "C" wd_status wd_cross_entropy(const wd_loss_args* a, void* ws, size_t ws_bytes, void* stream) { return loss_call(a, false, ws, ws_bytes, stream); }
+extern "C" wd_status wd_cross_entropy_grads_workspace_bytes(const wd_loss_args* a, size_t* bytes) { return loss_bytes(a, true, bytes); }
+extern "C" wd_status wd_cross_entropy_grads(const wd_loss_args* a, void* ws, size_t ws_bytes, void* stream) {
+  return loss_call(a, true, ws, ws_bytes, stream);
+}

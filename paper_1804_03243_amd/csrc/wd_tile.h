@@ -1,0 +1,246 @@
+// Products of matrices in tiles of matrix instructions: the operands' way through
+// LDS, and the loop over the columns that two matrices share.
+#pragma once
+
+#include "wd_num.h"
+
+namespace wd {
+
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
+typedef f32x4 __attribute__((aligned(2))) f32x4_any;
+
+__device__ __forceinline__ f32x4 mfma16(uint4 a, uint4 b, f32x4 c, Bf16) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 mfma16(uint4 a, uint4 b, f32x4 c, Half) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+
+// N consecutive outputs of a row, those from n on left out.
+template <class O, int N>
+__device__ __forceinline__ void store_out(O* out, const Few<O, N>& v, int n) {
+  if (n >= N) {
+    *(Few<O, N>*)out = v;
+  } else {
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+      if (i < n) out[i] = v.v[i];
+  }
+}
+
+// 16 bytes per lane from `base` (the same in every lane) + the lane's offset
+// straight to LDS at `to` + 16 * lane (the same `to` in every lane).  The compiler
+// does not see this load (its builtin makes every LDS read wait for all of them):
+// the data is there after loads_left() and a barrier.
+__device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, uint32_t to) {
+  const uint64_t p = (uint64_t)base;  // (into scalar registers, where the compiler would not hold it there)
+  base = (const void*)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(p >> 32)) << 32 |
+                       (uint32_t)__builtin_amdgcn_readfirstlane((int)p));
+  // (m0 is a register that the compiler keeps to itself, and warns of here; it holds no
+  // value there across other code, and is named so that none of its uses is put around this)
+#pragma clang diagnostic push
+#pragma clang diagnostic ignored "-Winline-asm"
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1" ::"v"(offset), "s"(base), "s"(to)
+               : "memory", "m0");
+#pragma clang diagnostic pop
+}
+// Waits until at most N of this wavefront's loads are on their way (they arrive in order).
+template <int N>
+__device__ __forceinline__ void loads_left() {
+  asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory");
+}
+
+constexpr int kStepK = 64;  // columns of a step: 128 bytes of a row
+
+// Where chunk c (16 bytes) of tile row r lies in LDS: at c ^ swizzle, so that the
+// 16 rows of an operand read fall on different banks.
+__device__ __forceinline__ int swizzle(int row) { return (row >> 1) & 7; }
+
+// The tile of this workgroup.  Workgroups go round the eight XCDs, each with an
+// L2 of its own: an XCD takes a run of tiles, in groups of kGroup rows of tiles
+// column by column, so that its workgroups share rows of x and of W.
+constexpr uint32_t kGroup = 8;
+__device__ __forceinline__ void my_tile(uint32_t rows, uint32_t cols, uint32_t& row, uint32_t& col) {
+  const uint32_t all = rows * cols, xcd = blockIdx.x % 8, q = all / 8, r = all % 8;
+  const uint32_t at = xcd * q + min(xcd, r) + blockIdx.x / 8;
+  const uint32_t group = at / (kGroup * cols), first = group * kGroup, height = min(kGroup, rows - first);
+  const uint32_t in = at - first * cols;
+  col = in / height;
+  row = first + in % height;
+}
+
+// Zeros to load where a matrix has ended.
+static __device__ const uint4 k_zeros[kStepK / 8] = {};
+
+// One operand of a tile's product, from the tile's first row or column and the
+// product's first shared column on.  By rows (KR = false) its memory has the shared
+// columns side by side, `ld` bytes from row to row; by shared columns (KR = true) the
+// tile's rows stand side by side, `ld` bytes from a shared column to the next.
+// Either way 16-byte aligned, ld a multiple of 16, and `count` > 0 of the tile's rows
+// exist: by rows, those past them repeat the last one; by shared columns, chunks of
+// eight past them repeat the first chunk (a chunk that holds the last row is read as a
+// whole: ld has room for it).
+struct Operand {
+  const void* p;
+  int64_t ld;
+  int count;
+};
+
+// Where rows 2c.. of a 16-row block of an operand by shared columns lie: chunk c of
+// shared column k at c ^ turn(k).  A transposing read takes four columns k..k+3 for each
+// quarter of the wavefront, eight columns apart: 16 pieces of 32 bytes, spread over the
+// banks as far as the line (ROWS * 2 bytes) lets them.
+template <int ROWS>
+__device__ __forceinline__ int turn(int k) {
+  if constexpr (ROWS >= 256) return ((k & 3) | ((k >> 3) & 3) << 2) * 2;
+  if constexpr (ROWS == 128) return ((k & 3) | ((k >> 3) & 1) << 2) * 2;
+  return ((k >> 1 & 1) | ((k >> 3) & 1) << 1) * 2;
+}
+
+// Transposing read of 16-bit values: within each 16 lanes, lane l gets value l % 4 of
+// what the lanes 4 t + l / 4 address, t = 0..3.
+__device__ __forceinline__ uint2 read_turned(uint32_t at) {
+  typedef __attribute__((ext_vector_type(4))) short s16x4;
+  return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)at));
+}
+
+// The loads of one operand (of ROWS rows) by WAVES wavefronts, and its reads.
+template <int ROWS, bool KR, int WAVES>
+struct Side {
+  static constexpr int kBytes = ROWS * 128;              // of a step
+  static constexpr int kParts = kBytes / 1024 / WAVES;   // loads of a wavefront per step
+  static constexpr int kChunks = KR ? ROWS / 8 : 8;      // chunks of a line in LDS
+  static constexpr int kLines = 64 / kChunks;            // lines of a load
+  static_assert(kBytes % (1024 * WAVES) == 0, "");
+  Operand o;
+  uint32_t from[kParts];
+
+  __device__ __forceinline__ void init(const Operand& op) {
+    o = op;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < kParts; ++i) {
+      const int line = (i * WAVES + wave) * kLines + lane / kChunks;
+      if constexpr (KR) {
+        const int c = (lane % kChunks) ^ turn<ROWS>(line);
+        from[i] = (uint32_t)(line * o.ld + (c * 8 < o.count ? c * 16 : 0));
+      } else {
+        from[i] = (uint32_t)(min(line, o.count - 1) * o.ld + ((lane % kChunks) ^ swizzle(line)) * 16);
+      }
+    }
+  }
+  // Starts the loads of shared columns k0.. of K (a multiple of eight by rows) to LDS at `to`.
+  __device__ __forceinline__ void stage(int k0, int K, uint32_t to) const {
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const char* base = (const char*)o.p + (KR ? (int64_t)k0 * o.ld : (int64_t)k0 * 2);
+    if (k0 + kStepK <= K) {
+#pragma unroll
+      for (int i = 0; i < kParts; ++i)
+        load_to_lds(base, from[i], __builtin_amdgcn_readfirstlane(to + (i * WAVES + wave) * 1024));
+    } else {  // the last ones, zeros behind them
+#pragma unroll
+      for (int i = 0; i < kParts; ++i) {
+        const uint32_t at = __builtin_amdgcn_readfirstlane(to + (i * WAVES + wave) * 1024);
+        const int line = (i * WAVES + wave) * kLines + lane / kChunks;
+        const int k = k0 + (KR ? line : ((lane % kChunks) ^ swizzle(line)) * 8);
+        if (k < K)
+          load_to_lds(base, from[i], at);
+        else
+          load_to_lds(k_zeros, 0, at);
+      }
+    }
+  }
+  // The lane's eight columns of half h (0, 1) of a step at LDS `at`, of row r0 + lane % 16
+  // (r0 a multiple of 16).
+  static __device__ __forceinline__ uint4 read(const char* lds, uint32_t lds0, int at, int r0, int h) {
+    const int lane = threadIdx.x & 63, quad = lane >> 4, l = lane & 15;
+    if constexpr (KR) {
+      const int k = h * 32 + quad * 8 + (l >> 2);
+      const int c = r0 / 8 + (l >> 1 & 1);
+      const uint32_t p = lds0 + at + k * (ROWS * 2) + ((c ^ turn<ROWS>(k)) << 4) + (l & 1) * 8;
+      const uint32_t q = lds0 + at + (k + 4) * (ROWS * 2) + ((c ^ turn<ROWS>(k + 4)) << 4) + (l & 1) * 8;
+      const uint2 lo = read_turned(p), hi = read_turned(q);
+      return make_uint4(lo.x, lo.y, hi.x, hi.y);
+    } else {
+      return *(const uint4*)(lds + at + (r0 + l) * 128 + (((quad | h << 2) ^ swizzle(l)) << 4));
+    }
+  }
+};
+
+// acc[i][j] += the products of x's rows (BM of the tile, TM blocks of 16 a wavefront)
+// with w's (BN, TN blocks) over K shared columns.  w is the matrix instruction's first
+// operand, so that a lane holds four consecutive rows of w (outputs, quad * 4 ..) of one
+// row of x (lane % 16).  Two steps of kStepK columns are in LDS.  A step is two halves:
+// while one is multiplied, the next half's operands are read into registers; between
+// the halves of a step every wavefront has read all of it, and the step after the next
+// starts into its place.  The caller's LDS is free again after a barrier.
+template <class T, int BM, int BN, int WM, int WN, bool XKR, bool WKR>
+struct Tile {
+  static constexpr int kWaves_ = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
+  static constexpr int kStep = (BM + BN) * 128, kBytes = 2 * kStep;
+  using X = Side<BM, XKR, kWaves_>;
+  using W = Side<BN, WKR, kWaves_>;
+
+  static __device__ __forceinline__ void multiply(const Operand& xo, const Operand& wo, int K, char* lds, f32x4 (&acc)[TM][TN]) {
+    const int wave = threadIdx.x >> 6;
+    const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+    X x;
+    W w;
+    x.init(xo);
+    w.init(wo);
+    const auto stage = [&](int k0, int at) {
+      x.stage(k0, K, lds0 + at);
+      w.stage(k0, K, lds0 + at + X::kBytes);
+    };
+    struct Operands {
+      uint4 w[TN], x[TM];
+    } even, odd;
+    const auto read = [&](int at, int half, Operands& o) {
+#pragma unroll
+      for (int j = 0; j < TN; ++j) o.w[j] = W::read(lds, lds0, at + X::kBytes, wn + j * 16, half);
+#pragma unroll
+      for (int i = 0; i < TM; ++i) o.x[i] = X::read(lds, lds0, at, wm + i * 16, half);
+    };
+    const auto products = [&](const Operands& o) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] = mfma16(o.w[j], o.x[i], acc[i][j], T{});
+      // an operand read between every few products
+      constexpr int kReads = TM * (XKR ? 2 : 1) + TN * (WKR ? 2 : 1), kEach = TM * TN / kReads > 0 ? TM * TN / kReads : 1;
+#pragma unroll
+      for (int i = 0; i < kReads; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, kEach, 0);
+      }
+    };
+    int now = 0, next = kStep;
+    stage(0, now);
+    if (kStepK < K) {
+      stage(kStepK, next);
+      2 * kStepK <= K ? loads_left<X::kParts + W::kParts>() : loads_left<0>();
+    } else {
+      loads_left<0>();
+    }
+    __syncthreads();
+    read(now, 0, even);
+    // (One copy of the products and no branch around them: with more the compiler
+    // holds the accumulators twice.  The last step's reads of a next one are of no use.)
+    for (int k0 = 0; k0 < K; k0 += kStepK) {
+      read(now, 1, odd);
+      products(even);
+      loads_left<0>();
+      __syncthreads();  // this step has been read, the next one is there
+      if (k0 + 2 * kStepK < K) stage(k0 + 2 * kStepK, now);
+      read(next, 0, even);
+      products(odd);
+      now = next;
+      next = kStep - next;
+    }
+  }
+};
+
+}  // namespace wd

@@ -112,10 +112,32 @@ class wd_loglikes_args(ctypes.Structure):
                 ("out_row", ctypes.c_void_p)]
 
 
+class wd_loss_args(ctypes.Structure):
+    _fields_ = [("N", ctypes.c_int64), ("D", ctypes.c_int32), ("P", ctypes.c_int32), ("type", ctypes.c_int32),
+                ("x", ctypes.c_void_p), ("x_ld", ctypes.c_int64), ("weight", ctypes.c_void_p),
+                ("weight_ld", ctypes.c_int64), ("bias", ctypes.c_void_p), ("target", ctypes.c_void_p),
+                ("loss", ctypes.c_void_p), ("stats", ctypes.c_void_p), ("grad", ctypes.c_void_p),
+                ("dx", ctypes.c_void_p), ("dx_ld", ctypes.c_int64), ("dweight", ctypes.c_void_p),
+                ("dweight_ld", ctypes.c_int64), ("dbias", ctypes.c_void_p)]
+
+
+class wd_gradient(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("n", ctypes.c_int64), ("out", ctypes.c_void_p),
+                ("type", ctypes.c_int32), ("out_type", ctypes.c_int32)]
+
+
+class wd_micro(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int64), ("D", ctypes.c_int32), ("codes", ctypes.c_void_p),
+                ("scales", ctypes.c_void_p)]
+
+
 EXPORTS = ["wd_graph_bytes", "wd_graph_load", "wd_graph_free", "wd_graph_eps_levels", "wd_graph_eps_paths",
            "wd_workspace_bytes", "wd_decode", "wd_decode_batch", "wd_decode_noalloc", "wd_stream_begin",
            "wd_stream_advance", "wd_stream_end", "wd_stream_free", "wd_project_workspace_bytes", "wd_project",
-           "wd_loglikes_workspace_bytes", "wd_loglikes", "wd_label_masks", "wd_lattice_determinize",
+           "wd_loglikes_workspace_bytes", "wd_loglikes", "wd_label_masks", "wd_cross_entropy_workspace_bytes",
+           "wd_cross_entropy", "wd_cross_entropy_grads_workspace_bytes", "wd_cross_entropy_grads",
+           "wd_clip_workspace_bytes", "wd_clip_gradients", "wd_micro_bytes", "wd_micro_quantize", "wd_micro_values",
+           "wd_micro_project_workspace_bytes", "wd_micro_project", "wd_lattice_determinize",
            "wd_clat_states", "wd_clat_arcs", "wd_clat_finals", "wd_clat_alignment", "wd_clat_free",
            "wd_result_status",
            "wd_result_cost", "wd_result_words", "wd_result_lattice", "wd_result_nodes",
@@ -162,6 +184,18 @@ def lib():
             "wd_loglikes_workspace_bytes": ([VP, P(ctypes.c_size_t)], ctypes.c_int),
             "wd_loglikes": ([VP, VP, ctypes.c_size_t, VP], ctypes.c_int),
             "wd_label_masks": ([VP, ctypes.c_int64, VP, VP, ctypes.c_int64, VP, ctypes.c_int64, VP], ctypes.c_int),
+            "wd_cross_entropy_workspace_bytes": ([VP, P(ctypes.c_size_t)], ctypes.c_int),
+            "wd_cross_entropy": ([VP, VP, ctypes.c_size_t, VP], ctypes.c_int),
+            "wd_cross_entropy_grads_workspace_bytes": ([VP, P(ctypes.c_size_t)], ctypes.c_int),
+            "wd_cross_entropy_grads": ([VP, VP, ctypes.c_size_t, VP], ctypes.c_int),
+            "wd_clip_workspace_bytes": ([ctypes.c_int64, P(ctypes.c_size_t)], ctypes.c_int),
+            "wd_clip_gradients": ([VP, ctypes.c_int64, ctypes.c_double, VP, VP, ctypes.c_size_t, VP], ctypes.c_int),
+            "wd_micro_bytes": ([ctypes.c_int64, ctypes.c_int32, P(ctypes.c_size_t), P(ctypes.c_size_t)], ctypes.c_int),
+            "wd_micro_quantize": ([VP, ctypes.c_int32, ctypes.c_int64, VP, VP], ctypes.c_int),
+            "wd_micro_values": ([VP, VP, ctypes.c_int32, ctypes.c_int64, VP], ctypes.c_int),
+            "wd_micro_project_workspace_bytes": ([VP, ctypes.c_int64, P(ctypes.c_size_t)], ctypes.c_int),
+            "wd_micro_project": ([VP, VP, VP, ctypes.c_int32, ctypes.c_int64, ctypes.c_int64, VP, ctypes.c_int32,
+                                  ctypes.c_int64, VP, ctypes.c_size_t, VP], ctypes.c_int),
             "wd_lattice_determinize": ([VP, ctypes.c_int64, VP, ctypes.c_int64, ctypes.c_int32, VP,
                                         ctypes.c_double, ctypes.c_int64, P(VP)], ctypes.c_int),
             "wd_clat_states": ([VP], ctypes.c_int32),
@@ -329,6 +363,64 @@ def wd_loglikes(args: wd_loglikes_args, ws: int | None, ws_bytes: int, stream: i
 def wd_label_masks(handle: int, N: int, off: int, states: int, n_states: int, mask: int, mask_ld: int,
                    stream: int) -> None:
     _check(lib().wd_label_masks(handle, N, off, states, n_states, mask, mask_ld, stream))
+
+
+def wd_cross_entropy_workspace_bytes(args: wd_loss_args) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().wd_cross_entropy_workspace_bytes(ctypes.byref(args), ctypes.byref(n)))
+    return n.value
+
+
+def wd_cross_entropy(args: wd_loss_args, ws: int | None, ws_bytes: int, stream: int) -> None:
+    _check(lib().wd_cross_entropy(ctypes.byref(args), ws, ws_bytes, stream))
+
+
+def wd_cross_entropy_grads_workspace_bytes(args: wd_loss_args) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().wd_cross_entropy_grads_workspace_bytes(ctypes.byref(args), ctypes.byref(n)))
+    return n.value
+
+
+def wd_cross_entropy_grads(args: wd_loss_args, ws: int | None, ws_bytes: int, stream: int) -> None:
+    _check(lib().wd_cross_entropy_grads(ctypes.byref(args), ws, ws_bytes, stream))
+
+
+def wd_clip_workspace_bytes(n_tensors: int) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().wd_clip_workspace_bytes(n_tensors, ctypes.byref(n)))
+    return n.value
+
+
+def wd_clip_gradients(gradients, n_tensors: int, max_norm: float, norm: int, ws: int | None, ws_bytes: int,
+                      stream: int) -> None:
+    """gradients: a ctypes array of n_tensors wd_gradient."""
+    _check(lib().wd_clip_gradients(gradients, n_tensors, max_norm, norm, ws, ws_bytes, stream))
+
+
+def wd_micro_bytes(rows: int, D: int) -> tuple[int, int]:
+    """Bytes of (codes, scales)."""
+    codes, scales = ctypes.c_size_t(), ctypes.c_size_t()
+    _check(lib().wd_micro_bytes(rows, D, ctypes.byref(codes), ctypes.byref(scales)))
+    return codes.value, scales.value
+
+
+def wd_micro_quantize(x: int, type: int, x_ld: int, out: wd_micro, stream: int) -> None:
+    _check(lib().wd_micro_quantize(x, type, x_ld, ctypes.byref(out), stream))
+
+
+def wd_micro_values(m: wd_micro, out: int, type: int, out_ld: int, stream: int) -> None:
+    _check(lib().wd_micro_values(ctypes.byref(m), out, type, out_ld, stream))
+
+
+def wd_micro_project_workspace_bytes(w: wd_micro, N: int) -> int:
+    n = ctypes.c_size_t()
+    _check(lib().wd_micro_project_workspace_bytes(ctypes.byref(w), N, ctypes.byref(n)))
+    return n.value
+
+
+def wd_micro_project(w: wd_micro, bias: int | None, x: int, type: int, x_ld: int, N: int, out: int, out_type: int,
+                     out_ld: int, ws: int | None, ws_bytes: int, stream: int) -> None:
+    _check(lib().wd_micro_project(ctypes.byref(w), bias, x, type, x_ld, N, out, out_type, out_ld, ws, ws_bytes, stream))
 
 
 def wd_lattice_determinize(links, nodes, start_state: int, node_final=None, beam: float = float("inf"),
@@ -957,3 +1049,257 @@ def loglikes(logits, *, normalize: bool = True, scale: float = 1.0, log_prior=No
     ws = torch.empty(nbytes, dtype=torch.uint8, device=dev) if nbytes else None
     _enqueue(dev, lambda stream: wd_loglikes(a, None if ws is None else ws.data_ptr(), nbytes, stream))
     return out
+
+
+# ------------------------------ fitting the output layer, holding it in four bits
+
+def _workspace(torch, nbytes, device):
+    """(tensor, address) of nbytes; (None, None) for none."""
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+    return ws, None if ws is None else ws.data_ptr()
+
+
+def _loss_args(hidden, weight, target, bias):
+    """The checked inputs of the loss as wd_loss_args."""
+    torch = _torch()
+    types = {t: v for t, v in _types(torch).items() if v != WD_F32}
+    dev = weight.device
+    _matrix(weight, types, dev, "weight")
+    _matrix(hidden, (weight.dtype,), dev, "hidden")
+    (N, D), P = hidden.shape, weight.shape[0]
+    if weight.shape[1] != D:
+        raise ValueError(f"weight must be P x {D}, as wide as hidden")
+    p_target, p_bias = _vector(target, torch.int32, dev, N, "target"), _vector(bias, torch.float32, dev, P, "bias")
+    if target is None:
+        raise ValueError("target is missing")
+    return wd_loss_args(N, D, P, types[weight.dtype], hidden.data_ptr(), _ld(hidden), weight.data_ptr(), _ld(weight),
+                        p_bias, p_target)
+
+
+def _loss(a, device, stats):
+    """Losses float32 [N], with the rows' statistics written to `stats` if given."""
+    torch = _torch()
+    loss = torch.empty(a.N, dtype=torch.float32, device=device)
+    a.loss, a.stats = loss.data_ptr(), None if stats is None else stats.data_ptr()
+    if a.N:
+        ws, p_ws = _workspace(torch, wd_cross_entropy_workspace_bytes(a), device)
+        _enqueue(device, lambda stream: wd_cross_entropy(a, p_ws, 0 if ws is None else ws.numel(), stream))
+    return loss
+
+
+def _loss_grads(a, hidden, weight, bias, stats, grad, wanted):
+    """Gradients of (hidden, weight, bias), None where not wanted."""
+    torch = _torch()
+    dev = weight.device
+    dx = torch.empty((a.N, a.D), dtype=hidden.dtype, device=dev) if wanted[0] else None
+    dw = torch.empty((a.P, a.D), dtype=weight.dtype, device=dev) if wanted[1] else None
+    db = torch.empty(a.P, dtype=torch.float32, device=dev) if wanted[2] and bias is not None else None
+    ptr = lambda t: None if t is None else t.data_ptr()  # noqa: E731
+    a.loss, a.stats, a.grad = None, stats.data_ptr(), ptr(grad)
+    a.dx, a.dx_ld, a.dweight, a.dweight_ld, a.dbias = ptr(dx), a.D, ptr(dw), a.D, ptr(db)
+    if dw is not None or db is not None or dx is not None and a.N:
+        ws, p_ws = _workspace(torch, wd_cross_entropy_grads_workspace_bytes(a), dev)
+        _enqueue(dev, lambda stream: wd_cross_entropy_grads(a, p_ws, 0 if ws is None else ws.numel(), stream))
+    return dx, dw, db
+
+
+_AUTOGRAD = None
+
+
+def _cross_entropy_function():
+    global _AUTOGRAD
+    if _AUTOGRAD is None:
+        torch = _torch()
+
+        class CrossEntropy(torch.autograd.Function):
+            @staticmethod
+            def forward(ctx, hidden, weight, target, bias):
+                a = _loss_args(hidden, weight, target, bias)
+                stats = torch.empty((a.N, 2), dtype=torch.float32, device=weight.device)
+                loss = _loss(a, weight.device, stats)
+                ctx.save_for_backward(hidden, weight, target, bias, stats)
+                return loss
+
+            @staticmethod
+            @torch.autograd.function.once_differentiable
+            def backward(ctx, grad):
+                if torch.cuda.is_current_stream_capturing():
+                    raise RuntimeError("cross_entropy's backward pass cannot be captured: capture cross_entropy_grads")
+                hidden, weight, target, bias, stats = ctx.saved_tensors
+                need = ctx.needs_input_grad
+                dx, dw, db = _loss_grads(_loss_args(hidden, weight, target, bias), hidden, weight, bias, stats,
+                                         grad.contiguous(), (need[0], need[1], need[3]))
+                return dx, dw, None, db
+
+        _AUTOGRAD = CrossEntropy
+    return _AUTOGRAD
+
+
+def cross_entropy(hidden, weight, target, bias=None):
+    """Losses (float32 [N]) of hidden rows [N, D] against their labels under the
+    output layer W x + bias (wd_cross_entropy): log sum exp z - z[target], without
+    the logits ever being in memory.
+
+    hidden [N, D] and weight [P, D] (both float16 or both bfloat16), target int32
+    [N] (a row whose target is outside 0..P-1 has loss 0 and no part in any
+    gradient), bias float32 [P].  Enqueued on the current stream.
+
+    Gradients of hidden, weight and bias flow back through autograd (in their
+    types; once, not twice).  A step that is captured in a graph uses
+    cross_entropy_grads: a backward pass under capture is refused, since autograd
+    would wait on streams that the capture does not hold."""
+    torch = _torch()
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (hidden, weight, bias)):
+        if weight.is_cuda and torch.cuda.is_current_stream_capturing():
+            raise ValueError("cross_entropy of tensors that require a gradient cannot be captured: use cross_entropy_grads")
+        return _cross_entropy_function().apply(hidden, weight, target, bias)
+    return _loss(_loss_args(hidden, weight, target, bias), weight.device, None)
+
+
+def cross_entropy_grads(hidden, weight, target, bias=None, grad=None):
+    """(losses, d_hidden, d_weight, d_bias) of cross_entropy for the gradient
+    `grad` (float32 [N]; default 1) of each row's loss: a step's losses and
+    gradients without autograd, for training loops of their own and captured
+    graphs.  A row with grad 0 has no part in the gradients.  d_bias is None
+    without a bias.  Tensors that require a gradient are taken as they are: the
+    results have no history."""
+    torch = _torch()
+    a = _loss_args(hidden, weight, target, bias)
+    dev = weight.device
+    _vector(grad, torch.float32, dev, a.N, "grad")
+    stats = torch.empty((a.N, 2), dtype=torch.float32, device=dev)
+    loss = _loss(a, dev, stats)
+    return (loss, *_loss_grads(a, hidden, weight, bias, stats, grad, (True, True, True)))
+
+
+def clip_gradients(gradients, max_norm: float, out=None):
+    """The norm over all values of the gradients (a 0-d float32 tensor), and the
+    gradients times min(1, max_norm / norm): in place, or into `out`, as many
+    tensors of the same sizes (of any type, e.g. an optimizer's in 32 bits).
+    max_norm infinity: the norm alone (and copies in `out`).  A norm that is not
+    finite leaves the values as they are (wd_clip_gradients).
+
+    gradients: contiguous float32, float16 or bfloat16 tensors on one device, e.g.
+    [p.grad for p in model.parameters() if p.grad is not None].  No two share
+    memory.  Enqueued on the current stream; nothing waits for the norm."""
+    torch = _torch()
+    types = _types(torch)
+    gradients = list(gradients)
+    if not gradients:
+        raise ValueError("clip_gradients needs tensors")
+    dev = gradients[0].device
+    outs = gradients if out is None else list(out)
+    if len(outs) != len(gradients):
+        raise ValueError("out needs a tensor for each gradient")
+    rows = []
+    for g, o in zip(gradients, outs):
+        if g.device != dev or g.dtype not in types or not g.is_contiguous():
+            raise ValueError(f"gradients must be contiguous float32, float16 or bfloat16 tensors on {dev}")
+        if g is o:
+            rows.append((g.data_ptr(), g.numel(), None, types[g.dtype], 0))
+        else:
+            if o.device != dev or o.dtype not in types or o.shape != g.shape or not o.is_contiguous():
+                raise ValueError(f"out must be contiguous tensors of the gradients' sizes on {dev}")
+            rows.append((g.data_ptr(), g.numel(), o.data_ptr(), types[g.dtype], types[o.dtype]))
+    if dev.type != "cuda":
+        raise ValueError("gradients must be on a GPU")
+    norm = torch.empty((), dtype=torch.float32, device=dev)
+    ws, p_ws = _workspace(torch, wd_clip_workspace_bytes(len(rows)), dev)
+    table = (wd_gradient * len(rows))(*rows)
+    _enqueue(dev, lambda stream: wd_clip_gradients(table, len(rows), max_norm, norm.data_ptr(), p_ws, ws.numel(), stream))
+    return norm
+
+
+class Micro:
+    """A matrix [rows, D] in microscaled 4-bit floating point (wd_micro): `codes`
+    and `scales` are its uint8 device tensors.  Made by micro(), or from tensors
+    that one had."""
+
+    def __init__(self, codes, scales, D: int):
+        torch = _torch()
+        rows, D = codes.shape[0], int(D)
+        want = wd_micro_bytes(rows, D)
+        for t, n, what in ((codes, want[0], "codes"), (scales, want[1], "scales")):
+            if t.dtype != torch.uint8 or t.dim() != 2 or t.shape[0] != rows or t.numel() != n or not t.is_contiguous() \
+                    or t.device != codes.device:
+                raise ValueError(f"{what} must be a contiguous uint8 tensor of {rows} rows, {n} bytes in all, on {codes.device}")
+        self.codes, self.scales, self.rows, self.D, self.device = codes, scales, rows, D, codes.device
+        # (tensors of our own on the same memory)
+        self._kept = (codes.detach(), scales.detach())
+        self.desc = wd_micro(rows, D, codes.data_ptr(), scales.data_ptr())
+
+    def values(self, dtype=None):
+        """The values [rows, D] that it stands for, in bfloat16 (default) or float32, both exact."""
+        torch = _torch()
+        dtype = torch.bfloat16 if dtype is None else dtype
+        if dtype not in (torch.bfloat16, torch.float32):
+            raise ValueError("values are bfloat16 or float32")
+        out = torch.empty((self.rows, self.D), dtype=dtype, device=self.device)
+        _enqueue(self.device, lambda stream: wd_micro_values(self.desc, out.data_ptr(), _types(torch)[dtype], self.D, stream))
+        return out
+
+
+def micro(x):
+    """x [rows, D] (float32, float16 or bfloat16) as a Micro: blocks of 32 columns
+    with a common power of two, four bits a value (wd_micro_quantize).  Enqueued on
+    the current stream.  There is no backward pass: tensors that require a gradient
+    are refused."""
+    torch = _torch()
+    types = _types(torch)
+    _matrix(x, types, x.device, "x")
+    _no_gradient(torch, "micro", x)
+    rows, D = x.shape
+    n_codes, n_scales = wd_micro_bytes(rows, D)
+    each = ((D + 31) // 32 * 16, (D + 511) // 512 * 16)
+    m = Micro(torch.empty((rows, each[0]), dtype=torch.uint8, device=x.device),
+              torch.empty((rows, each[1]), dtype=torch.uint8, device=x.device), D)
+    _enqueue(x.device, lambda stream: wd_micro_quantize(x.data_ptr(), types[x.dtype], _ld(x), m.desc, stream))
+    return m
+
+
+class MicroHead:
+    """An output layer whose weights are held in microscaled 4-bit floating point
+    (wd_micro_project): out[n] = W q(x[n]) + bias, q the rows' own four-bit form.
+
+    weight: a Micro of P rows, e.g. micro(W); bias: float32 [P].  Their memory is
+    kept and read by every call, as Head's is.  There is no backward pass."""
+
+    def __init__(self, weight, bias=None):
+        torch = _torch()
+        if not isinstance(weight, Micro):
+            raise ValueError("weight must be a Micro: micro(weight) makes one")
+        _vector(bias, torch.float32, weight.device, weight.rows, "bias")
+        self.weight, self.D, self.P, self.device = weight, weight.D, weight.rows, weight.device
+        self._bias = None if bias is None else bias.detach()
+        self._ws_bytes = {}  # by number of rows
+        wd_micro_project_workspace_bytes(weight.desc, 0)  # the library's checks
+
+    def project(self, x, out=None, out_dtype=None):
+        """Logits [N, P] of the rows x [N, D] (float32, float16 or bfloat16).
+        out_dtype: float32 (default), float16 or bfloat16; `out`: a tensor to write
+        instead.  Enqueued on the current stream."""
+        torch = _torch()
+        types = _types(torch)
+        _matrix(x, types, self.device, "x")
+        _no_gradient(torch, "project", x, out)
+        N = x.shape[0]
+        if x.shape[1] != self.D:
+            raise ValueError(f"x must be N x {self.D}")
+        if out is None:
+            out = torch.empty((N, self.P), dtype=torch.float32 if out_dtype is None else out_dtype, device=self.device)
+        else:
+            _matrix(out, types, self.device, "out")
+            if tuple(out.shape) != (N, self.P) or out_dtype not in (None, out.dtype):
+                raise ValueError(f"out must be {N} x {self.P} of out_dtype")
+        if out.dtype not in types:
+            raise ValueError("out_dtype must be float32, float16 or bfloat16")
+        nbytes = self._ws_bytes.get(N, -1)
+        if nbytes < 0:
+            nbytes = wd_micro_project_workspace_bytes(self.weight.desc, N)
+            if len(self._ws_bytes) < 256:
+                self._ws_bytes[N] = nbytes
+        ws, p_ws = _workspace(torch, nbytes, self.device)
+        _enqueue(self.device, lambda stream: wd_micro_project(
+            self.weight.desc, None if self._bias is None else self._bias.data_ptr(), x.data_ptr(), types[x.dtype], _ld(x), N,
+            out.data_ptr(), types[out.dtype], _ld(out), p_ws, nbytes, stream))
+        return out
