@@ -198,40 +198,6 @@ __global__ void __launch_bounds__(256) k_lay(const T* from, int64_t ld, int64_t 
   }
 }
 
-// A tile's values to memory, a block of 16 rows at a time through LDS (`mine`, the
-// wavefront's own), so that a store instruction writes whole lines of a row.  value(i, j, e)
-// is the lane's value of row i * 16 + lane % 16, column j * 16 + lane / 16 * 4 + e.
-template <class O, int TM, int TN, class Value>
-__device__ __forceinline__ void store_tile(O* out, int64_t ld, int64_t rows, int64_t cols, char* mine, Value value) {
-  constexpr int kCols = TN * 16, kEach = 16 / sizeof(O);
-  constexpr int kLine = kCols + kEach;  // a row in LDS, padded against bank conflicts
-  constexpr int kLanes = kCols / kEach, kRows = 64 / kLanes;
-  const int lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
-  O* lines = (O*)mine;
-  const int c = (lane % kLanes) * kEach, r0 = lane / kLanes, left = (int)min<int64_t>(cols - c, kEach);
-#pragma unroll
-  for (int i = 0; i < TM; ++i) {
-#pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      struct alignas(4 * sizeof(O)) Four {
-        O v[4];
-      } v;
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v.v[e] = O::of(value(i, j, e));
-      *(Four*)(lines + col * kLine + j * 16 + quad * 4) = v;
-    }
-#pragma unroll
-    for (int q = 0; q < 16; q += kRows) {
-      const uint4 v = *(const uint4*)(lines + (q + r0) * kLine + c);
-      const int64_t n = i * 16 + q + r0;
-      if (n < rows) store_out(out + n * ld + c, __builtin_bit_cast(Few<O, kEach>, v), left);
-    }
-  }
-}
-// Bytes of store_tile's LDS for each wavefront.
-template <class O, int TN>
-constexpr int kStoreBytes = 16 * (TN * 16 + 16 / (int)sizeof(O)) * (int)sizeof(O);
-
 template <class T, int BM, int BN, int WM, int WN>
 __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2) k_loss_dz(LossArgs a, uint32_t row_tiles, uint32_t col_tiles) {
   using Tl = Tile<T, BM, BN, WM, WN, false, false>;

@@ -25,47 +25,63 @@ __device__ __host__ __forceinline__ int64_t micro_scales(int64_t D) { return (D 
 // Where the scale of block b of a row stands.
 __device__ __forceinline__ int64_t scale_at(int64_t b) { return (b & ~15ll) + (b & 3) * 4 + ((b >> 2) & 3); }
 
+// Eight values of a row of D from column k on, zeros past its end.
+template <class T>
+__device__ __forceinline__ void load_values(const T* x, int k, int D, float (&v)[8]) {
+  if (k + 8 <= D) {
+    const Few<T, 8> w = *(const Few<T, 8>*)(x + k);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = w.v[j].f();
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = k + j < D ? x[k + j].f() : 0.0f;
+  }
+}
+
+// A lane's eight values as codes; the four lanes of a block, side by side, hold its 32.
+// Returns the block's scale byte.
+__device__ __forceinline__ uint32_t to_codes(const float (&v)[8], uint32_t& codes) {
+  uint32_t top = 0;  // magnitudes order as their bits do
+#pragma unroll
+  for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
+  top = max(top, dpp32<kDppQuadSwap1>(top, 0));
+  top = max(top, dpp32<kDppQuadSwap2>(top, 0));
+  const bool bad = top >= 0x7f800000u;
+  const int s = max((int)(top >> 23) - 2, 0);
+  const float by = __uint_as_float((uint32_t)(254 - s) << 23);  // 2^(127 - s), exact
+  uint32_t c = 0;
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0] * by, v[1] * by, 1.0f, 0);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2] * by, v[3] * by, 1.0f, 1);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4] * by, v[5] * by, 1.0f, 2);
+  c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6] * by, v[7] * by, 1.0f, 3);
+  codes = bad ? 0 : c;
+  return bad ? 255 : (uint32_t)s;
+}
+
 // Four lanes to a block, eight values each.  Bound by memory.  Lanes of a scale row's
 // padding write its zeros.
 template <class T>
-__global__ void __launch_bounds__(256) k_micro(const T* x, int64_t ld, int64_t N, int D, uint32_t* codes, uint8_t* scales) {
-  const int64_t blocks = micro_blocks(D), sl = micro_scales(D), per = sl * 4;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < N * per; i += (int64_t)gridDim.x * 256) {
+__global__ void __launch_bounds__(256) k_micro(const T* x, int64_t ld, uint32_t N, int D, uint32_t* codes, uint8_t* scales) {
+  const int64_t blocks = micro_blocks(D), sl = micro_scales(D);
+  const uint32_t per = (uint32_t)sl * 4;
+  for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < N * per; i += gridDim.x * 256) {
     const int64_t n = i / per;
     const int e = (int)(i % per), k = e * 8;  // (per is a multiple of 64: a block's lanes stay together)
-    float v[8] = {};
-    if (k + 8 <= D) {
-      const Few<T, 8> w = *(const Few<T, 8>*)(x + n * ld + k);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = w.v[j].f();
-    } else {
-#pragma unroll
-      for (int j = 0; j < 8; ++j)
-        if (k + j < D) v[j] = x[n * ld + k + j].f();
-    }
-    uint32_t top = 0;  // magnitudes order as their bits do
-#pragma unroll
-    for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
-    top = max(top, (uint32_t)__shfl_xor((int)top, 1));
-    top = max(top, (uint32_t)__shfl_xor((int)top, 2));
-    const bool bad = top >= 0x7f800000u;
-    const int s = max((int)(top >> 23) - 2, 0);
-    const float by = __uint_as_float((uint32_t)(254 - s) << 23);  // 2^(127 - s), exact
-    uint32_t c = 0;
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[0] * by, v[1] * by, 1.0f, 0);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[2] * by, v[3] * by, 1.0f, 1);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[4] * by, v[5] * by, 1.0f, 2);
-    c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[6] * by, v[7] * by, 1.0f, 3);
-    if (e < blocks * 4) codes[n * blocks * 4 + e] = bad ? 0 : c;
-    if ((e & 3) == 0) scales[n * sl + scale_at(e >> 2)] = e >= blocks * 4 ? 0 : bad ? 255 : (uint8_t)s;
+    float v[8];
+    load_values(x + n * ld, k, D, v);
+    uint32_t c;
+    const uint32_t s = to_codes(v, c);
+    if (e < blocks * 4) codes[n * blocks * 4 + e] = c;
+    if ((e & 3) == 0) scales[n * sl + scale_at(e >> 2)] = e >= blocks * 4 ? 0 : (uint8_t)s;
   }
 }
 
 // The values, exact in bfloat16 and 32 bits.
 template <class O>
-__global__ void __launch_bounds__(256) k_micro_values(const uint32_t* codes, const uint8_t* scales, int64_t N, int D, O* out, int64_t ld) {
-  const int64_t blocks = micro_blocks(D), sl = micro_scales(D), per = (D + 7) / 8;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < N * per; i += (int64_t)gridDim.x * 256) {
+__global__ void __launch_bounds__(256) k_micro_values(const uint32_t* codes, const uint8_t* scales, uint32_t N, int D, O* out, int64_t ld) {
+  const int64_t blocks = micro_blocks(D), sl = micro_scales(D);
+  const uint32_t per = (D + 7) / 8;
+  for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < N * per; i += gridDim.x * 256) {
     const int64_t n = i / per;
     const int e = (int)(i % per);
     const uint32_t c = codes[n * blocks * 4 + e];
@@ -98,44 +114,190 @@ struct MicroArgs {
   const float* bias;
   void* out;
   int64_t out_ld;
+  bool stream;                     // outputs past the caches
 };
 
-// A wavefront per 16 outputs and 16 rows, operands straight from memory: the simplest product.
-template <class O>
-__global__ void __launch_bounds__(256) k_micro_product(MicroArgs a, uint32_t col_blocks) {
-  const int lane = threadIdx.x & 63, l = lane & 15, quad = lane >> 4;
-  const int64_t at = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int64_t n = at / col_blocks * 16 + l;
-  const int p = (int)(at % col_blocks) * 16;
-  if (n - l >= a.N) return;
-  const int64_t wr = min(p + l, a.P - 1), xr = min<int64_t>(n, a.N - 1);
+// Many rows: tiles of BM rows and BN outputs, as the 16-bit products go (Tile): a step is
+// 128 bytes of a row, here 256 columns, its halves 128.  The scales of two steps
+// come with the even one, 16 bytes of each row, into two places of their own.  A
+// wavefront reads a byte of scale per operand, so that its products all take byte 0.
+template <class O, int BM, int BN, int WM, int WN>
+__global__ void __launch_bounds__(64 * WM * WN, 2) k_micro_tiles(MicroArgs a, uint32_t row_tiles, uint32_t col_tiles) {
+  constexpr int kWaves_ = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
+  using X = Side<BM, false, kWaves_>;
+  using W = Side<BN, false, kWaves_>;
+  constexpr int kStep = (BM + BN) * 128, kScales = 2 * kStep, kScaleStep = (BM + BN) * 16;
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  uint32_t row_tile, col_tile;
+  my_tile(row_tiles, col_tiles, row_tile, col_tile);
+  const int64_t n0 = (int64_t)row_tile * BM;
+  const int p0 = (int)col_tile * BN;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, l = lane & 15, quad = lane >> 4;
+  const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
+  const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
+  const int64_t ld = (int64_t)a.blocks * 16;
+  const int rows = (int)min<int64_t>(BM, a.N - n0), outs = min(BN, a.P - p0), K = a.blocks * 8;
+  X x;
+  W w;
+  x.init({a.x + n0 * ld, ld, rows});
+  w.init({a.w + (int64_t)p0 * ld, ld, outs});
+  // (64 rows' scales to a load, the tile's rows and then its outputs)
+  const int scale_row = wave * 64 + lane;
+  const uint32_t scale_from = (uint32_t)((scale_row < BM ? min(scale_row, rows - 1) : min(scale_row - BM, outs - 1)) * a.sl);
+  const auto stage = [&](int k0, int at) {
+    if (k0 / kStepK % 2 == 0) {
+      const uint32_t to = __builtin_amdgcn_readfirstlane(lds0 + kScales + (k0 / kStepK / 2 & 1) * kScaleStep + wave * 1024);
+      if (scale_row < BM)
+        load_to_lds(a.xs + n0 * a.sl + k0 / kStepK / 2 * 16, scale_from, to);
+      else if (scale_row < BM + BN)
+        load_to_lds(a.ws + (int64_t)p0 * a.sl + k0 / kStepK / 2 * 16, scale_from, to);
+    }
+    x.stage(k0, K, lds0 + at);
+    w.stage(k0, K, lds0 + at + X::kBytes);
+  };
+  struct Operands {
+    uint4 w[TN], x[TM];
+    int ws[TN], xs[TM];
+  } even, odd;
+  const auto read = [&](int k0, int at, int half, Operands& o) {
+    const char* s = lds + kScales + (k0 / kStepK / 2 & 1) * kScaleStep + quad * 4 + (k0 / kStepK % 2 * 2 + half);
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      o.w[j] = W::read(lds, lds0, at + X::kBytes, wn + j * 16, half);
+      o.ws[j] = *(const uint8_t*)(s + (BM + wn + j * 16 + l) * 16);
+    }
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      o.x[i] = X::read(lds, lds0, at, wm + i * 16, half);
+      o.xs[i] = *(const uint8_t*)(s + (wm + i * 16 + l) * 16);
+    }
+  };
+  f32x4 acc[TM][TN] = {};
+  const auto products = [&](const Operands& o) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = mfma4<0>(o.w[j], o.x[i], acc[i][j], o.ws[j], o.xs[i]);
+#pragma unroll
+    for (int i = 0; i < TM + TN; ++i) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, TM * TN / (TM + TN), 0);
+    }
+  };
+  int now = 0, next = kStep;
+  stage(0, now);
+  if (kStepK < K) stage(kStepK, next);
+  loads_left<0>();
+  __syncthreads();
+  read(0, now, 0, even);
+  for (int k0 = 0; k0 < K; k0 += kStepK) {
+    read(k0, now, 1, odd);
+    products(even);
+    loads_left<0>();
+    __syncthreads();  // this step has been read, the next one is there
+    if (k0 + 2 * kStepK < K) stage(k0 + 2 * kStepK, now);
+    read(k0 + kStepK, next, 0, even);
+    products(odd);
+    now = next;
+    next = kStep - next;
+  }
+  float bias[TN][4];
+#pragma unroll
+  for (int j = 0; j < TN; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) bias[j][e] = a.bias ? a.bias[min(p0 + wn + j * 16 + quad * 4 + e, a.P - 1)] : 0.0f;
+  __syncthreads();  // (every wavefront has read its last operands)
+  store_tile<O, TM, TN>((O*)a.out + (n0 + wm) * a.out_ld + p0 + wn, a.out_ld, a.N - n0 - wm, a.P - p0 - wn, lds + wave * kStoreBytes<O, TN>,
+                        [&](int i, int j, int e) { return acc[i][j][e] + bias[j][e]; }, a.stream);
+}
+
+// A few rows (kFewRows at most) in one launch: every workgroup brings them to their four-bit
+// form itself, in LDS, while its first reads of W are under way.  A wavefront takes 16
+// outputs, W straight from memory, the next 512 columns' reads under way while one is
+// multiplied.  Rows in LDS are an odd number of 16-byte blocks apart, so that reads of
+// several rows fall on different banks.
+constexpr int kFewRows = 8;
+template <class T, class O>
+__global__ void __launch_bounds__(256, 4) k_micro_few(MicroArgs a, const T* rows, int64_t ld, int D) {
+  extern __shared__ __attribute__((aligned(16))) char lds[];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, l = lane & 15, quad = lane >> 4;
+  const int p0 = (blockIdx.x * 4 + wave) * 16, N = (int)a.N;
+  const int line = a.blocks | 1;
+  uint8_t* scales = (uint8_t*)lds + N * line * 16;
+  const int64_t r = min(p0 + l, a.P - 1);
+  struct Operands {
+    uint4 w[4];
+    int s;
+  } o[2];
+  const auto read = [&](int b, Operands& o) {
+    o.s = *(const int*)(a.ws + r * a.sl + b + quad * 4);
+#pragma unroll
+    for (int h = 0; h < 4; ++h) o.w[h] = *(const uint4*)(a.w + (r * a.blocks + min(b + h * 4 + quad, a.blocks - 1)) * 16);
+  };
+  read(0, o[0]);
+  const int per = a.sl * 4;  // (a multiple of 64: a block's lanes stay together)
+  for (int i = threadIdx.x; i < N * per; i += 256) {
+    const int n = i / per, e = i % per;
+    float v[8];
+    load_values(rows + n * ld, e * 8, D, v);
+    uint32_t c;
+    const uint32_t s = to_codes(v, c);
+    if (e < a.blocks * 4) *(uint32_t*)(lds + n * line * 16 + e * 4) = c;
+    if ((e & 3) == 0) scales[n * a.sl + scale_at(e >> 2)] = e >= a.blocks * 4 ? 0 : (uint8_t)s;
+  }
+  __syncthreads();
   f32x4 acc = {0, 0, 0, 0};
-  for (int b = 0; b < a.blocks; b += 16) {
-    const int sw = *(const int*)(a.ws + wr * a.sl + b + quad * 4), sx = *(const int*)(a.xs + xr * a.sl + b + quad * 4);
-    uint4 w[4], x[4];
+  const int n = min(l, N - 1);  // (the other lanes' products are of no use)
+  const auto multiply = [&](int b, const Operands& o) {
+    const int s = *(const int*)(scales + n * a.sl + b + quad * 4);
+    uint4 x[4];
 #pragma unroll
     for (int h = 0; h < 4; ++h) {
       const int k = b + h * 4 + quad;
-      w[h] = x[h] = make_uint4(0, 0, 0, 0);
-      if (k < a.blocks) w[h] = *(const uint4*)(a.w + (wr * a.blocks + k) * 16), x[h] = *(const uint4*)(a.x + (xr * a.blocks + k) * 16);
+      x[h] = *(const uint4*)(lds + (n * line + min(k, a.blocks - 1)) * 16);
+      if (k >= a.blocks) x[h] = make_uint4(0, 0, 0, 0);
     }
-    acc = mfma4<0>(w[0], x[0], acc, sw, sx);
-    acc = mfma4<1>(w[1], x[1], acc, sw, sx);
-    acc = mfma4<2>(w[2], x[2], acc, sw, sx);
-    acc = mfma4<3>(w[3], x[3], acc, sw, sx);
+    acc = mfma4<0>(o.w[0], x[0], acc, o.s, s);
+    acc = mfma4<1>(o.w[1], x[1], acc, o.s, s);
+    acc = mfma4<2>(o.w[2], x[2], acc, o.s, s);
+    acc = mfma4<3>(o.w[3], x[3], acc, o.s, s);
+  };
+  for (int b = 0; b < a.blocks; b += 32) {
+    if (b + 16 < a.blocks) read(b + 16, o[1]);
+    multiply(b, o[0]);
+    if (b + 32 < a.blocks) read(b + 32, o[0]);
+    if (b + 16 < a.blocks) multiply(b + 16, o[1]);
   }
-  if (n >= a.N) return;
+  const int p = p0 + quad * 4;
+  if (l >= N) return;
   Few<O, 4> v;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) v.v[e] = O::of(acc[e] + (a.bias ? a.bias[min(p + quad * 4 + e, a.P - 1)] : 0.0f));
-  store_out((O*)a.out + n * a.out_ld + p + quad * 4, v, a.P - p - quad * 4);
+  for (int e = 0; e < 4; ++e) v.v[e] = O::of(acc[e] + (a.bias ? a.bias[min(p + e, a.P - 1)] : 0.0f));
+  store_out((O*)a.out + l * a.out_ld + p, v, a.P - p);
 }
+
+// Rows of a launch, whose lanes are counted in 32 bits.
+static int64_t micro_rows(int64_t lanes_of_a_row) { return std::max<int64_t>(1, (1 << 30) / lanes_of_a_row); }
 
 template <class T>
 static void launch_micro(const void* x, int64_t ld, int64_t N, int D, void* codes, void* scales, hipStream_t s) {
-  const uint64_t blocks = ((uint64_t)N * micro_scales(D) * 4 + 255) / 256;
-  hipLaunchKernelGGL((k_micro<T>), dim3((uint32_t)std::min<uint64_t>(blocks, 1 << 16)), dim3(256), 0, s, (const T*)x, ld, N, D, (uint32_t*)codes,
-                     (uint8_t*)scales);
+  const int64_t per = micro_scales(D) * 4, most = micro_rows(per);
+  for (int64_t n0 = 0; n0 < N; n0 += most) {
+    const int64_t n = std::min(most, N - n0);
+    hipLaunchKernelGGL((k_micro<T>), dim3((uint32_t)std::min<int64_t>((n * per + 255) / 256, 1 << 16)), dim3(256), 0, s, (const T*)x + n0 * ld, ld,
+                       (uint32_t)n, D, (uint32_t*)codes + n0 * micro_blocks(D) * 4, (uint8_t*)scales + n0 * micro_scales(D));
+  }
+}
+
+template <class O>
+static void launch_values(const wd_micro* m, void* out, int64_t ld, hipStream_t s) {
+  const int64_t per = (m->D + 7) / 8, most = micro_rows(per);
+  for (int64_t n0 = 0; n0 < m->rows; n0 += most) {
+    const int64_t n = std::min(most, m->rows - n0);
+    hipLaunchKernelGGL((k_micro_values<O>), dim3((uint32_t)std::min<int64_t>((n * per + 255) / 256, 1 << 16)), dim3(256), 0, s,
+                       (const uint32_t*)m->codes + n0 * micro_blocks(m->D) * 4, (const uint8_t*)m->scales + n0 * micro_scales(m->D), (uint32_t)n, m->D,
+                       (O*)out + n0 * ld, ld);
+  }
 }
 
 static void quantize(const void* x, int64_t ld, int64_t N, int D, int32_t type, void* codes, void* scales, hipStream_t s) {
@@ -147,11 +309,46 @@ static void quantize(const void* x, int64_t ld, int64_t N, int D, int32_t type, 
     launch_micro<Bf16>(x, ld, N, D, codes, scales, s);
 }
 
+template <class O, int BM, int BN, int WM, int WN>
+static void launch_micro_tiles(const MicroArgs& a, hipStream_t s) {
+  const uint32_t rows = (uint32_t)((a.N + BM - 1) / BM), cols = ((uint32_t)a.P + BN - 1) / BN;
+  auto* k = k_micro_tiles<O, BM, BN, WM, WN>;
+  constexpr int bytes = 2 * (BM + BN) * (128 + 16);
+  static_assert(kStoreBytes<O, BN / WN / 16> * WM * WN <= bytes, "");
+  static std::atomic<uint64_t> done{0};
+  allow_lds((const void*)k, bytes, done);
+  hipLaunchKernelGGL(k, dim3(rows * cols), dim3(64 * WM * WN), bytes, s, a, rows, cols);
+}
+
+template <class T, class O>
+static void launch_micro_few(const MicroArgs& a, const void* x, int64_t ld, int D, int bytes, hipStream_t s) {
+  hipLaunchKernelGGL((k_micro_few<T, O>), dim3(((uint32_t)a.P + 63) / 64), dim3(256), bytes, s, a, (const T*)x, ld, D);
+}
+
+// The call's rows, from x (of type T) or, in the calls that bring them to codes first, a.x.
 template <class O>
-static void launch_micro_product(const MicroArgs& a, hipStream_t s) {
-  const uint32_t cols = ((uint32_t)a.P + 15) / 16;
-  const uint64_t waves = (uint64_t)((a.N + 15) / 16) * cols;
-  hipLaunchKernelGGL((k_micro_product<O>), dim3((uint32_t)((waves + 3) / 4)), dim3(256), 0, s, a, cols);
+static void launch_micro_product(MicroArgs a, const void* x, int32_t type, int64_t ld, int D, uint8_t* codes, uint8_t* scales, hipStream_t s) {
+  const int64_t few = a.N * ((a.blocks | 1) * 16 + a.sl);  // bytes of LDS
+  if (a.N <= kFewRows && few <= 64 << 10) {
+    if (type == WD_F32)
+      launch_micro_few<F32, O>(a, x, ld, D, (int)few, s);
+    else if (type == WD_F16)
+      launch_micro_few<Half, O>(a, x, ld, D, (int)few, s);
+    else
+      launch_micro_few<Bf16, O>(a, x, ld, D, (int)few, s);
+    return;
+  }
+  quantize(x, ld, a.N, D, type, codes, scales, s);
+  const auto tiles = [&](int64_t m, int64_t n) { return ((a.N + m - 1) / m) * ((a.P + n - 1) / n); };
+  a.stream = (uint64_t)a.N * a.P * sizeof(O) >= (256u << 20);
+  if (a.N > 64 && tiles(128, 128) >= 384)
+    launch_micro_tiles<O, 128, 128, 2, 2>(a, s);
+  else if (a.N > 32 && tiles(64, 64) >= 192)
+    launch_micro_tiles<O, 64, 64, 2, 2>(a, s);
+  else if (a.N <= 32 && tiles(32, 64) >= 256)
+    launch_micro_tiles<O, 32, 64, 1, 4>(a, s);
+  else
+    launch_micro_tiles<O, 32, 32, 2, 2>(a, s);
 }
 
 }  // namespace wd
@@ -196,13 +393,7 @@ extern "C" wd_status wd_micro_values(const wd_micro* m, void* out, int32_t type,
   if (m->rows == 0) return WD_OK;
   if (!out) return fail(WD_EINVAL, "micro_values: null output");
   if ((uintptr_t)out & (type == WD_F32 ? 3 : 1)) return fail(WD_EINVAL, "micro_values: misaligned output");
-  const uint64_t blocks = ((uint64_t)m->rows * ((m->D + 7) / 8) + 255) / 256;
-  const dim3 grid((uint32_t)std::min<uint64_t>(blocks, 1 << 16)), block(256);
-  hipStream_t s = (hipStream_t)stream;
-  if (type == WD_F32)
-    hipLaunchKernelGGL((k_micro_values<F32>), grid, block, 0, s, (const uint32_t*)m->codes, (const uint8_t*)m->scales, m->rows, m->D, (F32*)out, out_ld);
-  else
-    hipLaunchKernelGGL((k_micro_values<Bf16>), grid, block, 0, s, (const uint32_t*)m->codes, (const uint8_t*)m->scales, m->rows, m->D, (Bf16*)out, out_ld);
+  type == WD_F32 ? launch_values<F32>(m, out, out_ld, (hipStream_t)stream) : launch_values<Bf16>(m, out, out_ld, (hipStream_t)stream);
   return hip_check(hipGetLastError(), "micro_values");
 }
 
@@ -238,20 +429,20 @@ extern "C" wd_status wd_micro_project(const wd_micro* w, const float* bias, cons
   if (!ws || ws_bytes < need || (uintptr_t)ws & 255) return fail(WD_EINVAL, "micro_project: workspace missing, too small or not 256-byte aligned");
   hipStream_t s = (hipStream_t)stream;
   const size_t xe = type == WD_F32 ? 4 : 2, oe = out_type == WD_F32 ? 4 : 2;
-  // (a launch has fewer than 2^32 threads)
-  const int64_t most = std::max<int64_t>(16, std::min<int64_t>(kMicroRows, (1ll << 24) / ((w->rows + 15) / 16) * 16));
+  // (a launch has fewer than 2^32 threads: 2^24 workgroups of 256)
+  const int64_t most = std::max<int64_t>(64, std::min<int64_t>(kMicroRows, (1ll << 23) / ((w->rows + 31) / 32) * 32));
   for (int64_t n0 = 0; n0 < N; n0 += most) {
     const int64_t n = std::min(most, N - n0);
     uint8_t *codes = (uint8_t*)ws, *scales = codes + align_up((uint64_t)n * micro_blocks(w->D) * 16, 256);
-    quantize((const char*)x + n0 * x_ld * xe, x_ld, n, w->D, type, codes, scales, s);
-    MicroArgs a{codes, scales, (const uint8_t*)w->codes, (const uint8_t*)w->scales, n, (int32_t)w->rows, (int32_t)micro_blocks(w->D), (int32_t)micro_scales(w->D),
-                bias, (char*)out + n0 * out_ld * oe, out_ld};
+    const MicroArgs a{codes, scales, (const uint8_t*)w->codes, (const uint8_t*)w->scales, n, (int32_t)w->rows, (int32_t)micro_blocks(w->D),
+                      (int32_t)micro_scales(w->D), bias, (char*)out + n0 * out_ld * oe, out_ld, false};
+    const void* rows = (const char*)x + n0 * x_ld * xe;
     if (out_type == WD_F32)
-      launch_micro_product<F32>(a, s);
+      launch_micro_product<F32>(a, rows, type, x_ld, w->D, codes, scales, s);
     else if (out_type == WD_F16)
-      launch_micro_product<Half>(a, s);
+      launch_micro_product<Half>(a, rows, type, x_ld, w->D, codes, scales, s);
     else
-      launch_micro_product<Bf16>(a, s);
+      launch_micro_product<Bf16>(a, rows, type, x_ld, w->D, codes, scales, s);
   }
   return hip_check(hipGetLastError(), "micro_project");
 }

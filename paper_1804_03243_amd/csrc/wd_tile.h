@@ -243,4 +243,45 @@ struct Tile {
   }
 };
 
+// A tile's values to memory, a block of 16 rows at a time through LDS (`mine`, the
+// wavefront's own), so that a store instruction writes whole lines of a row.  value(i, j, e)
+// is the lane's value of row i * 16 + lane % 16, column j * 16 + lane / 16 * 4 + e.
+// `stream`: past the caches, for outputs larger than they are.
+template <class O, int TM, int TN, class Value>
+__device__ __forceinline__ void store_tile(O* out, int64_t ld, int64_t rows, int64_t cols, char* mine, Value value, bool stream = false) {
+  constexpr int kCols = TN * 16, kEach = 16 / sizeof(O);
+  constexpr int kLine = kCols + kEach;  // a row in LDS, padded against bank conflicts
+  constexpr int kLanes = kCols / kEach, kRows = 64 / kLanes;
+  const int lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
+  O* lines = (O*)mine;
+  const int c = (lane % kLanes) * kEach, r0 = lane / kLanes, left = (int)min<int64_t>(cols - c, kEach);
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+#pragma unroll
+    for (int j = 0; j < TN; ++j) {
+      struct alignas(4 * sizeof(O)) Four {
+        O v[4];
+      } v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v.v[e] = O::of(value(i, j, e));
+      *(Four*)(lines + col * kLine + j * 16 + quad * 4) = v;
+    }
+#pragma unroll
+    for (int q = 0; q < 16; q += kRows) {
+      if (kRows > 16 && r0 >= 16) continue;  // (16 columns of 16 bits: half the lanes)
+      const uint4 v = *(const uint4*)(lines + (q + r0) * kLine + c);
+      const int64_t n = i * 16 + q + r0;
+      if (n < rows) {
+        if (stream && left >= kEach)
+          __builtin_nontemporal_store(__builtin_bit_cast(f32x4, v), (f32x4_any*)(out + n * ld + c));
+        else
+          store_out(out + n * ld + c, __builtin_bit_cast(Few<O, kEach>, v), left);
+      }
+    }
+  }
+}
+// Bytes of store_tile's LDS for each wavefront.
+template <class O, int TN>
+constexpr int kStoreBytes = 16 * (TN * 16 + 16 / (int)sizeof(O)) * (int)sizeof(O);
+
 }  // namespace wd

@@ -126,17 +126,20 @@ def test_products(wf, dtype, out, N, D, P):
             torch.randn(P, generator=gen), out)
 
 
-@pytest.mark.parametrize("N,D,P", [(5000, 328, 2056), (300, 1100, 6000), (1, 512, 100_000), (64, 96, 30_000), (2100, 72, 2100)])
+@pytest.mark.parametrize("N,D,P", [(5000, 328, 2056), (300, 1100, 6000), (1, 512, 100_000), (64, 96, 30_000), (2100, 72, 2100),
+                                   (20, 200, 20_001), (8, 1100, 4001), (9, 600, 4001), (32, 2000, 17_000), (6500, 40, 15_000)])
 def test_large_products(wf, N, D, P):
     """Tiles of every size, against 64 bits on the GPU."""
     gen = torch.Generator(DEV).manual_seed(N)
     x = torch.randn((N, D), generator=gen, device=DEV).to(BF16)
     w = wf.micro(torch.randn((P, D), generator=gen, device=DEV))
     bias = torch.randn(P, generator=gen, device=DEV)
-    y = wf.MicroHead(w, bias).project(x)
     X, W = wf.micro(x).values(F32).double(), w.values(F32).double()
     want, mag = X @ W.T + bias.double(), X.abs() @ W.abs().T + bias.double().abs()
-    close(y, want.cpu(), ((D + 8) * EPS * mag + EPS * want.abs()).cpu())
+    for dtype in (F32, BF16):
+        y = wf.MicroHead(w, bias).project(x, out_dtype=dtype)
+        rel, least = rounding(dtype)
+        close(y, want.cpu(), ((D + 8) * EPS * mag * (1 + rel) + rel * want.abs() + least).cpu())
 
 
 @pytest.mark.parametrize("N", [3, 70, 300])
