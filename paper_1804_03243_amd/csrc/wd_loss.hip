@@ -19,6 +19,7 @@
 // largest |g| to [2^14, 2^15), so that what is 2^29 times smaller than the largest
 // keeps its bits.  db sums the 32-bit values.
 #include <algorithm>
+#include <cmath>
 
 #include "wd_host.h"
 #include "wd_tile.h"
@@ -393,29 +394,36 @@ static void launch_product(const ProductArgs& a, int size, int splits, hipStream
 #undef WD_CALL
 }
 
-// How a product is cut: tiles, and splits of its shared columns so that there are enough
-// workgroups (at least eight steps each).
+// How a product is cut: its tiles' size, and splits of its shared columns for small outputs
+// (which cost 32-bit sums in memory and a launch).  By the time that each way would take:
+// us of a step, of a lone workgroup to a full chip; rounds of workgroups; the sums' bytes at
+// 6 TB/s and 3 us for the launch that joins them.  (Whole calls of one gradient, bfloat16:
+// dz W of 2048 x 1024 over 6000 labels in tiles of 128 80 us in four splits and 101 in one, of 256
+// 83 in six, of 64 88; dz^T x of 6000 x 1024 over 2048 rows 74 in tiles of 128, 88 of 256, 84
+// in two splits of them; dz W of 4096 x 1024 over 20000 347 in four splits of 256, 582 in one, 387
+// in one of 128; of 777 x 1000 over 3001 39 in three splits of 64, 48 in one.)
 struct Cut {
   int size, splits, k_each;
 };
 static Cut cut_product(int64_t M, int64_t C, int64_t K) {
-  Cut c;
+  static constexpr struct {
+    int size, slots;
+    double lone, full;
+  } kinds[] = {{256, 256, 1.8, 1.8}, {128, 512, 0.8, 1.0}, {64, 1024, 0.5, 0.9}};
   const int64_t steps = (K + kStepK - 1) / kStepK;
-  c.size = tile_size(M, C);
-  int64_t splits = 1;
-  if (c.size == kSmall) {  // a small output: larger tiles whose columns are split
-    for (int size : {256, 128, 64}) {
-      const int64_t tiles = tiles_of(M, C, size), want = (256 + tiles - 1) / tiles;
-      if (size == 64 || steps / want >= 8) {
-        c.size = size;
-        splits = std::max<int64_t>(1, std::min(want, steps / 8));
-        break;
-      }
+  Cut best{};
+  double least = INFINITY;
+  for (const auto& k : kinds) {
+    for (int64_t splits = 1; splits <= 32 && (splits == 1 || steps / splits >= 4); ++splits) {
+      const int64_t each = (steps + splits - 1) / splits, parts = (steps + each - 1) / each;
+      const double rounds = (double)(tiles_of(M, C, k.size) * parts) / k.slots;
+      const double busy = rounds <= 1 ? 1 : (rounds + std::ceil(rounds)) / 2;
+      const double us = busy * each * (k.lone + (k.full - k.lone) * std::min(rounds, 1.0)) +
+                        (parts > 1 ? 3 + (double)M * C * 4 * (2 * parts + 0.5) / 6e6 : 0.0);
+      if (us < least) least = us, best = {k.size, (int)parts, (int)(each * kStepK)};
     }
   }
-  c.k_each = (int)((steps + splits - 1) / splits) * kStepK;
-  c.splits = (int)((K + c.k_each - 1) / c.k_each);
-  return c;
+  return best;
 }
 
 // The plan of a call: what it copies, its pieces, and where things lie in the workspace.
