@@ -58,17 +58,23 @@ __device__ __forceinline__ float2 join(float2 a, float2 b) {
   return make_float2(top, a.y * __builtin_amdgcn_exp2f((a.x - at) * kLog2e) + b.y * __builtin_amdgcn_exp2f((b.x - at) * kLog2e));
 }
 
-// Rows and outputs of a tile; the logits of its rows are acc + bias, -inf past the last output.
+// What a tile's end reads of its outputs and rows, brought to LDS before the product: read from
+// memory there it is round trips that nothing hides (losses of 32000 rows to 6000 labels
+// 367 us with the reads at the end, 349 so; gradients of 4096 rows to 100000 3315 and 3220).  The logits are acc + bias, -inf
+// past the last output.
+template <int BN>
+__device__ __forceinline__ void keep_bias(const LossArgs& a, int p0, float* bias) {
+  for (int p = threadIdx.x; p < BN; p += blockDim.x) bias[p] = p0 + p >= a.P ? -INFINITY : a.bias ? a.bias[p0 + p] : 0.0f;
+}
 template <int TN>
-__device__ __forceinline__ void load_bias(const LossArgs& a, int p, float (&bias)[TN][4]) {
+__device__ __forceinline__ void read_bias(const float* kept, float (&bias)[TN][4]) {
   const int quad = (threadIdx.x & 63) >> 4;
 #pragma unroll
-  for (int j = 0; j < TN; ++j)
+  for (int j = 0; j < TN; ++j) {
+    const f32x4 v = *(const f32x4*)(kept + j * 16 + quad * 4);
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int at = p + j * 16 + quad * 4 + e;
-      bias[j][e] = at >= a.P ? -INFINITY : a.bias ? a.bias[at] : 0.0f;
-    }
+    for (int e = 0; e < 4; ++e) bias[j][e] = v[e];
+  }
 }
 
 template <class T, int BM, int BN, int WM, int WN>
@@ -80,19 +86,23 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
   my_tile(row_tiles, col_tiles, row_tile, col_tile);
   const int64_t n0 = (int64_t)row_tile * BM;
   const int p0 = (int)col_tile * BN;
+  float* kept_bias = (float*)(lds + Tl::kBytes);  // [BN]
+  int* labels = (int*)(kept_bias + BN);           // [BM]
+  keep_bias<BN>(a, p0, kept_bias);
+  for (int r = threadIdx.x; r < BM; r += 64 * WM * WN) labels[r] = n0 + r < a.N ? a.target[n0 + r] : -1;
   f32x4 acc[TM][TN] = {};
   Tl::multiply({(const char*)a.x + n0 * a.x_ld, a.x_ld, (int)min<int64_t>(BM, a.N - n0)},
                {(const char*)a.w + (int64_t)p0 * a.w_ld, a.w_ld, min(BN, a.P - p0)}, a.K, lds, acc);
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
   const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
   float bias[TN][4];
-  load_bias<TN>(a, p0 + wn, bias);
+  read_bias<TN>(kept_bias + wn, bias);
   __syncthreads();  // (every wavefront has read its last operands)
   float2* sums = (float2*)lds;  // [WN][BM]
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
     const int64_t n = n0 + wm + i * 16 + col;
-    const int t = n < a.N ? a.target[n] - p0 - wn : -1;
+    const int t = labels[wm + i * 16 + col] - p0 - wn;
     float top = -INFINITY;
 #pragma unroll
     for (int j = 0; j < TN; ++j)
@@ -209,40 +219,34 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
   my_tile(row_tiles, col_tiles, row_tile, col_tile);
   const int64_t n0 = (int64_t)row_tile * BM;
   const int p0 = (int)col_tile * BN;
+  float* kept_bias = (float*)(lds + Tl::kBytes);     // [BN]
+  RowInfo* infos = (RowInfo*)(kept_bias + BN);       // [BM]
+  keep_bias<BN>(a, p0, kept_bias);
+  for (int r = threadIdx.x; r < BM; r += 64 * WM * WN) infos[r] = n0 + r < a.N ? a.info[n0 + r] : RowInfo{0.0f, 0.0f, 0.0f, -1};
   f32x4 acc[TM][TN] = {};
   Tl::multiply({(const char*)a.x + n0 * a.x_ld, a.x_ld, (int)min<int64_t>(BM, a.N - n0)},
                {(const char*)a.w + (int64_t)p0 * a.w_ld, a.w_ld, min(BN, a.P - p0)}, a.K, lds, acc);
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
   const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
   float bias[TN][4], db[TN][4] = {};
-  load_bias<TN>(a, p0 + wn, bias);
-#pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    const int64_t n = n0 + wm + i * 16 + col;
-    const RowInfo r = n < a.N ? a.info[n] : RowInfo{0.0f, 0.0f, 0.0f, -1};
-    const int t = r.label < 0 ? -1 : r.label - a.p_first - p0 - wn;
-#pragma unroll
-    for (int j = 0; j < TN; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float v = r.gs * __builtin_amdgcn_exp2f((acc[i][j][e] + bias[j][e] - r.top) * kLog2e);
-        acc[i][j][e] = r.label >= 0 ? v : 0.0f;  // (a row left out may have infinite logits)
-      }
-    if (__any(t >= 0 && t < TN * 16)) {
-#pragma unroll
-      for (int j = 0; j < TN; ++j)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (t == j * 16 + quad * 4 + e) acc[i][j][e] -= r.g;
-    }
-#pragma unroll
-    for (int j = 0; j < TN; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) db[j][e] += acc[i][j][e];
-  }
+  read_bias<TN>(kept_bias + wn, bias);
   __syncthreads();  // (every wavefront has read its last operands)
+  // (Formed as they are stored, a block of 16 rows at a time: a pass of its own over the
+  // accumulators spilled, and took 3425 us for 3375 of the whole call of 4096 rows to 100000.)
+  RowInfo r{};
+  int t = -1;
   store_tile<T, TM, TN>((T*)a.dz + (n0 + wm) * a.dz_ld + p0 + wn, a.dz_ld, a.N - n0 - wm, a.dz_ld - p0 - wn, lds + wave * kStoreBytes<T, TN>,
-                        [&](int i, int j, int e) { return acc[i][j][e]; });
+                        [&](int i, int j, int e) {
+                          if (j == 0 && e == 0) {
+                            r = infos[wm + i * 16 + col];
+                            t = r.label < 0 ? -1 : r.label - a.p_first - p0 - wn - quad * 4;
+                          }
+                          float v = r.gs * __builtin_amdgcn_exp2f((acc[i][j][e] + bias[j][e] - r.top) * kLog2e);
+                          v = r.label >= 0 ? v : 0.0f;  // (a row left out may have infinite logits)
+                          if (t == j * 16 + e) v -= r.g;
+                          db[j][e] += v;
+                          return v;
+                        });
   if (!a.db_part) return;
   float* sums = (float*)(lds + kStoreBytes<T, TN> * WM * WN);  // [WM][BN]
 #pragma unroll
@@ -299,6 +303,10 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
   my_tile(row_tiles, col_tiles, row_tile, col_tile);
   const int64_t m0 = (int64_t)row_tile * BM;
   const int c0 = (int)col_tile * BN, k0 = (int)blockIdx.y * a.k_each;
+  int* in = (int*)(lds + Tl::kBytes);  // [BM] whether the row has a part in the gradients
+  if (a.out)
+    for (int r = threadIdx.x; r < BM; r += 64 * WM * WN) in[r] = !a.info || a.info[min<int64_t>(m0 + r, a.M - 1)].label >= 0;
+  const float by = a.out && a.power ? a.power[1] : 1.0f;
   f32x4 acc[TM][TN] = {};
   const char* x = (const char*)a.x + (XKR ? m0 * 2 + (int64_t)k0 * a.x_ld : m0 * a.x_ld + (int64_t)k0 * 2);
   Tl::multiply({x, a.x_ld, (int)min<int64_t>(BM, a.M - m0)}, {(const char*)a.w + (int64_t)k0 * a.w_ld + (int64_t)c0 * 2, a.w_ld, min(BN, a.C - c0)},
@@ -307,12 +315,8 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
   const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
   __syncthreads();  // (every wavefront has read its last operands)
   if (a.out) {
-    const float by = a.power ? a.power[1] : 1.0f;
-    bool in[TM];
-#pragma unroll
-    for (int i = 0; i < TM; ++i) in[i] = !a.info || a.info[min<int64_t>(m0 + wm + i * 16 + col, a.M - 1)].label >= 0;
     store_tile<T, TM, TN>((T*)a.out + (m0 + wm) * a.out_ld + c0 + wn, a.out_ld, a.M - m0 - wm, a.C - c0 - wn, lds + wave * kStoreBytes<T, TN>,
-                          [&](int i, int j, int e) { return in[i] ? acc[i][j][e] * by : 0.0f; });
+                          [&](int i, int j, int e) { return in[wm + i * 16 + col] ? acc[i][j][e] * by : 0.0f; });
   } else {
     store_tile<F32, TM, TN>((F32*)a.part + ((int64_t)blockIdx.y * a.M + m0 + wm) * a.part_ld + c0 + wn, a.part_ld, a.M - m0 - wm, a.C - c0 - wn,
                             lds + wave * kStoreBytes<F32, TN>, [&](int i, int j, int e) { return acc[i][j][e]; });
@@ -373,7 +377,7 @@ template <class T>
 static void launch_loss(const LossArgs& a, int size, hipStream_t s) {
 #define WD_CALL(B, WM, WN)                                                                                                      \
   static std::atomic<uint64_t> done{0};                                                                                         \
-  launch_tile(k_loss<T, B, B, WM, WN>, Tile<T, B, B, WM, WN, false, false>::kBytes, done, 64 * WM * WN, B, a.N, a.P, 1, s, a)
+  launch_tile(k_loss<T, B, B, WM, WN>, Tile<T, B, B, WM, WN, false, false>::kBytes + B * 8, done, 64 * WM * WN, B, a.N, a.P, 1, s, a)
   WD_TILES(size, WD_CALL)
 #undef WD_CALL
 }
@@ -381,7 +385,7 @@ template <class T>
 static void launch_dz(const LossArgs& a, int size, hipStream_t s) {
 #define WD_CALL(B, WM, WN)                                                                                                      \
   static std::atomic<uint64_t> done{0};                                                                                         \
-  launch_tile(k_loss_dz<T, B, B, WM, WN>, Tile<T, B, B, WM, WN, false, false>::kBytes, done, 64 * WM * WN, B, a.N, a.dz_ld, 1, s, a)
+  launch_tile(k_loss_dz<T, B, B, WM, WN>, Tile<T, B, B, WM, WN, false, false>::kBytes + B * 20, done, 64 * WM * WN, B, a.N, a.dz_ld, 1, s, a)
   WD_TILES(size, WD_CALL)
 #undef WD_CALL
 }
@@ -389,7 +393,7 @@ template <class T, bool XKR>
 static void launch_product(const ProductArgs& a, int size, int splits, hipStream_t s) {
 #define WD_CALL(B, WM, WN)                                                                                                      \
   static std::atomic<uint64_t> done{0};                                                                                         \
-  launch_tile(k_product<T, B, B, WM, WN, XKR>, Tile<T, B, B, WM, WN, XKR, true>::kBytes, done, 64 * WM * WN, B, a.M, a.C, splits, s, a)
+  launch_tile(k_product<T, B, B, WM, WN, XKR>, Tile<T, B, B, WM, WN, XKR, true>::kBytes + B * 4, done, 64 * WM * WN, B, a.M, a.C, splits, s, a)
   WD_TILES(size, WD_CALL)
 #undef WD_CALL
 }
@@ -435,7 +439,9 @@ struct LossPlan {
   size_t w, x, part, label_z, info, power, dz, db, sum, split, end;
 };
 
-constexpr int64_t kPieceBytes = 256ll << 20;  // of dz
+// Bytes of dz at a time.  (4096 rows to 100000 labels: 128 and 256 MB 3300 us, 512 3170, 1024
+// 3160: fewer, longer products.)
+constexpr int64_t kPieceBytes = 512ll << 20;
 
 static bool rows_fit(const void* p, int64_t ld, int64_t rows) { return !((uintptr_t)p & 15) && (ld % 8 == 0 || rows == 1) && ld < (1 << 22); }
 
