@@ -3,8 +3,9 @@
 //
 // Two passes, since the factor needs every value: sums of squares, a workgroup each a
 // number of chunks, in 64 bits (squares of 32-bit values neither overflow nor vanish, and
-// 64-bit multiply-adds are faster than memory brings values); then every workgroup
-// scales its chunks.  Bound by memory: all values are read twice and written once.
+// 64-bit multiply-adds are faster than memory brings values: with 32-bit ones the call took as
+// long); then every workgroup scales its chunks.  Bound by memory: all values are read twice and written once
+// (250 million of 16 bits into 32: 81 us, 6.2 TB/s, and 308, 4.9 TB/s).
 // The tensors' addresses come as kernel arguments, kTensors at a launch, so that a call
 // copies nothing and can be captured.
 #include <algorithm>
@@ -14,19 +15,26 @@
 
 namespace wd {
 
-constexpr int kTensors = 64;       // of a launch
-constexpr int kChunk = 16384;      // values
-constexpr int kClipGroups = 2048;  // workgroups of a launch at most
+constexpr int kTensors = 160;      // of a launch: its arguments fill 4 KB
+constexpr int kLargeChunk = 16384, kLeastChunk = 1024;  // values
+// Workgroups of a launch at most: about a chunk each.  (250 million values: 2048 428 us, 4096 419,
+// 8192 410, 16384 410.)
+constexpr int kClipGroups = 8192;
 constexpr int kClipThreads = 256;
+// Sums that every workgroup of the second pass adds up for itself; more have a launch of their
+// own.  (A call of 3 tensors, 120 thousand values: 16.2 us, and 20.2 with a launch for them and
+// chunks of 16384.)
+constexpr int kFewParts = 512;
 
 struct ClipArgs {
   const void* data[kTensors];
   void* out[kTensors];
-  int64_t n[kTensors];
   uint32_t first[kTensors + 1];  // chunk of the launch that a tensor begins with
-  uint8_t type[kTensors], out_type[kTensors];
-  int32_t tensors;
+  uint16_t tail[kTensors];       // values of its last chunk
+  uint8_t types[kTensors];       // of data and, times 16, of out
+  int32_t tensors, chunk;
 };
+static_assert(sizeof(ClipArgs) <= 4032, "");
 
 // The tensor of chunk c.
 __device__ __forceinline__ int tensor_of(const ClipArgs& a, uint32_t c) {
@@ -41,11 +49,29 @@ __device__ __forceinline__ int tensor_of(const ClipArgs& a, uint32_t c) {
   return lo;
 }
 
+// A workgroup's chunks are a run, each(tensor, first value, values) of one after another:
+// from its begin, or with `back` from its end.
+template <bool BACK, class F>
+__device__ __forceinline__ void run_of_chunks(const ClipArgs& a, F each) {
+  const uint32_t chunks = a.first[a.tensors], q = chunks / gridDim.x, r = chunks % gridDim.x, b = blockIdx.x;
+  const uint32_t from = b * q + min(b, r), to = from + q + (b < r ? 1 : 0);
+  int t = tensor_of(a, BACK ? to - 1 : from);
+  for (uint32_t i = from; i < to; ++i) {
+    const uint32_t c = BACK ? to - 1 - (i - from) : i;
+    if (BACK)
+      while (a.first[t] > c) --t;
+    else
+      while (a.first[t + 1] <= c) ++t;
+    each(t, (int64_t)(c - a.first[t]) * a.chunk, c + 1 == a.first[t + 1] ? (int)a.tail[t] : a.chunk);
+  }
+}
+
 __device__ __forceinline__ double wave_sum(double v) {
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
   return v;
 }
-// In every thread; the same bits every time.
+// In every thread of THREADS; the same bits every time.
+template <int THREADS>
 __device__ __forceinline__ double block_sum(double v, double* lds) {
   v = wave_sum(v);
   __syncthreads();
@@ -53,21 +79,38 @@ __device__ __forceinline__ double block_sum(double v, double* lds) {
   __syncthreads();
   v = lds[0];
 #pragma unroll
-  for (int k = 1; k < kClipThreads / 64; ++k) v += lds[k];
+  for (int k = 1; k < THREADS / 64; ++k) v += lds[k];
   return v;
+}
+
+// 16 bytes past the caches: most of the values are not there any more when they are read again (250
+// million values 428 us so, 455 by ordinary loads; in the second pass it makes no difference).
+template <class T, int N>
+__device__ __forceinline__ Few<T, N> load_once(const T* p) {
+  typedef uint32_t __attribute__((ext_vector_type(sizeof(Few<T, N>) / 4), aligned(sizeof(T)))) Words;
+  return __builtin_bit_cast(Few<T, N>, __builtin_nontemporal_load((const Words*)p));
+}
+
+template <class T, int N>
+__device__ __forceinline__ double add_squares(const Few<T, N>& v, double s) {
+#pragma unroll
+  for (int e = 0; e < N; ++e) s = __builtin_fma((double)v.v[e].f(), (double)v.v[e].f(), s);
+  return s;
 }
 
 template <class T>
 __device__ __forceinline__ double chunk_squares(const T* p, int n) {
-  constexpr int kEach = 16 / sizeof(T);
+  constexpr int kEach = 16 / sizeof(T), kAhead = 4, kStep = kClipThreads * kEach;
   double s = 0.0;
   int i = threadIdx.x * kEach;
-#pragma unroll 4
-  for (; i + kEach <= n; i += kClipThreads * kEach) {
-    const Few<T, kEach> v = *(const Few<T, kEach>*)(p + i);
+  for (; i + (kAhead - 1) * kStep + kEach <= n; i += kAhead * kStep) {  // (reads under way together)
+    Few<T, kEach> v[kAhead];
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) s = __builtin_fma((double)v.v[e].f(), (double)v.v[e].f(), s);
+    for (int k = 0; k < kAhead; ++k) v[k] = load_once<T, kEach>(p + i + k * kStep);
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) s = add_squares(v[k], s);
   }
+  for (; i + kEach <= n; i += kStep) s = add_squares(load_once<T, kEach>(p + i), s);
   for (; i < n; ++i) s = __builtin_fma((double)p[i].f(), (double)p[i].f(), s);
   return s;
 }
@@ -75,31 +118,36 @@ __device__ __forceinline__ double chunk_squares(const T* p, int n) {
 __global__ void __launch_bounds__(kClipThreads) k_clip_squares(ClipArgs a, double* part) {
   __shared__ double lds[kClipThreads / 64];
   double s = 0.0;
-  for (uint32_t c = blockIdx.x; c < a.first[a.tensors]; c += gridDim.x) {
-    const int t = tensor_of(a, c);
-    const int64_t at = (int64_t)(c - a.first[t]) * kChunk;
-    const int n = (int)min<int64_t>(kChunk, a.n[t] - at);
-    if (a.type[t] == WD_F32)
+  run_of_chunks<false>(a, [&](int t, int64_t at, int n) {
+    const int type = a.types[t] & 15;
+    if (type == WD_F32)
       s += chunk_squares((const F32*)a.data[t] + at, n);
-    else if (a.type[t] == WD_F16)
+    else if (type == WD_F16)
       s += chunk_squares((const Half*)a.data[t] + at, n);
     else
       s += chunk_squares((const Bf16*)a.data[t] + at, n);
-  }
-  s = block_sum(s, lds);
+  });
+  s = block_sum<kClipThreads>(s, lds);
   if (threadIdx.x == 0) part[blockIdx.x] = s;
 }
 
-// The norm from the launches' sums, and the factor: 1 where the norm is not above
-// max_norm, and where it is not finite (nothing is scaled then).
-__global__ void __launch_bounds__(kClipThreads) k_clip_norm(const double* part, int64_t parts, double max_norm, float* norm, float* factor) {
-  __shared__ double lds[kClipThreads / 64];
+// The norm from the launches' sums, in every thread.
+template <int THREADS>
+__device__ __forceinline__ double norm_of(const double* part, int64_t parts, double* lds) {
   double s = 0.0;
-  for (int64_t i = threadIdx.x; i < parts; i += kClipThreads) s += part[i];
-  s = sqrt(block_sum(s, lds));
+#pragma unroll 8
+  for (int64_t i = threadIdx.x; i < parts; i += THREADS) s += part[i];
+  return sqrt(block_sum<THREADS>(s, lds));
+}
+// 1 where the norm is not above max_norm, and where it is not finite (nothing is scaled then).
+__device__ __forceinline__ float factor_of(double norm, double max_norm) { return norm > max_norm && norm < INFINITY ? (float)(max_norm / norm) : 1.0f; }
+
+__global__ void __launch_bounds__(1024) k_clip_norm(const double* part, int64_t parts, double max_norm, float* norm, float* factor) {
+  __shared__ double lds[16];
+  const double s = norm_of<1024>(part, parts, lds);
   if (threadIdx.x != 0) return;
   *norm = (float)s;
-  *factor = s > max_norm && s < INFINITY ? (float)(max_norm / s) : 1.0f;
+  *factor = factor_of(s, max_norm);
 }
 
 template <class T, class O>
@@ -127,23 +175,28 @@ __device__ __forceinline__ void chunk_to(const T* p, void* out, int out_type, in
     chunk_scaled(p + at, (Bf16*)out + at, n, by);
 }
 
-__global__ void __launch_bounds__(kClipThreads) k_clip_scale(ClipArgs a, const float* factor) {
-  const float by = *factor;
-  // the chunks that were read last first: they may still be in the caches
-  const uint32_t chunks = a.first[a.tensors];
-  for (uint32_t i = blockIdx.x; i < chunks; i += gridDim.x) {
-    const uint32_t c = chunks - 1 - i;
-    const int t = tensor_of(a, c);
-    if (by == 1.0f && a.out[t] == a.data[t]) continue;
-    const int64_t at = (int64_t)(c - a.first[t]) * kChunk;
-    const int n = (int)min<int64_t>(kChunk, a.n[t] - at);
-    if (a.type[t] == WD_F32)
-      chunk_to((const F32*)a.data[t], a.out[t], a.out_type[t], at, n, by);
-    else if (a.type[t] == WD_F16)
-      chunk_to((const Half*)a.data[t], a.out[t], a.out_type[t], at, n, by);
-    else
-      chunk_to((const Bf16*)a.data[t], a.out[t], a.out_type[t], at, n, by);
+// Few sums: the workgroups add them up, and the first one writes the norm (`norm` not NULL).
+__global__ void __launch_bounds__(kClipThreads) k_clip_scale(ClipArgs a, const float* factor, const double* part, int parts, double max_norm, float* norm) {
+  __shared__ double lds[kClipThreads / 64];
+  float by;
+  if (parts) {
+    const double s = norm_of<kClipThreads>(part, parts, lds);
+    if (norm && blockIdx.x == 0 && threadIdx.x == 0) *norm = (float)s;
+    by = factor_of(s, max_norm);
+  } else {
+    by = *factor;
   }
+  // the chunks that were read last first: they may still be in the caches
+  run_of_chunks<true>(a, [&](int t, int64_t at, int n) {
+    if (by == 1.0f && a.out[t] == a.data[t]) return;
+    const int type = a.types[t] & 15, out_type = a.types[t] >> 4;
+    if (type == WD_F32)
+      chunk_to((const F32*)a.data[t], a.out[t], out_type, at, n, by);
+    else if (type == WD_F16)
+      chunk_to((const Half*)a.data[t], a.out[t], out_type, at, n, by);
+    else
+      chunk_to((const Bf16*)a.data[t], a.out[t], out_type, at, n, by);
+  });
 }
 
 }  // namespace wd
@@ -151,7 +204,6 @@ __global__ void __launch_bounds__(kClipThreads) k_clip_scale(ClipArgs a, const f
 using namespace wd;
 
 static size_t type_bytes(int32_t type) { return type == WD_F32 ? 4 : 2; }
-// A launch more may begin in the middle of a long list, where its tensors have too many chunks together.
 static int64_t clip_launches(int64_t tensors) { return (tensors + kTensors - 1) / kTensors; }
 
 extern "C" wd_status wd_clip_workspace_bytes(int64_t n_tensors, size_t* bytes) {
@@ -200,21 +252,26 @@ extern "C" wd_status wd_clip_gradients(const wd_gradient* g, int64_t n_tensors, 
   hipStream_t s = (hipStream_t)stream;
   float* factor = (float*)ws;
   double* part = (double*)((char*)ws + 256);
-  int64_t parts = 0;
+  // Smaller chunks where there are few values, for as many workgroups as the chip holds.
+  uint64_t values = 0;
+  for (int64_t i = 0; i < n_tensors; ++i) values += (uint64_t)g[i].n;
+  int chunk = kLeastChunk;
+  while (chunk < kLargeChunk && values / chunk > 1024) chunk *= 2;
   const auto each = [&](auto&& launch) -> wd_status {
     for (int64_t i0 = 0; i0 < n_tensors; i0 += kTensors) {
       ClipArgs a;
-      a.tensors = 0;
+      a.tensors = 0, a.chunk = chunk;
       uint64_t chunks = 0;
       for (int64_t i = i0; i < std::min(i0 + kTensors, n_tensors); ++i) {
         const wd_gradient& t = g[i];
         if (t.n == 0) continue;
         const int k = a.tensors++;
-        a.data[k] = t.data, a.out[k] = t.out ? t.out : (void*)t.data, a.n[k] = t.n;
-        a.type[k] = (uint8_t)t.type, a.out_type[k] = (uint8_t)(t.out ? t.out_type : t.type);
-        a.first[k] = (uint32_t)chunks;
-        chunks += (uint64_t)(t.n + kChunk - 1) / kChunk;
-        if (chunks > UINT32_MAX - kClipGroups) return fail(WD_EINVAL, "clip: too many values for one call");
+        const uint64_t n = (uint64_t)(t.n + chunk - 1) / chunk;
+        a.data[k] = t.data, a.out[k] = t.out ? t.out : (void*)t.data;
+        a.types[k] = (uint8_t)(t.type | (t.out ? t.out_type : t.type) << 4);
+        a.first[k] = (uint32_t)chunks, a.tail[k] = (uint16_t)(t.n - (int64_t)(n - 1) * chunk);
+        chunks += n;
+        if (chunks > INT32_MAX) return fail(WD_EINVAL, "clip: too many values for one call");
       }
       if (a.tensors == 0) continue;
       a.first[a.tensors] = (uint32_t)chunks;
@@ -222,15 +279,23 @@ extern "C" wd_status wd_clip_gradients(const wd_gradient* g, int64_t n_tensors, 
     }
     return WD_OK;
   };
-  wd_status st = each([&](const ClipArgs& a, uint32_t groups) {
+  int64_t parts = 0;
+  wd_status st = each([](const ClipArgs&, uint32_t) {});  // (refused before any device work)
+  if (st != WD_OK) return st;
+  each([&](const ClipArgs& a, uint32_t groups) {
     hipLaunchKernelGGL(k_clip_squares, dim3(groups), dim3(kClipThreads), 0, s, a, part + parts);
     parts += groups;
   });
-  if (st != WD_OK) return st;
-  hipLaunchKernelGGL(k_clip_norm, dim3(1), dim3(kClipThreads), 0, s, part, parts, max_norm, norm, factor);
-  if (max_norm < INFINITY || apart)
-    st = each([&](const ClipArgs& a, uint32_t groups) { hipLaunchKernelGGL(k_clip_scale, dim3(groups), dim3(kClipThreads), 0, s, a, factor); });
-  return st != WD_OK ? st : hip_check(hipGetLastError(), "clip");
+  const bool scaled = max_norm < INFINITY || apart, few = parts > 0 && parts <= kFewParts && scaled;
+  if (!few) hipLaunchKernelGGL(k_clip_norm, dim3(1), dim3(1024), 0, s, part, parts, max_norm, norm, factor);
+  if (scaled) {
+    float* to = norm;
+    each([&](const ClipArgs& a, uint32_t groups) {
+      hipLaunchKernelGGL(k_clip_scale, dim3(groups), dim3(kClipThreads), 0, s, a, factor, part, few ? (int)parts : 0, max_norm, to);
+      to = nullptr;
+    });
+  }
+  return hip_check(hipGetLastError(), "clip");
 } catch (const std::bad_alloc&) {
   return fail(WD_EINVAL, "clip: out of host memory");
 }

@@ -175,37 +175,63 @@ __global__ void __launch_bounds__(1024) k_power(const float* g, int64_t N, float
   power[1] = 1.0f / power[0];
 }
 
-__global__ void __launch_bounds__(256) k_row_info(const float2* stats, const float* g, const int32_t* target, int32_t P, int64_t N,
-                                                  const float* power, RowInfo* info) {
-  const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  if (n >= N) return;
+// What the gradients need of a row.
+__device__ __forceinline__ RowInfo row_info(const float2* stats, const float* g, const int32_t* target, int32_t P, const float* power, int64_t n) {
   const float2 s = stats[n];
   const int t = target[n];
   const float gn = (g ? g[n] : 1.0f) * (power ? power[0] : 1.0f);
   // (a row without a finite logit has no softmax)
   const bool in = t >= 0 && t < P && gn != 0.0f && !(s.x == -INFINITY && s.y == 0.0f);
-  info[n] = in ? RowInfo{s.x, gn / s.y, gn, t} : RowInfo{0.0f, 0.0f, 0.0f, -1};
+  return in ? RowInfo{s.x, gn / s.y, gn, t} : RowInfo{0.0f, 0.0f, 0.0f, -1};
 }
 
-// Rows of D elements to rows of `to_ld` >= D with zeros behind them; rows without a part
-// in the gradients (info) are zeros, so that nothing of theirs reaches a sum.
+// Eight elements of a row of D from k on, zeros past its end.
 template <class T>
-__global__ void __launch_bounds__(256) k_lay(const T* from, int64_t ld, int64_t N, int D, const RowInfo* info, T* to, int64_t to_ld) {
-  const int64_t per = to_ld / 8;
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < N * per; i += (int64_t)gridDim.x * 256) {
+__device__ __forceinline__ Few<T, 8> load_few(const T* row, int k, int D) {
+  if (k + 8 <= D) return *(const Few<T, 8>*)(row + k);
+  Few<T, 8> v{};
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (k + e < D) v.v[e] = row[k + e];
+  return v;
+}
+
+// Rows of D elements to rows of `to_ld` >= D (a multiple of eight) with zeros behind them.
+template <class T>
+__global__ void __launch_bounds__(256) k_lay(const T* from, int64_t ld, uint32_t N, int D, T* to, int64_t to_ld) {
+  const uint32_t per = (uint32_t)(to_ld / 8);
+  for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < N * per; i += gridDim.x * 256) {
     const int64_t n = i / per;
     const int k = (int)(i % per) * 8;
-    Few<T, 8> v{};
-    if (!info || info[n].label >= 0) {
-      if (k + 8 <= D) {
-        v = *(const Few<T, 8>*)(from + n * ld + k);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (k + e < D) v.v[e] = from[n * ld + k + e];
-      }
-    }
-    *(uint4*)(to + n * to_ld + k) = __builtin_bit_cast(uint4, v);
+    *(uint4*)(to + n * to_ld + k) = __builtin_bit_cast(uint4, load_few(from + n * ld, k, D));
+  }
+}
+
+// The same of the rows of x that the gradients read, with what they need of each row.  A row
+// without a part in them is zeros, so that nothing of its reaches a sum.
+struct PrepareArgs {
+  const void* x;
+  int64_t x_ld;
+  uint32_t N;
+  int32_t D, P;
+  const float2* stats;
+  const float* g;
+  const int32_t* target;
+  const float* power;
+  RowInfo* info;
+  void* to;
+  int64_t to_ld;
+};
+template <class T>
+__global__ void __launch_bounds__(256) k_loss_prepare(PrepareArgs a) {
+  const uint32_t per = (uint32_t)(a.to_ld / 8);
+  for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < a.N * per; i += gridDim.x * 256) {
+    const int64_t n = i / per;
+    const int k = (int)(i % per) * 8;
+    const RowInfo r = row_info(a.stats, a.g, a.target, a.P, a.power, n);
+    const Few<T, 8> v = load_few((const T*)a.x + n * a.x_ld, k, a.D);
+    if (k == 0) a.info[n] = r;
+    *(uint4*)((T*)a.to + n * a.to_ld + k) = r.label >= 0 ? __builtin_bit_cast(uint4, v) : make_uint4(0, 0, 0, 0);
   }
 }
 
@@ -266,16 +292,23 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
   }
 }
 
-// db of a piece: the row tiles' sums in their order.
-__global__ void __launch_bounds__(256) k_loss_db(const float* part, int tiles, int P, const float* power, bool add, float* db) {
-  const int p = blockIdx.x * 256 + threadIdx.x;
-  if (p >= P) return;
+// db of a piece: the row tiles' sums in their order, behind those of earlier pieces.
+struct DbArgs {
+  const float* part;  // [tiles][P]; NULL: not wanted
+  int32_t tiles, P;
+  const float* power;
+  bool add;
+  float* db;
+};
+__device__ __forceinline__ void sum_db(const DbArgs& a, int64_t p) {
+  if (p >= a.P) return;
   float s = 0.0f;
 #pragma unroll 8
-  for (int t = 0; t < tiles; ++t) s += part[(int64_t)t * P + p];
-  if (power) s *= power[1];
-  db[p] = add ? db[p] + s : s;
+  for (int t = 0; t < a.tiles; ++t) s += a.part[(int64_t)t * a.P + p];
+  if (a.power) s *= a.power[1];
+  a.db[p] = a.add ? a.db[p] + s : s;
 }
+__global__ void __launch_bounds__(256) k_loss_db(DbArgs a) { sum_db(a, (int64_t)blockIdx.x * 256 + threadIdx.x); }
 
 // out[m][c] = sum over k of x(m, k) w(c, k): dz W (x by rows, w by shared columns) and
 // dz^T x (both by shared columns).
@@ -291,6 +324,7 @@ struct ProductArgs {
   int64_t part_ld;
   const float* power;  // NULL: 1
   const RowInfo* info; // rows without a part in the gradients are zeros; NULL: none
+  DbArgs db;           // dz^T x: the labels' db, by the workgroups of the first columns
 };
 
 template <class T, int BM, int BN, int WM, int WN, bool XKR>
@@ -314,6 +348,8 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15;
   const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
   __syncthreads();  // (every wavefront has read its last operands)
+  if (XKR && a.db.part && col_tile == 0 && blockIdx.y == 0)
+    for (int r = threadIdx.x; r < BM; r += 64 * WM * WN) sum_db(a.db, m0 + r);
   if (a.out) {
     store_tile<T, TM, TN>((T*)a.out + (m0 + wm) * a.out_ld + c0 + wn, a.out_ld, a.M - m0 - wm, a.C - c0 - wn, lds + wave * kStoreBytes<T, TN>,
                           [&](int i, int j, int e) { return in[wm + i * 16 + col] ? acc[i][j][e] * by : 0.0f; });
@@ -500,10 +536,21 @@ static LossPlan plan_loss(const wd_loss_args* a, bool grads) {
   return p;
 }
 
+// launch(n0, n) for the rows in parts whose lanes (a row's `per`) are counted in 32 bits.
+template <class F>
+static void in_rows(int64_t N, int64_t per, F launch) {
+  const int64_t most = std::max<int64_t>(1, (1 << 30) / per);
+  for (int64_t n0 = 0; n0 < N; n0 += most) {
+    const int64_t n = std::min(most, N - n0);
+    launch(n0, n, dim3((uint32_t)std::min<int64_t>((n * per + 255) / 256, 1 << 16)));
+  }
+}
+
 template <class T>
-static void lay(const void* from, int64_t ld, int64_t N, int D, const RowInfo* info, void* to, int64_t to_ld, hipStream_t s) {
-  const uint64_t blocks = ((uint64_t)N * (to_ld / 8) + 255) / 256;
-  hipLaunchKernelGGL((k_lay<T>), dim3((uint32_t)std::min<uint64_t>(blocks, 1 << 16)), dim3(256), 0, s, (const T*)from, ld, N, D, info, (T*)to, to_ld);
+static void lay(const void* from, int64_t ld, int64_t N, int D, void* to, int64_t to_ld, hipStream_t s) {
+  in_rows(N, to_ld / 8, [&](int64_t n0, int64_t n, dim3 grid) {
+    hipLaunchKernelGGL((k_lay<T>), grid, dim3(256), 0, s, (const T*)from + n0 * ld, ld, (uint32_t)n, D, (T*)to + n0 * to_ld, to_ld);
+  });
 }
 
 template <class T>
@@ -511,7 +558,7 @@ static void run_loss(const wd_loss_args* a, const LossPlan& p, char* ws, hipStre
   const void* w = a->weight;
   int64_t w_ld = a->weight_ld * 2;
   if (p.copy_w) {
-    lay<T>(a->weight, a->weight_ld, a->P, a->D, nullptr, ws + p.w, p.Dp, s);
+    lay<T>(a->weight, a->weight_ld, a->P, a->D, ws + p.w, p.Dp, s);
     w = ws + p.w, w_ld = p.Dp * 2;
   }
   const int size = tile_size(p.block, a->P), tiles = (a->P + size - 1) / size;
@@ -520,7 +567,7 @@ static void run_loss(const wd_loss_args* a, const LossPlan& p, char* ws, hipStre
     const void* x = (const T*)a->x + n0 * a->x_ld;
     int64_t x_ld = a->x_ld * 2;
     if (p.copy_x) {
-      lay<T>(x, a->x_ld, n, a->D, nullptr, ws + p.x, p.Dp, s);
+      lay<T>(x, a->x_ld, n, a->D, ws + p.x, p.Dp, s);
       x = ws + p.x, x_ld = p.Dp * 2;
     }
     LossArgs l{};
@@ -529,8 +576,10 @@ static void run_loss(const wd_loss_args* a, const LossPlan& p, char* ws, hipStre
     launch_loss<T>(l, size, s);
     float* loss = a->loss ? a->loss + n0 : nullptr;
     float2* stats = a->stats ? (float2*)a->stats + n0 : nullptr;
-    if (tiles <= 64)
+    if (tiles <= 8 || (tiles <= 64 && n >= 16384))
       hipLaunchKernelGGL((k_loss_join<4>), dim3((uint32_t)((n + 63) / 64)), dim3(256), 0, s, l.part, tiles, l.label_z, l.target, l.P, n, loss, stats);
+    else if (tiles <= 64)
+      hipLaunchKernelGGL((k_loss_join<16>), dim3((uint32_t)((n + 15) / 16)), dim3(256), 0, s, l.part, tiles, l.label_z, l.target, l.P, n, loss, stats);
     else
       hipLaunchKernelGGL((k_loss_join<64>), dim3((uint32_t)((n + 3) / 4)), dim3(256), 0, s, l.part, tiles, l.label_z, l.target, l.P, n, loss, stats);
   }
@@ -551,22 +600,26 @@ static void run_grads(const wd_loss_args* a, const LossPlan& p, char* ws, hipStr
     ProductArgs q{};
     q.M = P, q.C = (int)D, q.out = a->dweight, q.out_ld = a->dweight_ld;
     if (a->dweight) join(q, 0, nullptr, nullptr);
-    if (a->dbias) hipLaunchKernelGGL(k_loss_db, dim3((uint32_t)((P + 255) / 256)), dim3(256), 0, s, nullptr, 0, (int)P, nullptr, false, a->dbias);
+    if (a->dbias) hipLaunchKernelGGL(k_loss_db, dim3((uint32_t)((P + 255) / 256)), dim3(256), 0, s, DbArgs{nullptr, 0, (int)P, nullptr, false, a->dbias});
     return;
   }
   if (p.copy_w) {
-    lay<T>(a->weight, a->weight_ld, P, (int)D, nullptr, ws + p.w, p.Dp, s);
+    lay<T>(a->weight, a->weight_ld, P, (int)D, ws + p.w, p.Dp, s);
     w = ws + p.w, w_ld = p.Dp * 2;
   }
   if (__is_same(T, Half)) {
     power = (const float*)(ws + p.power);
     hipLaunchKernelGGL(k_power, dim3(1), dim3(1024), 0, s, a->grad, N, (float*)(ws + p.power));
   }
-  hipLaunchKernelGGL(k_row_info, dim3((uint32_t)((N + 255) / 256)), dim3(256), 0, s, (const float2*)a->stats, a->grad, a->target, (int32_t)P, N, power, info);
   float* sum = (float*)(ws + p.sum);
   for (int64_t n0 = 0; n0 < N; n0 += p.rows) {
     const int64_t n = std::min(p.rows, N - n0);
-    lay<T>((const T*)a->x + n0 * a->x_ld, a->x_ld, n, (int)D, info + n0, ws + p.x, p.Dp, s);
+    in_rows(n, p.Dp / 8, [&](int64_t r0, int64_t rows, dim3 grid) {
+      const int64_t at = n0 + r0;
+      const PrepareArgs prepare{(const T*)a->x + at * a->x_ld, a->x_ld, (uint32_t)rows, (int)D, (int)P, (const float2*)a->stats + at,
+                                a->grad ? a->grad + at : nullptr, a->target + at, power, info + at, (T*)(ws + p.x) + r0 * p.Dp, p.Dp};
+      hipLaunchKernelGGL((k_loss_prepare<T>), grid, dim3(256), 0, s, prepare);
+    });
     for (int64_t c0 = 0; c0 < P; c0 += p.cols) {
       const int64_t c = std::min(p.cols, P - c0);
       LossArgs l{};
@@ -575,14 +628,13 @@ static void run_grads(const wd_loss_args* a, const LossPlan& p, char* ws, hipStr
       l.db_part = a->dbias ? (float*)(ws + p.db) : nullptr;
       const int size = tile_size(n, l.dz_ld);
       launch_dz<T>(l, size, s);
-      if (a->dbias)
-        hipLaunchKernelGGL(k_loss_db, dim3((uint32_t)((c + 255) / 256)), dim3(256), 0, s, l.db_part, (int)((n + size - 1) / size), (int)c, power, n0 > 0,
-                           a->dbias + c0);
+      const DbArgs db{l.db_part, (int)((n + size - 1) / size), (int)c, power, n0 > 0, a->dbias + c0};
+      if (a->dbias && !a->dweight) hipLaunchKernelGGL(k_loss_db, dim3((uint32_t)((c + 255) / 256)), dim3(256), 0, s, db);
       if (a->dweight) {
         const Cut cut = cut_product(c, D, n);
         ProductArgs q{};
         q.x = l.dz, q.x_ld = l.dz_ld * 2, q.w = ws + p.x, q.w_ld = p.Dp * 2, q.M = c, q.C = (int)D, q.K = (int)n, q.k_each = cut.k_each;
-        q.part = (float*)(ws + p.split), q.part_ld = p.Dp, q.power = power, q.out_ld = a->dweight_ld;
+        q.part = (float*)(ws + p.split), q.part_ld = p.Dp, q.power = power, q.out_ld = a->dweight_ld, q.db = db;
         void* out = (T*)a->dweight + c0 * a->dweight_ld;
         const bool pieces = p.rows < N, last = n0 + p.rows >= N;
         q.out = !pieces && cut.splits == 1 ? out : nullptr;

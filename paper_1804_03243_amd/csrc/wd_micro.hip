@@ -172,6 +172,9 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_micro_tiles(MicroArgs a, ui
       o.xs[i] = *(const uint8_t*)(s + (wm + i * 16 + l) * 16);
     }
   };
+  // (read from memory at the tile's end it would be a round trip that nothing hides)
+  float* kept_bias = (float*)(lds + 2 * (kStep + kScaleStep));
+  for (int p = threadIdx.x; p < BN; p += 64 * kWaves_) kept_bias[p] = a.bias && p < outs ? a.bias[p0 + p] : 0.0f;
   f32x4 acc[TM][TN] = {};
   const auto products = [&](const Operands& o) {
 #pragma unroll
@@ -201,11 +204,9 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_micro_tiles(MicroArgs a, ui
     now = next;
     next = kStep - next;
   }
-  float bias[TN][4];
+  f32x4 bias[TN];
 #pragma unroll
-  for (int j = 0; j < TN; ++j)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) bias[j][e] = a.bias ? a.bias[min(p0 + wn + j * 16 + quad * 4 + e, a.P - 1)] : 0.0f;
+  for (int j = 0; j < TN; ++j) bias[j] = *(const f32x4*)(kept_bias + wn + j * 16 + quad * 4);
   __syncthreads();  // (every wavefront has read its last operands)
   store_tile<O, TM, TN>((O*)a.out + (n0 + wm) * a.out_ld + p0 + wn, a.out_ld, a.N - n0 - wm, a.P - p0 - wn, lds + wave * kStoreBytes<O, TN>,
                         [&](int i, int j, int e) { return acc[i][j][e] + bias[j][e]; }, a.stream);
@@ -313,8 +314,8 @@ template <class O, int BM, int BN, int WM, int WN>
 static void launch_micro_tiles(const MicroArgs& a, hipStream_t s) {
   const uint32_t rows = (uint32_t)((a.N + BM - 1) / BM), cols = ((uint32_t)a.P + BN - 1) / BN;
   auto* k = k_micro_tiles<O, BM, BN, WM, WN>;
-  constexpr int bytes = 2 * (BM + BN) * (128 + 16);
-  static_assert(kStoreBytes<O, BN / WN / 16> * WM * WN <= bytes, "");
+  constexpr int stages = 2 * (BM + BN) * (128 + 16), bytes = stages + BN * 4;
+  static_assert(kStoreBytes<O, BN / WN / 16> * WM * WN <= stages, "");
   static std::atomic<uint64_t> done{0};
   allow_lds((const void*)k, bytes, done);
   hipLaunchKernelGGL(k, dim3(rows * cols), dim3(64 * WM * WN), bytes, s, a, rows, cols);

@@ -861,6 +861,14 @@ def _enqueue(device, call):
 
 
 _TYPES = {}
+_HALF_TYPES = {}
+
+
+def _half_types(torch):
+    """The same of the 16-bit types."""
+    if not _HALF_TYPES:
+        _HALF_TYPES.update({t: v for t, v in _types(torch).items() if v != WD_F32})
+    return _HALF_TYPES
 
 
 def _types(torch):
@@ -1062,7 +1070,7 @@ def _workspace(torch, nbytes, device):
 def _loss_args(hidden, weight, target, bias):
     """The checked inputs of the loss as wd_loss_args."""
     torch = _torch()
-    types = {t: v for t, v in _types(torch).items() if v != WD_F32}
+    types = _half_types(torch)
     dev = weight.device
     _matrix(weight, types, dev, "weight")
     _matrix(hidden, (weight.dtype,), dev, "hidden")
@@ -1172,6 +1180,9 @@ def cross_entropy_grads(hidden, weight, target, bias=None, grad=None):
     return (loss, *_loss_grads(a, hidden, weight, bias, stats, grad, (True, True, True)))
 
 
+_CLIP_BYTES = {}  # workspace by number of tensors
+
+
 def clip_gradients(gradients, max_norm: float, out=None):
     """The norm over all values of the gradients (a 0-d float32 tensor), and the
     gradients times min(1, max_norm / norm): in place, or into `out`, as many
@@ -1204,9 +1215,14 @@ def clip_gradients(gradients, max_norm: float, out=None):
     if dev.type != "cuda":
         raise ValueError("gradients must be on a GPU")
     norm = torch.empty((), dtype=torch.float32, device=dev)
-    ws, p_ws = _workspace(torch, wd_clip_workspace_bytes(len(rows)), dev)
+    nbytes = _CLIP_BYTES.get(len(rows), -1)
+    if nbytes < 0:
+        nbytes = wd_clip_workspace_bytes(len(rows))
+        if len(_CLIP_BYTES) < 256:
+            _CLIP_BYTES[len(rows)] = nbytes
+    ws = torch.empty(nbytes, dtype=torch.uint8, device=dev)
     table = (wd_gradient * len(rows))(*rows)
-    _enqueue(dev, lambda stream: wd_clip_gradients(table, len(rows), max_norm, norm.data_ptr(), p_ws, ws.numel(), stream))
+    _enqueue(dev, lambda stream: wd_clip_gradients(table, len(rows), max_norm, norm.data_ptr(), ws.data_ptr(), nbytes, stream))
     return norm
 
 
