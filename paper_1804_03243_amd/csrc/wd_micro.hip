@@ -13,6 +13,7 @@
 // so the scales of 512 columns stand as [quarter q][product h], block 4 h + q at 4 q + h.
 // Columns past D are zeros, scales past the last block 0.
 #include <algorithm>
+#include <type_traits>
 
 #include "wd_host.h"
 #include "wd_tile.h"
@@ -119,8 +120,7 @@ struct MicroArgs {
 
 // Many rows: tiles of BM rows and BN outputs, as the 16-bit products go (Tile): a step is
 // 128 bytes of a row, here 256 columns, its halves 128.  The scales of two steps
-// come with the even one, 16 bytes of each row, into two places of their own.  A
-// wavefront reads a byte of scale per operand, so that its products all take byte 0.
+// come with the even one, 16 bytes of each row, into two places of their own.
 template <class O, int BM, int BN, int WM, int WN>
 __global__ void __launch_bounds__(64 * WM * WN, 2) k_micro_tiles(MicroArgs a, uint32_t row_tiles, uint32_t col_tiles) {
   constexpr int kWaves_ = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
@@ -157,33 +157,36 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_micro_tiles(MicroArgs a, ui
   };
   struct Operands {
     uint4 w[TN], x[TM];
-    int ws[TN], xs[TM];
   } even, odd;
-  const auto read = [&](int k0, int at, int half, Operands& o) {
-    const char* s = lds + kScales + (k0 / kStepK / 2 & 1) * kScaleStep + quad * 4 + (k0 / kStepK % 2 * 2 + half);
+  struct Scales {  // of a step: byte 0 its first half's, byte 1 its second's
+    int w[TN], x[TM];
+  } scale, next_scale;
+  const auto read = [&](int at, int half, Operands& o) {
 #pragma unroll
-    for (int j = 0; j < TN; ++j) {
-      o.w[j] = W::read(lds, lds0, at + X::kBytes, wn + j * 16, half);
-      o.ws[j] = *(const uint8_t*)(s + (BM + wn + j * 16 + l) * 16);
-    }
+    for (int j = 0; j < TN; ++j) o.w[j] = W::read(lds, lds0, at + X::kBytes, wn + j * 16, half);
 #pragma unroll
-    for (int i = 0; i < TM; ++i) {
-      o.x[i] = X::read(lds, lds0, at, wm + i * 16, half);
-      o.xs[i] = *(const uint8_t*)(s + (wm + i * 16 + l) * 16);
-    }
+    for (int i = 0; i < TM; ++i) o.x[i] = X::read(lds, lds0, at, wm + i * 16, half);
+  };
+  const auto read_scales = [&](int k0, Scales& s) {
+    const char* from = lds + kScales + (k0 / kStepK / 2 & 1) * kScaleStep + (wm + l) * 16 + quad * 4;
+    const int by = k0 / kStepK % 2 * 16;
+#pragma unroll
+    for (int j = 0; j < TN; ++j) s.w[j] = *(const int*)(from + (BM + wn - wm + j * 16) * 16) >> by;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) s.x[i] = *(const int*)(from + i * 256) >> by;
   };
   // (read from memory at the tile's end it would be a round trip that nothing hides)
   float* kept_bias = (float*)(lds + 2 * (kStep + kScaleStep));
   for (int p = threadIdx.x; p < BN; p += 64 * kWaves_) kept_bias[p] = a.bias && p < outs ? a.bias[p0 + p] : 0.0f;
   f32x4 acc[TM][TN] = {};
-  const auto products = [&](const Operands& o) {
+  const auto products = [&](const Operands& o, auto half) {
 #pragma unroll
     for (int i = 0; i < TM; ++i)
 #pragma unroll
-      for (int j = 0; j < TN; ++j) acc[i][j] = mfma4<0>(o.w[j], o.x[i], acc[i][j], o.ws[j], o.xs[i]);
+      for (int j = 0; j < TN; ++j) acc[i][j] = mfma4<half.value>(o.w[j], o.x[i], acc[i][j], scale.w[j], scale.x[i]);
 #pragma unroll
     for (int i = 0; i < TM + TN; ++i) {
-      __builtin_amdgcn_sched_group_barrier(0x100, 2, 0);
+      __builtin_amdgcn_sched_group_barrier(0x100, 1 + half.value, 0);
       __builtin_amdgcn_sched_group_barrier(0x008, TM * TN / (TM + TN), 0);
     }
   };
@@ -192,15 +195,18 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_micro_tiles(MicroArgs a, ui
   if (kStepK < K) stage(kStepK, next);
   loads_left<0>();
   __syncthreads();
-  read(0, now, 0, even);
+  read(now, 0, even);
+  read_scales(0, scale);
   for (int k0 = 0; k0 < K; k0 += kStepK) {
-    read(k0, now, 1, odd);
-    products(even);
+    read(now, 1, odd);
+    products(even, std::integral_constant<int, 0>{});
     loads_left<0>();
     __syncthreads();  // this step has been read, the next one is there
     if (k0 + 2 * kStepK < K) stage(k0 + 2 * kStepK, now);
-    read(k0 + kStepK, next, 0, even);
-    products(odd);
+    read(next, 0, even);
+    read_scales(k0 + kStepK, next_scale);
+    products(odd, std::integral_constant<int, 1>{});
+    scale = next_scale;
     now = next;
     next = kStep - next;
   }
