@@ -81,7 +81,7 @@ template <class T, int BM, int BN, int WM, int WN>
 __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2) k_loss(LossArgs a, uint32_t row_tiles, uint32_t col_tiles) {
   using Tl = Tile<T, BM, BN, WM, WN, false, false>;
   constexpr int TM = Tl::TM, TN = Tl::TN;
-  extern __shared__ __attribute__((aligned(16))) char lds[];
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
   uint32_t row_tile, col_tile;
   my_tile(row_tiles, col_tiles, row_tile, col_tile);
   const int64_t n0 = (int64_t)row_tile * BM;
@@ -240,7 +240,7 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
   using Tl = Tile<T, BM, BN, WM, WN, false, false>;
   constexpr int TM = Tl::TM, TN = Tl::TN;
   static_assert(kStoreBytes<T, TN> * WM * WN + WM * BN * 4 <= Tl::kBytes, "");
-  extern __shared__ __attribute__((aligned(16))) char lds[];
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
   uint32_t row_tile, col_tile;
   my_tile(row_tiles, col_tiles, row_tile, col_tile);
   const int64_t n0 = (int64_t)row_tile * BM;
@@ -332,7 +332,7 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
   using Tl = Tile<T, BM, BN, WM, WN, XKR, true>;
   constexpr int TM = Tl::TM, TN = Tl::TN;
   static_assert(kStoreBytes<F32, TN> * WM * WN <= Tl::kBytes, "");
-  extern __shared__ __attribute__((aligned(16))) char lds[];
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
   uint32_t row_tile, col_tile;
   my_tile(row_tiles, col_tiles, row_tile, col_tile);
   const int64_t m0 = (int64_t)row_tile * BM;

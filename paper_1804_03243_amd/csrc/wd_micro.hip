@@ -127,33 +127,33 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_micro_tiles(MicroArgs a, ui
   using X = Side<BM, false, kWaves_>;
   using W = Side<BN, false, kWaves_>;
   constexpr int kStep = (BM + BN) * 128, kScales = 2 * kStep, kScaleStep = (BM + BN) * 16;
-  extern __shared__ __attribute__((aligned(16))) char lds[];
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
   uint32_t row_tile, col_tile;
   my_tile(row_tiles, col_tiles, row_tile, col_tile);
   const int64_t n0 = (int64_t)row_tile * BM;
   const int p0 = (int)col_tile * BN;
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, l = lane & 15, quad = lane >> 4;
+  const int wave = wave_number(), lane = threadIdx.x & 63, l = lane & 15, quad = lane >> 4;
   const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
   const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
   const int64_t ld = (int64_t)a.blocks * 16;
   const int rows = (int)min<int64_t>(BM, a.N - n0), outs = min(BN, a.P - p0), K = a.blocks * 8;
   X x;
   W w;
-  x.init({a.x + n0 * ld, ld, rows});
-  w.init({a.w + (int64_t)p0 * ld, ld, outs});
+  x.init({a.x + n0 * ld, ld, rows}, wm, lds0);
+  w.init({a.w + (int64_t)p0 * ld, ld, outs}, wn, lds0 + X::kBytes);
   // (64 rows' scales to a load, the tile's rows and then its outputs)
   const int scale_row = wave * 64 + lane;
   const uint32_t scale_from = (uint32_t)((scale_row < BM ? min(scale_row, rows - 1) : min(scale_row - BM, outs - 1)) * a.sl);
   const auto stage = [&](int k0, int at) {
     if (k0 / kStepK % 2 == 0) {
-      const uint32_t to = __builtin_amdgcn_readfirstlane(lds0 + kScales + (k0 / kStepK / 2 & 1) * kScaleStep + wave * 1024);
+      const uint32_t to = lds0 + kScales + (k0 / kStepK / 2 & 1) * kScaleStep + wave * 1024;
       if (scale_row < BM)
         load_to_lds(a.xs + n0 * a.sl + k0 / kStepK / 2 * 16, scale_from, to);
       else if (scale_row < BM + BN)
         load_to_lds(a.ws + (int64_t)p0 * a.sl + k0 / kStepK / 2 * 16, scale_from, to);
     }
-    x.stage(k0, K, lds0 + at);
-    w.stage(k0, K, lds0 + at + X::kBytes);
+    x.stage(k0, K, at);
+    w.stage(k0, K, at);
   };
   struct Operands {
     uint4 w[TN], x[TM];
@@ -163,9 +163,9 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_micro_tiles(MicroArgs a, ui
   } scale, next_scale;
   const auto read = [&](int at, int half, Operands& o) {
 #pragma unroll
-    for (int j = 0; j < TN; ++j) o.w[j] = W::read(lds, lds0, at + X::kBytes, wn + j * 16, half);
+    for (int j = 0; j < TN; ++j) o.w[j] = w.rows(at, j, half);
 #pragma unroll
-    for (int i = 0; i < TM; ++i) o.x[i] = X::read(lds, lds0, at, wm + i * 16, half);
+    for (int i = 0; i < TM; ++i) o.x[i] = x.rows(at, i, half);
   };
   const auto read_scales = [&](int k0, Scales& s) {
     const char* from = lds + kScales + (k0 / kStepK / 2 & 1) * kScaleStep + (wm + l) * 16 + quad * 4;
@@ -226,7 +226,7 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_micro_tiles(MicroArgs a, ui
 constexpr int kFewRows = 8;
 template <class T, class O>
 __global__ void __launch_bounds__(256, 4) k_micro_few(MicroArgs a, const T* rows, int64_t ld, int D) {
-  extern __shared__ __attribute__((aligned(16))) char lds[];
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, l = lane & 15, quad = lane >> 4;
   const int p0 = (blockIdx.x * 4 + wave) * 16, N = (int)a.N;
   const int line = a.blocks | 1;

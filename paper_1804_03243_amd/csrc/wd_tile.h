@@ -38,6 +38,7 @@ __device__ __forceinline__ void load_to_lds(const void* base, uint32_t offset, u
   const uint64_t p = (uint64_t)base;  // (into scalar registers, where the compiler would not hold it there)
   base = (const void*)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(p >> 32)) << 32 |
                        (uint32_t)__builtin_amdgcn_readfirstlane((int)p));
+  to = (uint32_t)__builtin_amdgcn_readfirstlane((int)to);
   // (m0 is a register that the compiler keeps to itself, and warns of here; it holds no
   // value there across other code, and is named so that none of its uses is put around this)
 #pragma clang diagnostic push
@@ -106,7 +107,13 @@ __device__ __forceinline__ uint2 read_turned(uint32_t at) {
   return __builtin_bit_cast(uint2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(uintptr_t)at));
 }
 
-// The loads of one operand (of ROWS rows) by WAVES wavefronts, and its reads.
+// The wavefront's number, as a value that the compiler holds once for the wavefront.
+__device__ __forceinline__ int wave_number() { return __builtin_amdgcn_readfirstlane(threadIdx.x >> 6); }
+
+// The loads of one operand (of ROWS rows) by WAVES wavefronts, and a wavefront's reads of
+// blocks of 16 rows from its first one, r0, on (a multiple of the rows that it has).
+// Addresses are laid out so that a read costs an addition at most: blocks, halves and
+// places are constants of the instruction or one bit of the address.
 template <int ROWS, bool KR, int WAVES>
 struct Side {
   static constexpr int kBytes = ROWS * 128;              // of a step
@@ -116,10 +123,13 @@ struct Side {
   static_assert(kBytes % (1024 * WAVES) == 0, "");
   Operand o;
   uint32_t from[kParts];
+  uint32_t to;    // where the wavefront's first load goes
+  uint32_t read;  // where the lane's first read is
 
-  __device__ __forceinline__ void init(const Operand& op) {
+  __device__ __forceinline__ void init(const Operand& op, int r0, uint32_t lds) {
     o = op;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int wave = wave_number(), lane = threadIdx.x & 63, quad = lane >> 4, l = lane & 15;
+    to = lds + wave * 1024;
 #pragma unroll
     for (int i = 0; i < kParts; ++i) {
       const int line = (i * WAVES + wave) * kLines + lane / kChunks;
@@ -130,41 +140,42 @@ struct Side {
         from[i] = (uint32_t)(min(line, o.count - 1) * o.ld + ((lane % kChunks) ^ swizzle(line)) * 16);
       }
     }
+    if constexpr (KR) {
+      const int k = quad * 8 + (l >> 2);
+      read = lds + k * (ROWS * 2) + (((r0 / 8 | (l >> 1 & 1)) ^ turn<ROWS>(k)) << 4) + (l & 1) * 8;
+    } else {
+      read = lds + (r0 + l) * 128 + ((quad ^ swizzle(l)) << 4);
+    }
   }
-  // Starts the loads of shared columns k0.. of K (a multiple of eight by rows) to LDS at `to`.
-  __device__ __forceinline__ void stage(int k0, int K, uint32_t to) const {
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  // Starts the loads of shared columns k0.. of K (a multiple of eight by rows) to the step at `at`.
+  __device__ __forceinline__ void stage(int k0, int K, int at) const {
     const char* base = (const char*)o.p + (KR ? (int64_t)k0 * o.ld : (int64_t)k0 * 2);
     if (k0 + kStepK <= K) {
 #pragma unroll
-      for (int i = 0; i < kParts; ++i)
-        load_to_lds(base, from[i], __builtin_amdgcn_readfirstlane(to + (i * WAVES + wave) * 1024));
+      for (int i = 0; i < kParts; ++i) load_to_lds(base, from[i], to + at + i * WAVES * 1024);
     } else {  // the last ones, zeros behind them
+      const int lane = threadIdx.x & 63;
 #pragma unroll
       for (int i = 0; i < kParts; ++i) {
-        const uint32_t at = __builtin_amdgcn_readfirstlane(to + (i * WAVES + wave) * 1024);
-        const int line = (i * WAVES + wave) * kLines + lane / kChunks;
+        const int line = (i * WAVES + wave_number()) * kLines + lane / kChunks;
         const int k = k0 + (KR ? line : ((lane % kChunks) ^ swizzle(line)) * 8);
         if (k < K)
-          load_to_lds(base, from[i], at);
+          load_to_lds(base, from[i], to + at + i * WAVES * 1024);
         else
-          load_to_lds(k_zeros, 0, at);
+          load_to_lds(k_zeros, 0, to + at + i * WAVES * 1024);
       }
     }
   }
-  // The lane's eight columns of half h (0, 1) of a step at LDS `at`, of row r0 + lane % 16
-  // (r0 a multiple of 16).
-  static __device__ __forceinline__ uint4 read(const char* lds, uint32_t lds0, int at, int r0, int h) {
-    const int lane = threadIdx.x & 63, quad = lane >> 4, l = lane & 15;
+  // The lane's eight columns of half h (0, 1) of the step at `at`, of row r0 + i * 16 + lane % 16.
+  __device__ __forceinline__ uint4 rows(int at, int i, int h) const {
     if constexpr (KR) {
-      const int k = h * 32 + quad * 8 + (l >> 2);
-      const int c = r0 / 8 + (l >> 1 & 1);
-      const uint32_t p = lds0 + at + k * (ROWS * 2) + ((c ^ turn<ROWS>(k)) << 4) + (l & 1) * 8;
-      const uint32_t q = lds0 + at + (k + 4) * (ROWS * 2) + ((c ^ turn<ROWS>(k + 4)) << 4) + (l & 1) * 8;
-      const uint2 lo = read_turned(p), hi = read_turned(q);
+      const uint32_t p = (read ^ (i << 5)) + at + h * 32 * (ROWS * 2);
+      const uint2 lo = read_turned(p), hi = read_turned(p + 4 * (ROWS * 2));
       return make_uint4(lo.x, lo.y, hi.x, hi.y);
     } else {
-      return *(const uint4*)(lds + at + (r0 + l) * 128 + (((quad | h << 2) ^ swizzle(l)) << 4));
+      typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+      const u32x4 v = *(const __attribute__((address_space(3))) u32x4*)(uintptr_t)((read ^ (h << 6)) + at + i * 2048);
+      return make_uint4(v.x, v.y, v.z, v.w);
     }
   }
 };
@@ -186,25 +197,24 @@ struct Tile {
   using W = Side<BN, WKR, kWaves_>;
 
   static __device__ __forceinline__ void multiply(const Operand& xo, const Operand& wo, int K, char* lds, f32x4 (&acc)[TM][TN]) {
-    const int wave = threadIdx.x >> 6;
-    const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
+    const int wave = wave_number(), wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) char*)lds;
     X x;
     W w;
-    x.init(xo);
-    w.init(wo);
+    x.init(xo, wm, lds0);
+    w.init(wo, wn, lds0 + X::kBytes);
     const auto stage = [&](int k0, int at) {
-      x.stage(k0, K, lds0 + at);
-      w.stage(k0, K, lds0 + at + X::kBytes);
+      x.stage(k0, K, at);
+      w.stage(k0, K, at);
     };
     struct Operands {
       uint4 w[TN], x[TM];
     } even, odd;
     const auto read = [&](int at, int half, Operands& o) {
 #pragma unroll
-      for (int j = 0; j < TN; ++j) o.w[j] = W::read(lds, lds0, at + X::kBytes, wn + j * 16, half);
+      for (int j = 0; j < TN; ++j) o.w[j] = w.rows(at, j, half);
 #pragma unroll
-      for (int i = 0; i < TM; ++i) o.x[i] = X::read(lds, lds0, at, wm + i * 16, half);
+      for (int i = 0; i < TM; ++i) o.x[i] = x.rows(at, i, half);
     };
     const auto products = [&](const Operands& o) {
 #pragma unroll
