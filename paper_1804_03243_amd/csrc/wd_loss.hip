@@ -325,18 +325,19 @@ struct ProductArgs {
   const float* power;  // NULL: 1
   const RowInfo* info; // rows without a part in the gradients are zeros; NULL: none
   DbArgs db;           // dz^T x: the labels' db, by the workgroups of the first columns
+  uint32_t row_tiles, col_tiles, splits;
 };
 
 template <class T, int BM, int BN, int WM, int WN, bool XKR>
-__global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2) k_product(ProductArgs a, uint32_t row_tiles, uint32_t col_tiles) {
+__device__ __forceinline__ void product_tile(const ProductArgs& a, uint32_t number, char* lds) {
   using Tl = Tile<T, BM, BN, WM, WN, XKR, true>;
   constexpr int TM = Tl::TM, TN = Tl::TN;
   static_assert(kStoreBytes<F32, TN> * WM * WN <= Tl::kBytes, "");
-  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const uint32_t tiles = a.row_tiles * a.col_tiles, split = number / tiles;
   uint32_t row_tile, col_tile;
-  my_tile(row_tiles, col_tiles, row_tile, col_tile);
+  tile_at(number % tiles, a.row_tiles, a.col_tiles, row_tile, col_tile);
   const int64_t m0 = (int64_t)row_tile * BM;
-  const int c0 = (int)col_tile * BN, k0 = (int)blockIdx.y * a.k_each;
+  const int c0 = (int)col_tile * BN, k0 = (int)split * a.k_each;
   int* in = (int*)(lds + Tl::kBytes);  // [BM] whether the row has a part in the gradients
   if (a.out)
     for (int r = threadIdx.x; r < BM; r += 64 * WM * WN) in[r] = !a.info || a.info[min<int64_t>(m0 + r, a.M - 1)].label >= 0;
@@ -348,15 +349,28 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15;
   const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
   __syncthreads();  // (every wavefront has read its last operands)
-  if (XKR && a.db.part && col_tile == 0 && blockIdx.y == 0)
+  if (XKR && a.db.part && col_tile == 0 && split == 0)
     for (int r = threadIdx.x; r < BM; r += 64 * WM * WN) sum_db(a.db, m0 + r);
   if (a.out) {
     store_tile<T, TM, TN>((T*)a.out + (m0 + wm) * a.out_ld + c0 + wn, a.out_ld, a.M - m0 - wm, a.C - c0 - wn, lds + wave * kStoreBytes<T, TN>,
                           [&](int i, int j, int e) { return in[wm + i * 16 + col] ? acc[i][j][e] * by : 0.0f; });
   } else {
-    store_tile<F32, TM, TN>((F32*)a.part + ((int64_t)blockIdx.y * a.M + m0 + wm) * a.part_ld + c0 + wn, a.part_ld, a.M - m0 - wm, a.C - c0 - wn,
+    store_tile<F32, TM, TN>((F32*)a.part + ((int64_t)split * a.M + m0 + wm) * a.part_ld + c0 + wn, a.part_ld, a.M - m0 - wm, a.C - c0 - wn,
                             lds + wave * kStoreBytes<F32, TN>, [&](int i, int j, int e) { return acc[i][j][e]; });
   }
+}
+
+// Both products of a piece in one launch, so that one fills what the other leaves of the
+// chip: dz^T x, then dz W (either may have no workgroups), those with more steps first.
+template <class T, int B, int WM, int WN>
+__global__ void __launch_bounds__(64 * WM * WN, B * B / WM / WN > 8192 ? 1 : 2) k_products(ProductArgs dw, ProductArgs dx, bool dx_first) {
+  extern __shared__ __attribute__((aligned(1024))) char lds[];
+  const uint32_t of_dw = dw.row_tiles * dw.col_tiles * dw.splits, of_dx = dx.row_tiles * dx.col_tiles * dx.splits;
+  const uint32_t number = blockIdx.x, first = dx_first ? of_dx : of_dw;
+  if ((number < first) != dx_first)
+    product_tile<T, B, B, WM, WN, true>(dw, dx_first ? number - first : number, lds);
+  else
+    product_tile<T, B, B, WM, WN, false>(dx, dx_first ? number : number - first, lds);
 }
 
 // The splits' sums in their order, behind those of earlier pieces (`sum`, in 32 bits), to
@@ -425,42 +439,77 @@ static void launch_dz(const LossArgs& a, int size, hipStream_t s) {
   WD_TILES(size, WD_CALL)
 #undef WD_CALL
 }
-template <class T, bool XKR>
-static void launch_product(const ProductArgs& a, int size, int splits, hipStream_t s) {
-#define WD_CALL(B, WM, WN)                                                                                                      \
-  static std::atomic<uint64_t> done{0};                                                                                         \
-  launch_tile(k_product<T, B, B, WM, WN, XKR>, Tile<T, B, B, WM, WN, XKR, true>::kBytes + B * 4, done, 64 * WM * WN, B, a.M, a.C, splits, s, a)
-  WD_TILES(size, WD_CALL)
-#undef WD_CALL
+template <class T, int B, int WM, int WN>
+static void launch_products_of(ProductArgs dw, ProductArgs dx, hipStream_t s) {
+  uint32_t groups = 0;
+  for (ProductArgs* q : {&dw, &dx}) {
+    q->row_tiles = (uint32_t)((q->M + B - 1) / B), q->col_tiles = (uint32_t)((q->C + B - 1) / B);
+    groups += q->row_tiles * q->col_tiles * q->splits;
+  }
+  auto* k = k_products<T, B, WM, WN>;
+  constexpr int bytes = Tile<T, B, B, WM, WN, true, true>::kBytes + B * 4;
+  static std::atomic<uint64_t> done{0};
+  allow_lds((const void*)k, bytes, done);
+  hipLaunchKernelGGL(k, dim3(groups), dim3(64 * WM * WN), bytes, s, dw, dx, dx.k_each > dw.k_each);
+}
+// A product with no splits is not wanted.
+template <class T>
+static void launch_products(const ProductArgs& dw, const ProductArgs& dx, int size, hipStream_t s) {
+  if (size == kLarge)
+    launch_products_of<T, 256, 2, 4>(dw, dx, s);
+  else if (size == kMiddle)
+    launch_products_of<T, 128, 2, 2>(dw, dx, s);
+  else
+    launch_products_of<T, 64, 2, 2>(dw, dx, s);
 }
 
-// How a product is cut: its tiles' size, and splits of its shared columns for small outputs
-// (which cost 32-bit sums in memory and a launch).  By the time that each way would take:
-// us of a step, of a lone workgroup to a full chip; rounds of workgroups; the sums' bytes at
-// 6 TB/s and 3 us for the launch that joins them.  (Whole calls of one gradient, bfloat16:
-// dz W of 2048 x 1024 over 6000 labels in tiles of 128 80 us in four splits and 101 in one, of 256
-// 83 in six, of 64 88; dz^T x of 6000 x 1024 over 2048 rows 74 in tiles of 128, 88 of 256, 84
-// in two splits of them; dz W of 4096 x 1024 over 20000 347 in four splits of 256, 582 in one, 387
-// in one of 128; of 777 x 1000 over 3001 39 in three splits of 64, 48 in one.)
+// How the products of a piece are cut: their tiles' size, and splits of their shared
+// columns for small outputs (which cost 32-bit sums in memory and a launch).  By the time
+// that each way would take: us of a step, of a lone workgroup to a full chip; rounds of
+// workgroups; the sums' bytes at 6 TB/s and 3 us for the launch that joins them.  (Whole calls
+// of one gradient, bfloat16: dz W of 2048 x 1024 over 6000 labels in tiles of 128 80 us in four
+// splits and 101 in one, of 256 83 in six, of 64 88; dz^T x of 6000 x 1024 over 2048 rows 74 in tiles
+// of 128, 88 of 256, 84 in two splits of them; dz W of 4096 x 1024 over 20000 347 in four splits of
+// 256, 582 in one, 387 in one of 128; of 777 x 1000 over 3001 39 in three splits of 64, 48 in one.)
 struct Cut {
-  int size, splits, k_each;
+  int size;
+  int splits[2], k_each[2];  // of dz^T x (labels x D over the rows) and dz W (rows x D over the labels); 0: not wanted
 };
-static Cut cut_product(int64_t M, int64_t C, int64_t K) {
+static Cut cut_products(int64_t rows, int64_t labels, int64_t D, bool dw, bool dx) {
   static constexpr struct {
     int size, slots;
     double lone, full;
   } kinds[] = {{256, 256, 1.8, 1.8}, {128, 512, 0.8, 1.0}, {64, 1024, 0.5, 0.9}};
-  const int64_t steps = (K + kStepK - 1) / kStepK;
+  const int64_t M[2] = {dw ? labels : 0, dx ? rows : 0}, steps[2] = {(rows + kStepK - 1) / kStepK, (labels + kStepK - 1) / kStepK};
   Cut best{};
   double least = INFINITY;
   for (const auto& k : kinds) {
-    for (int64_t splits = 1; splits <= 32 && (splits == 1 || steps / splits >= 4); ++splits) {
-      const int64_t each = (steps + splits - 1) / splits, parts = (steps + each - 1) / each;
-      const double rounds = (double)(tiles_of(M, C, k.size) * parts) / k.slots;
-      const double busy = rounds <= 1 ? 1 : (rounds + std::ceil(rounds)) / 2;
-      const double us = busy * each * (k.lone + (k.full - k.lone) * std::min(rounds, 1.0)) +
-                        (parts > 1 ? 3 + (double)M * C * 4 * (2 * parts + 0.5) / 6e6 : 0.0);
-      if (us < least) least = us, best = {k.size, (int)parts, (int)(each * kStepK)};
+    const int64_t tiles[2] = {tiles_of(M[0], D, k.size), tiles_of(M[1], D, k.size)};
+    const auto more = [&](int i, int64_t s) {  // whether s splits are worth a look
+      return s <= 1 || (s <= 32 && tiles[i] * s <= 2 * k.slots && steps[i] / s >= 4);
+    };
+    for (int64_t s0 = M[0] ? 1 : 0; s0 == 0 || more(0, s0); s0 += s0 < 4 ? 1 : s0 / 4) {
+      for (int64_t s1 = M[1] ? 1 : 0; s1 == 0 || more(1, s1); s1 += s1 < 4 ? 1 : s1 / 4) {
+        const int64_t s[2] = {s0, s1};
+        int64_t groups = 0, work = 0, longest = 0, each[2] = {}, parts[2] = {};
+        double joins = 0.0;
+        for (int i = 0; i < 2; ++i) {
+          if (!M[i]) continue;
+          each[i] = (steps[i] + s[i] - 1) / s[i], parts[i] = (steps[i] + each[i] - 1) / each[i];
+          groups += tiles[i] * parts[i], work += tiles[i] * parts[i] * each[i], longest = std::max(longest, each[i]);
+          if (parts[i] > 1) joins += 3 + (double)M[i] * D * 4 * (2 * parts[i] + 0.5) / 6e6;
+        }
+        const double rounds = (double)groups / k.slots;
+        const double busy = rounds <= 1 ? (double)longest : std::max((double)longest, work / (double)k.slots * (1 + std::ceil(rounds) / rounds) / 2);
+        const double us = busy * (k.lone + (k.full - k.lone) * std::min(rounds, 1.0)) + joins;
+        if (us < least) {
+          least = us;
+          best.size = k.size;
+          for (int i = 0; i < 2; ++i) best.splits[i] = (int)parts[i], best.k_each[i] = (int)(each[i] * kStepK);
+        }
+        if (s1 == 0) break;
+      }
+      if (s0 == 0) break;
     }
   }
   return best;
@@ -480,6 +529,13 @@ struct LossPlan {
 constexpr int64_t kPieceBytes = 512ll << 20;
 
 static bool rows_fit(const void* p, int64_t ld, int64_t rows) { return !((uintptr_t)p & 15) && (ld % 8 == 0 || rows == 1) && ld < (1 << 22); }
+
+// Of the sums of product i (M rows) of a piece, which are needed for splits and for pieces: of the rows
+// (i = 0), of the labels (1).
+static uint64_t split_bytes(const LossPlan& p, const Cut& cut, int i, int64_t M, int64_t all) {
+  const bool pieces = (i == 0 ? p.rows : p.cols) < all;
+  return cut.splits[i] > 1 || (cut.splits[i] && pieces) ? (uint64_t)cut.splits[i] * M * p.Dp * 4 : 0;
+}
 
 static LossPlan plan_loss(const wd_loss_args* a, bool grads) {
   LossPlan p{};
@@ -525,9 +581,8 @@ static LossPlan plan_loss(const wd_loss_args* a, bool grads) {
       for (int64_t c : {p.cols, (P - 1) % p.cols + 1}) {
         const int size = tile_size(n, align_up(c, 64));
         db = std::max(db, (uint64_t)((n + size - 1) / size) * c * 4);
-        const Cut cx = cut_product(n, D, c), cw = cut_product(c, D, n);
-        if (a->dx && (cx.splits > 1 || p.cols < P)) split = std::max(split, (uint64_t)cx.splits * n * p.Dp * 4);
-        if (a->dweight && (cw.splits > 1 || p.rows < N)) split = std::max(split, (uint64_t)cw.splits * c * p.Dp * 4);
+        const Cut cut = cut_products(n, c, D, a->dweight, a->dx);
+        split = std::max(split, split_bytes(p, cut, 0, c, N) + split_bytes(p, cut, 1, n, P));
       }
     p.db = take(db);
     p.split = take(split);
@@ -630,33 +685,26 @@ static void run_grads(const wd_loss_args* a, const LossPlan& p, char* ws, hipStr
       launch_dz<T>(l, size, s);
       const DbArgs db{l.db_part, (int)((n + size - 1) / size), (int)c, power, n0 > 0, a->dbias + c0};
       if (a->dbias && !a->dweight) hipLaunchKernelGGL(k_loss_db, dim3((uint32_t)((c + 255) / 256)), dim3(256), 0, s, db);
-      if (a->dweight) {
-        const Cut cut = cut_product(c, D, n);
-        ProductArgs q{};
-        q.x = l.dz, q.x_ld = l.dz_ld * 2, q.w = ws + p.x, q.w_ld = p.Dp * 2, q.M = c, q.C = (int)D, q.K = (int)n, q.k_each = cut.k_each;
-        q.part = (float*)(ws + p.split), q.part_ld = p.Dp, q.power = power, q.out_ld = a->dweight_ld, q.db = db;
-        void* out = (T*)a->dweight + c0 * a->dweight_ld;
-        const bool pieces = p.rows < N, last = n0 + p.rows >= N;
-        q.out = !pieces && cut.splits == 1 ? out : nullptr;
-        launch_product<T, true>(q, cut.size, cut.splits, s);
-        if (!q.out) {
-          q.out = last ? out : nullptr;
-          join(q, cut.splits, n0 > 0 ? sum : nullptr, sum);
-        }
+      if (!a->dweight && !a->dx) continue;
+      const Cut cut = cut_products(n, c, D, a->dweight, a->dx);
+      ProductArgs dw{}, dx{};
+      dw.x = l.dz, dw.x_ld = l.dz_ld * 2, dw.w = ws + p.x, dw.w_ld = p.Dp * 2, dw.M = c, dw.C = (int)D, dw.K = (int)n, dw.k_each = cut.k_each[0];
+      dw.part = (float*)(ws + p.split), dw.part_ld = p.Dp, dw.power = power, dw.out_ld = a->dweight_ld, dw.db = db, dw.splits = cut.splits[0];
+      dx.x = l.dz, dx.x_ld = l.dz_ld * 2, dx.w = l.w, dx.w_ld = w_ld, dx.M = n, dx.C = (int)D, dx.K = (int)c, dx.k_each = cut.k_each[1];
+      dx.part = (float*)(ws + p.split + split_bytes(p, cut, 0, c, N)), dx.part_ld = p.Dp, dx.power = power, dx.info = info + n0, dx.out_ld = a->dx_ld;
+      dx.splits = cut.splits[1];
+      void *out_w = (T*)a->dweight + c0 * a->dweight_ld, *out_x = (T*)a->dx + n0 * a->dx_ld;
+      const bool sums_w = p.rows < N || dw.splits > 1, sums_x = p.cols < P || dx.splits > 1;  // (through 32-bit sums)
+      if (!sums_w) dw.out = out_w;
+      if (!sums_x) dx.out = out_x;
+      launch_products<T>(dw, dx, cut.size, s);
+      if (a->dweight && sums_w) {
+        if (n0 + p.rows >= N) dw.out = out_w;
+        join(dw, (int)dw.splits, n0 > 0 ? sum : nullptr, sum);
       }
-      if (a->dx) {
-        const Cut cut = cut_product(n, D, c);
-        ProductArgs q{};
-        q.x = l.dz, q.x_ld = l.dz_ld * 2, q.w = l.w, q.w_ld = w_ld, q.M = n, q.C = (int)D, q.K = (int)c, q.k_each = cut.k_each;
-        q.part = (float*)(ws + p.split), q.part_ld = p.Dp, q.power = power, q.info = info + n0, q.out_ld = a->dx_ld;
-        void* out = (T*)a->dx + n0 * a->dx_ld;
-        const bool pieces = p.cols < P, last = c0 + p.cols >= P;
-        q.out = !pieces && cut.splits == 1 ? out : nullptr;
-        launch_product<T, false>(q, cut.size, cut.splits, s);
-        if (!q.out) {
-          q.out = last ? out : nullptr;
-          join(q, cut.splits, c0 > 0 ? sum : nullptr, sum);
-        }
+      if (a->dx && sums_x) {
+        if (c0 + p.cols >= P) dx.out = out_x;
+        join(dx, (int)dx.splits, c0 > 0 ? sum : nullptr, sum);
       }
     }
   }

@@ -59,18 +59,19 @@ constexpr int kStepK = 64;  // columns of a step: 128 bytes of a row
 // 16 rows of an operand read fall on different banks.
 __device__ __forceinline__ int swizzle(int row) { return (row >> 1) & 7; }
 
-// The tile of this workgroup.  Workgroups go round the eight XCDs, each with an
+// The tile of a workgroup by its number.  Workgroups go round the eight XCDs, each with an
 // L2 of its own: an XCD takes a run of tiles, in groups of kGroup rows of tiles
 // column by column, so that its workgroups share rows of x and of W.
 constexpr uint32_t kGroup = 8;
-__device__ __forceinline__ void my_tile(uint32_t rows, uint32_t cols, uint32_t& row, uint32_t& col) {
-  const uint32_t all = rows * cols, xcd = blockIdx.x % 8, q = all / 8, r = all % 8;
-  const uint32_t at = xcd * q + min(xcd, r) + blockIdx.x / 8;
+__device__ __forceinline__ void tile_at(uint32_t number, uint32_t rows, uint32_t cols, uint32_t& row, uint32_t& col) {
+  const uint32_t all = rows * cols, xcd = number % 8, q = all / 8, r = all % 8;
+  const uint32_t at = xcd * q + min(xcd, r) + number / 8;
   const uint32_t group = at / (kGroup * cols), first = group * kGroup, height = min(kGroup, rows - first);
   const uint32_t in = at - first * cols;
   col = in / height;
   row = first + in % height;
 }
+__device__ __forceinline__ void my_tile(uint32_t rows, uint32_t cols, uint32_t& row, uint32_t& col) { tile_at(blockIdx.x, rows, cols, row, col); }
 
 // Zeros to load where a matrix has ended.
 static __device__ const uint4 k_zeros[kStepK / 8] = {};
