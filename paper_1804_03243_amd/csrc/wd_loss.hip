@@ -160,26 +160,34 @@ __global__ void __launch_bounds__(256) k_loss_join(const float2* part, int tiles
   if (loss) loss[n] = t < 0 || t >= P ? 0.0f : v.y == 0.0f ? INFINITY : (v.x - label_z[n]) + logf(v.y);
 }
 
-// The power of two of the gradients (half precision), and its reciprocal.
-__global__ void __launch_bounds__(1024) k_power(const float* g, int64_t N, float* power) {
-  __shared__ float tops[16];
+// The power of two of the gradients (half precision) by THREADS threads, in each of them.
+template <int THREADS>
+__device__ __forceinline__ float power_of(const float* g, int64_t N, float* tops) {
   float top = g ? 0.0f : 1.0f;
-  for (int64_t n = threadIdx.x; g && n < N; n += 1024) top = fmaxf(top, fabsf(g[n]) < INFINITY ? fabsf(g[n]) : 0.0f);
+  for (int64_t n = threadIdx.x; g && n < N; n += THREADS) top = fmaxf(top, fabsf(g[n]) < INFINITY ? fabsf(g[n]) : 0.0f);
   for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o));
   if ((threadIdx.x & 63) == 0) tops[threadIdx.x >> 6] = top;
   __syncthreads();
-  if (threadIdx.x != 0) return;
-  for (int k = 1; k < 16; ++k) top = fmaxf(top, tops[k]);
+#pragma unroll
+  for (int k = 0; k < THREADS / 64; ++k) top = fmaxf(top, tops[k]);
   const int e = max(-100, min(100, 14 - ((int)(__float_as_uint(top) >> 23) - 127)));
-  power[0] = __uint_as_float((uint32_t)(127 + (top > 0.0f ? e : 0)) << 23);
-  power[1] = 1.0f / power[0];
+  return __uint_as_float((uint32_t)(127 + (top > 0.0f ? e : 0)) << 23);
+}
+// It and its reciprocal, where a launch for it costs less than every workgroup of the next
+// one forming it.  (Up to kFewPowers rows these do: 777 rows 62.5 us in all with a launch, 61.6
+// without.)
+constexpr int64_t kFewPowers = 4096;
+__global__ void __launch_bounds__(1024) k_power(const float* g, int64_t N, float* power) {
+  __shared__ float tops[16];
+  const float p = power_of<1024>(g, N, tops);
+  if (threadIdx.x == 0) power[0] = p, power[1] = 1.0f / p;
 }
 
 // What the gradients need of a row.
-__device__ __forceinline__ RowInfo row_info(const float2* stats, const float* g, const int32_t* target, int32_t P, const float* power, int64_t n) {
+__device__ __forceinline__ RowInfo row_info(const float2* stats, const float* g, const int32_t* target, int32_t P, float power, int64_t n) {
   const float2 s = stats[n];
   const int t = target[n];
-  const float gn = (g ? g[n] : 1.0f) * (power ? power[0] : 1.0f);
+  const float gn = (g ? g[n] : 1.0f) * power;
   // (a row without a finite logit has no softmax)
   const bool in = t >= 0 && t < P && gn != 0.0f && !(s.x == -INFINITY && s.y == 0.0f);
   return in ? RowInfo{s.x, gn / s.y, gn, t} : RowInfo{0.0f, 0.0f, 0.0f, -1};
@@ -217,18 +225,28 @@ struct PrepareArgs {
   const float2* stats;
   const float* g;
   const int32_t* target;
-  const float* power;
+  float* power;        // the power of two and its reciprocal; NULL: 1
+  const float* all_g;  // form it first, of all_N rows' g (NULL: of ones); all_N = 0: it is there
+  int64_t all_N;
   RowInfo* info;
   void* to;
   int64_t to_ld;
 };
 template <class T>
 __global__ void __launch_bounds__(256) k_loss_prepare(PrepareArgs a) {
+  __shared__ float tops[4];
+  float power = 1.0f;
+  if (a.all_N) {
+    power = power_of<256>(a.all_g, a.all_N, tops);
+    if (blockIdx.x == 0 && threadIdx.x == 0) a.power[0] = power, a.power[1] = 1.0f / power;
+  } else if (a.power) {
+    power = a.power[0];
+  }
   const uint32_t per = (uint32_t)(a.to_ld / 8);
   for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < a.N * per; i += gridDim.x * 256) {
     const int64_t n = i / per;
     const int k = (int)(i % per) * 8;
-    const RowInfo r = row_info(a.stats, a.g, a.target, a.P, a.power, n);
+    const RowInfo r = row_info(a.stats, a.g, a.target, a.P, power, n);
     const Few<T, 8> v = load_few((const T*)a.x + n * a.x_ld, k, a.D);
     if (k == 0) a.info[n] = r;
     *(uint4*)((T*)a.to + n * a.to_ld + k) = r.label >= 0 ? __builtin_bit_cast(uint4, v) : make_uint4(0, 0, 0, 0);
@@ -645,7 +663,7 @@ static void run_grads(const wd_loss_args* a, const LossPlan& p, char* ws, hipStr
   const int64_t N = a->N, P = a->P, D = a->D;
   const void* w = a->weight;
   int64_t w_ld = a->weight_ld * 2;
-  const float* power = nullptr;
+  float* power = nullptr;
   RowInfo* info = (RowInfo*)(ws + p.info);
   const auto join = [&](ProductArgs q, int splits, const float* before, float* sum) {
     const uint64_t blocks = ((uint64_t)q.M * ((q.C + 3) / 4) + 255) / 256;
@@ -662,9 +680,10 @@ static void run_grads(const wd_loss_args* a, const LossPlan& p, char* ws, hipStr
     lay<T>(a->weight, a->weight_ld, P, (int)D, ws + p.w, p.Dp, s);
     w = ws + p.w, w_ld = p.Dp * 2;
   }
+  const bool own_power = __is_same(T, Half) && N <= kFewPowers;
   if (__is_same(T, Half)) {
-    power = (const float*)(ws + p.power);
-    hipLaunchKernelGGL(k_power, dim3(1), dim3(1024), 0, s, a->grad, N, (float*)(ws + p.power));
+    power = (float*)(ws + p.power);
+    if (!own_power) hipLaunchKernelGGL(k_power, dim3(1), dim3(1024), 0, s, a->grad, N, power);
   }
   float* sum = (float*)(ws + p.sum);
   for (int64_t n0 = 0; n0 < N; n0 += p.rows) {
@@ -672,7 +691,7 @@ static void run_grads(const wd_loss_args* a, const LossPlan& p, char* ws, hipStr
     in_rows(n, p.Dp / 8, [&](int64_t r0, int64_t rows, dim3 grid) {
       const int64_t at = n0 + r0;
       const PrepareArgs prepare{(const T*)a->x + at * a->x_ld, a->x_ld, (uint32_t)rows, (int)D, (int)P, (const float2*)a->stats + at,
-                                a->grad ? a->grad + at : nullptr, a->target + at, power, info + at, (T*)(ws + p.x) + r0 * p.Dp, p.Dp};
+                                a->grad ? a->grad + at : nullptr, a->target + at, power, a->grad, own_power ? N : 0, info + at, (T*)(ws + p.x) + r0 * p.Dp, p.Dp};
       hipLaunchKernelGGL((k_loss_prepare<T>), grid, dim3(256), 0, s, prepare);
     });
     for (int64_t c0 = 0; c0 < P; c0 += p.cols) {
