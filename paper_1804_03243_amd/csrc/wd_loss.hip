@@ -14,8 +14,9 @@
 // twice costs 2 N D P operations of 8, keeping them would cost N P values of memory.
 //
 // What is rounded: dz to 16 bits, as matrix instructions take it; half a step of the
-// type, relative to each value, as large as the rounding of the gradients themselves,
-// whose sums run in 32 bits.  Half precision has dz times a power of two that takes the
+// type, relative to each value, as large as the rounding of the gradients themselves (over
+// many rows they are 1.4 times as far from 64 bits as exact ones rounded), whose sums run
+// in 32 bits.  Up to 64 rows dz has two terms (kCarefulRows).  Half precision has dz times a power of two that takes the
 // largest |g| to [2^14, 2^15), so that what is 2^29 times smaller than the largest
 // keeps its bits.  db sums the 32-bit values.
 #include <algorithm>
@@ -48,6 +49,7 @@ struct LossArgs {
   const RowInfo* info;    // gradients: of the launch's rows
   int32_t p_first;    // gradients: the first output's label
   void* dz;           // gradients: [N][dz_ld], zeros from P on
+  void* rest;         // gradients: dz's second term, what the rounding left, as dz
   int64_t dz_ld;      // in elements, a multiple of 64
   float* db_part;     // gradients: [row tile][P]; NULL: not wanted
 };
@@ -77,9 +79,9 @@ __device__ __forceinline__ void read_bias(const float* kept, float (&bias)[TN][4
   }
 }
 
-template <class T, int BM, int BN, int WM, int WN>
+template <class T, int BM, int BN, int WM, int WN, bool EXACT>
 __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2) k_loss(LossArgs a, uint32_t row_tiles, uint32_t col_tiles) {
-  using Tl = Tile<T, BM, BN, WM, WN, false, false>;
+  using Tl = Tile<T, BM, BN, WM, WN, false, false, EXACT>;
   constexpr int TM = Tl::TM, TN = Tl::TN;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   uint32_t row_tile, col_tile;
@@ -230,6 +232,7 @@ struct PrepareArgs {
   int64_t all_N;
   RowInfo* info;
   void* to;
+  void* again;         // the rows once more; NULL: not wanted
   int64_t to_ld;
 };
 template <class T>
@@ -249,13 +252,15 @@ __global__ void __launch_bounds__(256) k_loss_prepare(PrepareArgs a) {
     const RowInfo r = row_info(a.stats, a.g, a.target, a.P, power, n);
     const Few<T, 8> v = load_few((const T*)a.x + n * a.x_ld, k, a.D);
     if (k == 0) a.info[n] = r;
-    *(uint4*)((T*)a.to + n * a.to_ld + k) = r.label >= 0 ? __builtin_bit_cast(uint4, v) : make_uint4(0, 0, 0, 0);
+    const uint4 w = r.label >= 0 ? __builtin_bit_cast(uint4, v) : make_uint4(0, 0, 0, 0);
+    *(uint4*)((T*)a.to + n * a.to_ld + k) = w;
+    if (a.again) *(uint4*)((T*)a.again + n * a.to_ld + k) = w;
   }
 }
 
-template <class T, int BM, int BN, int WM, int WN>
+template <class T, int BM, int BN, int WM, int WN, bool EXACT>
 __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2) k_loss_dz(LossArgs a, uint32_t row_tiles, uint32_t col_tiles) {
-  using Tl = Tile<T, BM, BN, WM, WN, false, false>;
+  using Tl = Tile<T, BM, BN, WM, WN, false, false, EXACT>;
   constexpr int TM = Tl::TM, TN = Tl::TN;
   static_assert(kStoreBytes<T, TN> * WM * WN + WM * BN * 4 <= Tl::kBytes, "");
   extern __shared__ __attribute__((aligned(1024))) char lds[];
@@ -289,8 +294,15 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
                           v = r.label >= 0 ? v : 0.0f;  // (a row left out may have infinite logits)
                           if (t == j * 16 + e) v -= r.g;
                           db[j][e] += v;
+                          acc[i][j][e] = v;
                           return v;
                         });
+  if constexpr (EXACT)  // (with two terms)
+    store_tile<T, TM, TN>((T*)a.rest + (n0 + wm) * a.dz_ld + p0 + wn, a.dz_ld, a.N - n0 - wm, a.dz_ld - p0 - wn, lds + wave * kStoreBytes<T, TN>,
+                          [&](int i, int j, int e) {
+                            const float v = acc[i][j][e] - T::of(acc[i][j][e]).f();
+                            return fabsf(v) < INFINITY ? v : 0.0f;
+                          });
   if (!a.db_part) return;
   float* sums = (float*)(lds + kStoreBytes<T, TN> * WM * WN);  // [WM][BN]
 #pragma unroll
@@ -417,11 +429,21 @@ __global__ void __launch_bounds__(256) k_product_join(ProductArgs a, int splits,
 
 // ------------------------------------------------------------------ host
 
+// A few rows' gradients have few roundings that could even out (one row's dW is off by the
+// rounding of its label's dz alone, up to 2^-8 in bfloat16), and their losses hang on a few
+// sums: dz is held in two terms there, whose rows stand behind each other (so do the rows of
+// x, twice the same), and the logits are summed with EXACT.  Their time is
+// launches and the weights' way through the chip: losses of 16 rows of 1024 to 6000 labels 13.0 us
+// plainly and 14.6 so (18.6 with each step added by itself), their gradients 47.6 and 53.2.  Errors against 64 bits of 3
+// rows to 6000, plainly and so: loss 5.7e-7 and 2.1e-7, dx 2.3e-3 and 1.6e-3 (the rounding of
+// exact gradients: 1.6e-3).
+constexpr int64_t kCarefulRows = 64;
+
 // Tiles: the largest that gives every compute unit one (256, 192 of the middle ones).
 enum TileSize { kSmall = 64, kMiddle = 128, kLarge = 256 };
 static int64_t tiles_of(int64_t M, int64_t C, int size) { return ((M + size - 1) / size) * ((C + size - 1) / size); }
 static TileSize tile_size(int64_t M, int64_t C) {
-  return tiles_of(M, C, 256) >= 256 ? kLarge : tiles_of(M, C, 128) >= 192 ? kMiddle : kSmall;
+  return M <= kCarefulRows ? kSmall : tiles_of(M, C, 256) >= 256 ? kLarge : tiles_of(M, C, 128) >= 192 ? kMiddle : kSmall;
 }
 
 template <class K, class A>
@@ -443,17 +465,27 @@ static void launch_tile(K* kernel, int bytes, std::atomic<uint64_t>& done, int t
 
 template <class T>
 static void launch_loss(const LossArgs& a, int size, hipStream_t s) {
+  if (a.N <= kCarefulRows) {
+    static std::atomic<uint64_t> done{0};
+    launch_tile(k_loss<T, 64, 64, 2, 2, true>, Tile<T, 64, 64, 2, 2, false, false>::kBytes + 64 * 8, done, 256, 64, a.N, a.P, 1, s, a);
+    return;
+  }
 #define WD_CALL(B, WM, WN)                                                                                                      \
   static std::atomic<uint64_t> done{0};                                                                                         \
-  launch_tile(k_loss<T, B, B, WM, WN>, Tile<T, B, B, WM, WN, false, false>::kBytes + B * 8, done, 64 * WM * WN, B, a.N, a.P, 1, s, a)
+  launch_tile(k_loss<T, B, B, WM, WN, false>, Tile<T, B, B, WM, WN, false, false>::kBytes + B * 8, done, 64 * WM * WN, B, a.N, a.P, 1, s, a)
   WD_TILES(size, WD_CALL)
 #undef WD_CALL
 }
 template <class T>
 static void launch_dz(const LossArgs& a, int size, hipStream_t s) {
+  if (a.N <= kCarefulRows) {
+    static std::atomic<uint64_t> done{0};
+    launch_tile(k_loss_dz<T, 64, 64, 2, 2, true>, Tile<T, 64, 64, 2, 2, false, false>::kBytes + 64 * 20, done, 256, 64, a.N, a.dz_ld, 1, s, a);
+    return;
+  }
 #define WD_CALL(B, WM, WN)                                                                                                      \
   static std::atomic<uint64_t> done{0};                                                                                         \
-  launch_tile(k_loss_dz<T, B, B, WM, WN>, Tile<T, B, B, WM, WN, false, false>::kBytes + B * 20, done, 64 * WM * WN, B, a.N, a.dz_ld, 1, s, a)
+  launch_tile(k_loss_dz<T, B, B, WM, WN, false>, Tile<T, B, B, WM, WN, false, false>::kBytes + B * 20, done, 64 * WM * WN, B, a.N, a.dz_ld, 1, s, a)
   WD_TILES(size, WD_CALL)
 #undef WD_CALL
 }
@@ -539,6 +571,7 @@ struct LossPlan {
   bool copy_x, copy_w;       // (for the product W x)
   int64_t block;             // loss: rows of a launch
   int64_t rows, cols;        // gradients: rows and labels of a piece
+  int64_t terms;             // gradients: of dz
   size_t w, x, part, label_z, info, power, dz, db, sum, split, end;
 };
 
@@ -548,10 +581,10 @@ constexpr int64_t kPieceBytes = 512ll << 20;
 
 static bool rows_fit(const void* p, int64_t ld, int64_t rows) { return !((uintptr_t)p & 15) && (ld % 8 == 0 || rows == 1) && ld < (1 << 22); }
 
-// Of the sums of product i (M rows) of a piece, which are needed for splits and for pieces: of the rows
-// (i = 0), of the labels (1).
+// Of the sums of product i (M rows) of a piece, which are needed for splits, for pieces of the rows
+// (i = 0) or of the labels (1), and for dz's terms (1).
 static uint64_t split_bytes(const LossPlan& p, const Cut& cut, int i, int64_t M, int64_t all) {
-  const bool pieces = (i == 0 ? p.rows : p.cols) < all;
+  const bool pieces = (i == 0 ? p.rows : p.cols) < all || (i == 1 && p.terms > 1);
   return cut.splits[i] > 1 || (cut.splits[i] && pieces) ? (uint64_t)cut.splits[i] * M * p.Dp * 4 : 0;
 }
 
@@ -578,6 +611,7 @@ static LossPlan plan_loss(const wd_loss_args* a, bool grads) {
   } else {
     p.rows = N;
     p.cols = P;
+    p.terms = N <= kCarefulRows ? 2 : 1;
     const int64_t most = kPieceBytes / 2;
     if ((uint64_t)N * align_up(P, 64) > (uint64_t)most) {
       if (N > P)
@@ -588,10 +622,10 @@ static LossPlan plan_loss(const wd_loss_args* a, bool grads) {
       p.rows = std::min<int64_t>(N, align_up((N + (N + p.rows - 1) / p.rows - 1) / ((N + p.rows - 1) / p.rows), 256));
       p.cols = std::min<int64_t>(P, align_up((P + (P + p.cols - 1) / p.cols - 1) / ((P + p.cols - 1) / p.cols), 256));
     }
-    p.x = take((uint64_t)p.rows * p.Dp * 2);
+    p.x = take((uint64_t)p.rows * p.terms * p.Dp * 2);
     p.info = take((uint64_t)N * sizeof(RowInfo));
     p.power = take(8);
-    p.dz = take((uint64_t)p.rows * align_up(p.cols, 64) * 2);
+    p.dz = take((uint64_t)p.rows * p.terms * align_up(p.cols, 64) * 2);
     if (p.rows < N) p.sum = take((uint64_t)P * p.Dp * 4);
     if (p.cols < P) p.sum = take((uint64_t)N * p.Dp * 4);
     uint64_t db = 0, split = 0;  // (the last piece may be cut otherwise)
@@ -599,8 +633,8 @@ static LossPlan plan_loss(const wd_loss_args* a, bool grads) {
       for (int64_t c : {p.cols, (P - 1) % p.cols + 1}) {
         const int size = tile_size(n, align_up(c, 64));
         db = std::max(db, (uint64_t)((n + size - 1) / size) * c * 4);
-        const Cut cut = cut_products(n, c, D, a->dweight, a->dx);
-        split = std::max(split, split_bytes(p, cut, 0, c, N) + split_bytes(p, cut, 1, n, P));
+        const Cut cut = cut_products(n * p.terms, c, D, a->dweight, a->dx);
+        split = std::max(split, split_bytes(p, cut, 0, c, N) + split_bytes(p, cut, 1, n * p.terms, P));
       }
     p.db = take(db);
     p.split = take(split);
@@ -691,7 +725,8 @@ static void run_grads(const wd_loss_args* a, const LossPlan& p, char* ws, hipStr
     in_rows(n, p.Dp / 8, [&](int64_t r0, int64_t rows, dim3 grid) {
       const int64_t at = n0 + r0;
       const PrepareArgs prepare{(const T*)a->x + at * a->x_ld, a->x_ld, (uint32_t)rows, (int)D, (int)P, (const float2*)a->stats + at,
-                                a->grad ? a->grad + at : nullptr, a->target + at, power, a->grad, own_power ? N : 0, info + at, (T*)(ws + p.x) + r0 * p.Dp, p.Dp};
+                                a->grad ? a->grad + at : nullptr, a->target + at, power, a->grad, own_power ? N : 0, info + at, (T*)(ws + p.x) + r0 * p.Dp,
+                                p.terms > 1 ? (T*)(ws + p.x) + (n + r0) * p.Dp : nullptr, p.Dp};
       hipLaunchKernelGGL((k_loss_prepare<T>), grid, dim3(256), 0, s, prepare);
     });
     for (int64_t c0 = 0; c0 < P; c0 += p.cols) {
@@ -699,21 +734,21 @@ static void run_grads(const wd_loss_args* a, const LossPlan& p, char* ws, hipStr
       LossArgs l{};
       l.x = ws + p.x, l.w = (const char*)w + c0 * w_ld, l.x_ld = p.Dp * 2, l.w_ld = w_ld, l.N = n, l.P = (int)c, l.K = (int)p.Dp;
       l.bias = a->bias ? a->bias + c0 : nullptr, l.info = info + n0, l.p_first = (int)c0, l.dz = ws + p.dz, l.dz_ld = align_up(c, 64);
-      l.db_part = a->dbias ? (float*)(ws + p.db) : nullptr;
+      l.db_part = a->dbias ? (float*)(ws + p.db) : nullptr, l.rest = p.terms > 1 ? (T*)l.dz + n * l.dz_ld : nullptr;
       const int size = tile_size(n, l.dz_ld);
       launch_dz<T>(l, size, s);
       const DbArgs db{l.db_part, (int)((n + size - 1) / size), (int)c, power, n0 > 0, a->dbias + c0};
       if (a->dbias && !a->dweight) hipLaunchKernelGGL(k_loss_db, dim3((uint32_t)((c + 255) / 256)), dim3(256), 0, s, db);
       if (!a->dweight && !a->dx) continue;
-      const Cut cut = cut_products(n, c, D, a->dweight, a->dx);
+      const Cut cut = cut_products(n * p.terms, c, D, a->dweight, a->dx);
       ProductArgs dw{}, dx{};
-      dw.x = l.dz, dw.x_ld = l.dz_ld * 2, dw.w = ws + p.x, dw.w_ld = p.Dp * 2, dw.M = c, dw.C = (int)D, dw.K = (int)n, dw.k_each = cut.k_each[0];
+      dw.x = l.dz, dw.x_ld = l.dz_ld * 2, dw.w = ws + p.x, dw.w_ld = p.Dp * 2, dw.M = c, dw.C = (int)D, dw.K = (int)(n * p.terms), dw.k_each = cut.k_each[0];
       dw.part = (float*)(ws + p.split), dw.part_ld = p.Dp, dw.power = power, dw.out_ld = a->dweight_ld, dw.db = db, dw.splits = cut.splits[0];
-      dx.x = l.dz, dx.x_ld = l.dz_ld * 2, dx.w = l.w, dx.w_ld = w_ld, dx.M = n, dx.C = (int)D, dx.K = (int)c, dx.k_each = cut.k_each[1];
+      dx.x = l.dz, dx.x_ld = l.dz_ld * 2, dx.w = l.w, dx.w_ld = w_ld, dx.M = n * p.terms, dx.C = (int)D, dx.K = (int)c, dx.k_each = cut.k_each[1];
       dx.part = (float*)(ws + p.split + split_bytes(p, cut, 0, c, N)), dx.part_ld = p.Dp, dx.power = power, dx.info = info + n0, dx.out_ld = a->dx_ld;
       dx.splits = cut.splits[1];
       void *out_w = (T*)a->dweight + c0 * a->dweight_ld, *out_x = (T*)a->dx + n0 * a->dx_ld;
-      const bool sums_w = p.rows < N || dw.splits > 1, sums_x = p.cols < P || dx.splits > 1;  // (through 32-bit sums)
+      const bool sums_w = p.rows < N || dw.splits > 1, sums_x = p.cols < P || dx.splits > 1 || p.terms > 1;  // (through 32-bit sums)
       if (!sums_w) dw.out = out_w;
       if (!sums_x) dx.out = out_x;
       launch_products<T>(dw, dx, cut.size, s);
@@ -723,7 +758,8 @@ static void run_grads(const wd_loss_args* a, const LossPlan& p, char* ws, hipStr
       }
       if (a->dx && sums_x) {
         if (c0 + p.cols >= P) dx.out = out_x;
-        join(dx, (int)dx.splits, c0 > 0 ? sum : nullptr, sum);
+        dx.M = n;  // (a split's terms are as many splits)
+        join(dx, (int)(dx.splits * p.terms), c0 > 0 ? sum : nullptr, sum);
       }
     }
   }

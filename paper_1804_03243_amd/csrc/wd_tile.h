@@ -190,7 +190,9 @@ struct Side {
 // starts into its place.  (Three or four steps in LDS in the smallest tiles: no faster,
 // and up to 17% slower.)  What the caller has written to other LDS before is there behind it
 // for every wavefront; kBytes of `lds` are free again after a barrier.
-template <class T, int BM, int BN, int WM, int WN, bool XKR, bool WKR>
+// EXACT: the sums of four steps are formed by themselves and added up with what each
+// addition rounds off, so that a sum is off by the roundings within four steps and one more.
+template <class T, int BM, int BN, int WM, int WN, bool XKR, bool WKR, bool EXACT = false>
 struct Tile {
   static constexpr int kWaves_ = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
   static constexpr int kStep = (BM + BN) * 128, kBytes = 2 * kStep;
@@ -217,11 +219,16 @@ struct Tile {
 #pragma unroll
       for (int i = 0; i < TM; ++i) o.x[i] = x.rows(at, i, half);
     };
+    f32x4 part[EXACT ? TM : 1][EXACT ? TN : 1] = {}, off[EXACT ? TM : 1][EXACT ? TN : 1] = {};
     const auto products = [&](const Operands& o) {
 #pragma unroll
       for (int i = 0; i < TM; ++i)
 #pragma unroll
-        for (int j = 0; j < TN; ++j) acc[i][j] = mfma16(o.w[j], o.x[i], acc[i][j], T{});
+        for (int j = 0; j < TN; ++j)
+          if constexpr (EXACT)
+            part[i][j] = mfma16(o.w[j], o.x[i], part[i][j], T{});
+          else
+            acc[i][j] = mfma16(o.w[j], o.x[i], acc[i][j], T{});
       // an operand read between every few products
       constexpr int kReads = TM * (XKR ? 2 : 1) + TN * (WKR ? 2 : 1), kEach = TM * TN / kReads > 0 ? TM * TN / kReads : 1;
 #pragma unroll
@@ -229,6 +236,19 @@ struct Tile {
         __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         __builtin_amdgcn_sched_group_barrier(0x008, kEach, 0);
       }
+    };
+    const auto add = [&]() {
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            const float a = acc[i][j][e], b = part[i][j][e], s = a + b, v = s - a, r = (a - (s - v)) + (b - v);
+            acc[i][j][e] = s;
+            off[i][j][e] += fabsf(r) < INFINITY ? r : 0.0f;  // (sums that are not finite stay as they are)
+            part[i][j][e] = 0.0f;
+          }
     };
     int now = 0, next = kStep;
     stage(0, now);
@@ -250,8 +270,16 @@ struct Tile {
       if (k0 + 2 * kStepK < K) stage(k0 + 2 * kStepK, now);
       read(next, 0, even);
       products(odd);
+      if constexpr (EXACT)
+        if (k0 / kStepK % 4 == 3 || k0 + kStepK >= K) add();
       now = next;
       next = kStep - next;
+    }
+    if constexpr (EXACT) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[i][j] += off[i][j];
     }
   }
 };
