@@ -16,9 +16,9 @@
 // What is rounded: dz to 16 bits, as matrix instructions take it; half a step of the
 // type, relative to each value, as large as the rounding of the gradients themselves (over
 // many rows they are 1.4 times as far from 64 bits as exact ones rounded), whose sums run
-// in 32 bits.  Up to 64 rows dz has two terms (kCarefulRows).  Half precision has dz times a power of two that takes the
-// largest |g| to [2^14, 2^15), so that what is 2^29 times smaller than the largest
-// keeps its bits.  db sums the 32-bit values.
+// in 32 bits.  Up to 64 rows dz has two terms (kCarefulRows).  Half precision has dz
+// times a power of two that takes the largest |g| to [2^14, 2^15), so that what is 2^29
+// times smaller than the largest keeps its bits.  db sums the 32-bit values.
 #include <algorithm>
 #include <cmath>
 
@@ -443,7 +443,8 @@ constexpr int64_t kCarefulRows = 64;
 enum TileSize { kSmall = 64, kMiddle = 128, kLarge = 256 };
 static int64_t tiles_of(int64_t M, int64_t C, int size) { return ((M + size - 1) / size) * ((C + size - 1) / size); }
 static TileSize tile_size(int64_t M, int64_t C) {
-  return M <= kCarefulRows ? kSmall : tiles_of(M, C, 256) >= 256 ? kLarge : tiles_of(M, C, 128) >= 192 ? kMiddle : kSmall;
+  return M <= kCarefulRows ? kSmall :  // (64 rows to 100000 labels: 48 us, in tiles of 128 63)
+         tiles_of(M, C, 256) >= 256 ? kLarge : tiles_of(M, C, 128) >= 192 ? kMiddle : kSmall;
 }
 
 template <class K, class A>
@@ -464,8 +465,8 @@ static void launch_tile(K* kernel, int bytes, std::atomic<uint64_t>& done, int t
   }
 
 template <class T>
-static void launch_loss(const LossArgs& a, int size, hipStream_t s) {
-  if (a.N <= kCarefulRows) {
+static void launch_loss(const LossArgs& a, int size, bool careful, hipStream_t s) {
+  if (careful) {
     static std::atomic<uint64_t> done{0};
     launch_tile(k_loss<T, 64, 64, 2, 2, true>, Tile<T, 64, 64, 2, 2, false, false>::kBytes + 64 * 8, done, 256, 64, a.N, a.P, 1, s, a);
     return;
@@ -478,7 +479,7 @@ static void launch_loss(const LossArgs& a, int size, hipStream_t s) {
 }
 template <class T>
 static void launch_dz(const LossArgs& a, int size, hipStream_t s) {
-  if (a.N <= kCarefulRows) {
+  if (a.rest) {
     static std::atomic<uint64_t> done{0};
     launch_tile(k_loss_dz<T, 64, 64, 2, 2, true>, Tile<T, 64, 64, 2, 2, false, false>::kBytes + 64 * 20, done, 256, 64, a.N, a.dz_ld, 1, s, a);
     return;
@@ -604,9 +605,10 @@ static LossPlan plan_loss(const wd_loss_args* a, bool grads) {
   if (!grads) {
     const int64_t cols = (P + 255) / 256;
     p.block = std::min(N, std::max<int64_t>(16, 8192 / cols) * 256);
-    const int64_t tiles = (P + tile_size(p.block, P) - 1) / tile_size(p.block, P);
     if (p.copy_x) p.x = take((uint64_t)p.block * p.Dp * 2);
-    p.part = take((uint64_t)p.block * tiles * sizeof(float2));
+    uint64_t parts = 0;  // (the last block may have smaller tiles)
+    for (int64_t n : {p.block, (N - 1) % p.block + 1}) parts = std::max(parts, (uint64_t)n * ((P + tile_size(n, P) - 1) / tile_size(n, P)));
+    p.part = take(parts * sizeof(float2));
     p.label_z = take((uint64_t)p.block * 4);
   } else {
     p.rows = N;
@@ -668,9 +670,9 @@ static void run_loss(const wd_loss_args* a, const LossPlan& p, char* ws, hipStre
     lay<T>(a->weight, a->weight_ld, a->P, a->D, ws + p.w, p.Dp, s);
     w = ws + p.w, w_ld = p.Dp * 2;
   }
-  const int size = tile_size(p.block, a->P), tiles = (a->P + size - 1) / size;
   for (int64_t n0 = 0; n0 < a->N; n0 += p.block) {
     const int64_t n = std::min(p.block, a->N - n0);
+    const int size = tile_size(n, a->P), tiles = (a->P + size - 1) / size;
     const void* x = (const T*)a->x + n0 * a->x_ld;
     int64_t x_ld = a->x_ld * 2;
     if (p.copy_x) {
@@ -680,7 +682,7 @@ static void run_loss(const wd_loss_args* a, const LossPlan& p, char* ws, hipStre
     LossArgs l{};
     l.x = x, l.w = w, l.x_ld = x_ld, l.w_ld = w_ld, l.N = n, l.P = a->P, l.K = (int)p.Dp, l.bias = a->bias;
     l.target = a->target + n0, l.part = (float2*)(ws + p.part), l.label_z = (float*)(ws + p.label_z);
-    launch_loss<T>(l, size, s);
+    launch_loss<T>(l, size, a->N <= kCarefulRows, s);
     float* loss = a->loss ? a->loss + n0 : nullptr;
     float2* stats = a->stats ? (float2*)a->stats + n0 : nullptr;
     if (tiles <= 8 || (tiles <= 64 && n >= 16384))

@@ -1203,7 +1203,10 @@ def clip_gradients(gradients, max_norm: float, out=None):
     if len(outs) != len(gradients):
         raise ValueError("out needs a tensor for each gradient")
     rows = []
+    lost = torch.is_grad_enabled()
     for g, o in zip(gradients, outs):
+        if lost and (g.requires_grad or o.requires_grad):
+            _no_gradient(torch, "clip_gradients", g, o)
         if g.device != dev or g.dtype not in types or not g.is_contiguous():
             raise ValueError(f"gradients must be contiguous float32, float16 or bfloat16 tensors on {dev}")
         if g is o:

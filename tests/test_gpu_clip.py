@@ -175,6 +175,7 @@ def test_refusals(wf):
     t = torch.ones(100, device=DEV)
     for bad in (lambda: wf.clip_gradients([], 1.0), lambda: wf.clip_gradients([t.cpu()], 1.0), lambda: wf.clip_gradients([t.double()], 1.0),
                 lambda: wf.clip_gradients([t[::2]], 1.0), lambda: wf.clip_gradients([t], 1.0, out=[]),
+                lambda: wf.clip_gradients([t.clone().requires_grad_()], 1.0), lambda: wf.clip_gradients([t], 1.0, out=[t.clone().requires_grad_()]),
                 lambda: wf.clip_gradients([t], 1.0, out=[t[:50]]), lambda: wf.clip_gradients([t], 1.0, out=[t.int()])):
         with pytest.raises(ValueError):
             bad()

@@ -109,7 +109,7 @@ def label_slack(d, label, more, x):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F16])
-@pytest.mark.parametrize("N,D,P", [(1300, 40, 120_001), (150_001, 24, 1001), (70_000, 16, 300)])
+@pytest.mark.parametrize("N,D,P", [(2300, 40, 120_001), (300_001, 24, 1001), (70_000, 16, 300), (3, 16, 5_000_000)])
 def test_pieces(wf, dtype, N, D, P):
     """Gradients in several pieces of the labels, and of the rows; losses in several launches."""
     d = on(make(N, D, P, dtype, seed=5))
@@ -360,3 +360,45 @@ def test_refusals(wf):
                 lambda: wf.cross_entropy_grads(x, w, t, b, d["grad"][:9])):
         with pytest.raises(ValueError):
             bad()
+
+
+def test_blocks_of_rows(wf):
+    """Losses in several launches, the last of a few rows (other tiles than the others')."""
+    N, D, P = 4096 * 2 + 40, 16, 140_001  # (blocks of 4096 rows)
+    d = on(make(N, D, P, BF16, seed=8))
+    loss = wf.cross_entropy(d["x"], d["weight"], d["target"], d["bias"])
+    has = (d["target"] >= 0) & (d["target"] < P)
+    for a in range(0, N, 2048):
+        r = slice(a, min(a + 2048, N))
+        z = d["x"][r].double() @ d["weight"].double().T + d["bias"].double()
+        err = (D + 8) * plain.EPS * (d["x"][r].double().abs() @ d["weight"].double().abs().T + d["bias"].double().abs()).amax(1)
+        want = torch.where(has[r], torch.logsumexp(z, 1) - z.gather(1, d["target"][r].long().clamp(0, P - 1)[:, None])[:, 0], 0.0)
+        slack = 3 * err + (P / 64 + 64) * plain.EPS + 16 * plain.EPS * z.abs().amax(1) + plain.EPS * want
+        close(loss[r], want.cpu(), slack.cpu())
+
+
+@pytest.mark.parametrize("dtype", [BF16, F16])
+@pytest.mark.parametrize("N", [1, 2, 64])
+def test_few_rows_are_rounded_once(wf, dtype, N):
+    """Up to 64 rows dz has two terms: the gradients are those of exact ones rounded, but for
+    32-bit sums and what two terms leave (2^-17 of a value in bfloat16, 2^-22 in half precision)."""
+    d = make(N, 96, 200, dtype, seed=31 + N)
+    d["target"][0] = 7
+    d["x"][0] *= 0.25  # (not sure of its label)
+    g = on(d)
+    want = plain.cross_entropy(**d)
+    got = wf.cross_entropy_grads(g["x"], g["weight"], g["target"], g["bias"], g["grad"])
+    rel, least = plain.rounding(dtype)
+    terms = {BF16: 2.0 ** -16, F16: 2.0 ** -21}[dtype]
+    z = d["x"].double() @ d["weight"].double().T + d["bias"].double()
+    p = torch.softmax(z, 1)
+    # (a logit's 32-bit error, the sum's and the exponential's, relative to each probability)
+    logit = (104 * plain.EPS * (d["x"].double().abs() @ d["weight"].double().abs().T + d["bias"].double().abs())).amax(1, keepdim=True)
+    dz = (4 * logit + 96 * plain.EPS + 8 * plain.EPS * (z.amax(1, keepdim=True) - z).abs()) * p * d["grad"].double()[:, None]
+    size = (p * d["grad"].double()[:, None])
+    has = (d["target"] >= 0) & (d["target"] < 200)
+    size[has, d["target"][has].long()] += d["grad"].double()[has]
+    for v, k, err in ((got[1], "dx", (dz + (terms + 500 * plain.EPS) * size) @ d["weight"].double().abs()),
+                      (got[2], "dweight", (dz + (terms + 500 * plain.EPS) * size).T @ d["x"].double().abs())):
+        small = 2.0 ** -38 * float(d["grad"].max()) * 300 * 8 if dtype is F16 else 0.0  # (what half precision's second term cannot hold)
+        close(v, want[k], err * (1 + rel) + rel * want[k].abs() + least + small)

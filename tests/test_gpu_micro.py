@@ -237,3 +237,12 @@ def test_refusals(wf):
                 lambda: wf.Micro(m.codes, m.scales, 100), lambda: wf.Micro(m.codes[:3], m.scales, 40), lambda: wf.Micro(m.codes.int(), m.scales, 40)):
         with pytest.raises(ValueError):
             bad()
+
+
+@pytest.mark.parametrize("N", [3, 40, 300])
+@pytest.mark.parametrize("power", [0, 60, -60, 100])
+def test_products_of_far_apart_sizes(wf, N, power):
+    """Rows and weights whose powers of two cancel in the product."""
+    gen = torch.Generator().manual_seed(9)
+    x, w = torch.randn((N, 130), generator=gen) * 2.0 ** power, torch.randn((100, 130), generator=gen) * 2.0 ** -power
+    project(wf, x, w, None)
