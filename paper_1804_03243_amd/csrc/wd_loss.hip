@@ -60,14 +60,13 @@ __device__ __forceinline__ float2 join(float2 a, float2 b) {
   return make_float2(top, a.y * __builtin_amdgcn_exp2f((a.x - at) * kLog2e) + b.y * __builtin_amdgcn_exp2f((b.x - at) * kLog2e));
 }
 
-// What a tile's end reads of its outputs and rows, brought to LDS before the product: read from
-// memory there it is round trips that nothing hides (losses of 32000 rows to 6000 labels
-// 367 us with the reads at the end, 349 so; gradients of 4096 rows to 100000 3315 and 3220).  The logits are acc + bias, -inf
-// past the last output.
-template <int BN>
-__device__ __forceinline__ void keep_bias(const LossArgs& a, int p0, float* bias) {
-  for (int p = threadIdx.x; p < BN; p += blockDim.x) bias[p] = p0 + p >= a.P ? -INFINITY : a.bias ? a.bias[p0 + p] : 0.0f;
-}
+// What a tile's end needs of its outputs and rows is read before the product, a value or a row to
+// a thread, and passed round through LDS behind it: read at the end it is round trips that
+// nothing hides (losses of 32000 rows to 6000 labels 367 us, and 349 without; gradients of
+// 4096 rows to 100000 3315 and 3220).  Nor does the product wait for it: passed round before
+// the first step, gradients of 777 rows to 777 labels are 62.9 us, and 61.1 so; of 256 rows to
+// 100000 138.1 and 136.8.  The logits are acc + bias, -inf past the last output.
+__device__ __forceinline__ float bias_of(const LossArgs& a, int p) { return p >= a.P ? -INFINITY : a.bias ? a.bias[p] : 0.0f; }
 template <int TN>
 __device__ __forceinline__ void read_bias(const float* kept, float (&bias)[TN][4]) {
   const int quad = (threadIdx.x & 63) >> 4;
@@ -90,16 +89,20 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
   const int p0 = (int)col_tile * BN;
   float* kept_bias = (float*)(lds + Tl::kBytes);  // [BN]
   int* labels = (int*)(kept_bias + BN);           // [BM]
-  keep_bias<BN>(a, p0, kept_bias);
-  for (int r = threadIdx.x; r < BM; r += 64 * WM * WN) labels[r] = n0 + r < a.N ? a.target[n0 + r] : -1;
+  static_assert(BM <= 64 * WM * WN && BN <= 64 * WM * WN, "");
+  const int mine = threadIdx.x;
+  const float my_bias = mine < BN ? bias_of(a, p0 + mine) : 0.0f;
+  const int my_label = mine < BM && n0 + mine < a.N ? a.target[n0 + mine] : -1;
   f32x4 acc[TM][TN] = {};
   Tl::multiply({(const char*)a.x + n0 * a.x_ld, a.x_ld, (int)min<int64_t>(BM, a.N - n0)},
                {(const char*)a.w + (int64_t)p0 * a.w_ld, a.w_ld, min(BN, a.P - p0)}, a.K, lds, acc);
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
   const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
+  if (mine < BN) kept_bias[mine] = my_bias;
+  if (mine < BM) labels[mine] = my_label;
+  __syncthreads();  // (every wavefront has read its last operands)
   float bias[TN][4];
   read_bias<TN>(kept_bias + wn, bias);
-  __syncthreads();  // (every wavefront has read its last operands)
   float2* sums = (float2*)lds;  // [WN][BM]
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
@@ -270,16 +273,20 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
   const int p0 = (int)col_tile * BN;
   float* kept_bias = (float*)(lds + Tl::kBytes);     // [BN]
   RowInfo* infos = (RowInfo*)(kept_bias + BN);       // [BM]
-  keep_bias<BN>(a, p0, kept_bias);
-  for (int r = threadIdx.x; r < BM; r += 64 * WM * WN) infos[r] = n0 + r < a.N ? a.info[n0 + r] : RowInfo{0.0f, 0.0f, 0.0f, -1};
+  static_assert(BM <= 64 * WM * WN && BN <= 64 * WM * WN, "");
+  const int mine = threadIdx.x;
+  const float my_bias = mine < BN ? bias_of(a, p0 + mine) : 0.0f;
+  const RowInfo my_info = mine < BM && n0 + mine < a.N ? a.info[n0 + mine] : RowInfo{0.0f, 0.0f, 0.0f, -1};
   f32x4 acc[TM][TN] = {};
   Tl::multiply({(const char*)a.x + n0 * a.x_ld, a.x_ld, (int)min<int64_t>(BM, a.N - n0)},
                {(const char*)a.w + (int64_t)p0 * a.w_ld, a.w_ld, min(BN, a.P - p0)}, a.K, lds, acc);
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15, quad = lane >> 4;
   const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
+  if (mine < BN) kept_bias[mine] = my_bias;
+  if (mine < BM) infos[mine] = my_info;
+  __syncthreads();  // (every wavefront has read its last operands)
   float bias[TN][4], db[TN][4] = {};
   read_bias<TN>(kept_bias + wn, bias);
-  __syncthreads();  // (every wavefront has read its last operands)
   // (Formed as they are stored, a block of 16 rows at a time: a pass of its own over the
   // accumulators spilled, and took 3425 us for 3375 of the whole call of 4096 rows to 100000.)
   RowInfo r{};
@@ -369,8 +376,8 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, uint32_t numb
   const int64_t m0 = (int64_t)row_tile * BM;
   const int c0 = (int)col_tile * BN, k0 = (int)split * a.k_each;
   int* in = (int*)(lds + Tl::kBytes);  // [BM] whether the row has a part in the gradients
-  if (a.out)
-    for (int r = threadIdx.x; r < BM; r += 64 * WM * WN) in[r] = !a.info || a.info[min<int64_t>(m0 + r, a.M - 1)].label >= 0;
+  const bool mine = a.out && (int)threadIdx.x < BM;
+  const int my_in = mine && (!a.info || a.info[min<int64_t>(m0 + threadIdx.x, a.M - 1)].label >= 0);
   const float by = a.out && a.power ? a.power[1] : 1.0f;
   f32x4 acc[TM][TN] = {};
   const char* x = (const char*)a.x + (XKR ? m0 * 2 + (int64_t)k0 * a.x_ld : m0 * a.x_ld + (int64_t)k0 * 2);
@@ -378,6 +385,7 @@ __device__ __forceinline__ void product_tile(const ProductArgs& a, uint32_t numb
                min(a.k_each, a.K - k0), lds, acc);
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, col = lane & 15;
   const int wm = (wave / WN) * (BM / WM), wn = (wave % WN) * (BN / WN);
+  if (mine) in[threadIdx.x] = my_in;
   __syncthreads();  // (every wavefront has read its last operands)
   if (XKR && a.db.part && col_tile == 0 && split == 0)
     for (int r = threadIdx.x; r < BM; r += 64 * WM * WN) sum_db(a.db, m0 + r);

@@ -177,7 +177,8 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_micro_tiles(MicroArgs a, ui
   };
   // (read from memory at the tile's end it would be a round trip that nothing hides)
   float* kept_bias = (float*)(lds + 2 * (kStep + kScaleStep));
-  for (int p = threadIdx.x; p < BN; p += 64 * kWaves_) kept_bias[p] = a.bias && p < outs ? a.bias[p0 + p] : 0.0f;
+  static_assert(BN <= 64 * kWaves_, "");
+  const float my_bias = a.bias && (int)threadIdx.x < min(BN, outs) ? a.bias[p0 + threadIdx.x] : 0.0f;
   f32x4 acc[TM][TN] = {};
   const auto products = [&](const Operands& o, auto half) {
 #pragma unroll
@@ -210,10 +211,11 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_micro_tiles(MicroArgs a, ui
     now = next;
     next = kStep - next;
   }
+  if ((int)threadIdx.x < BN) kept_bias[threadIdx.x] = my_bias;
+  __syncthreads();  // (every wavefront has read its last operands)
   f32x4 bias[TN];
 #pragma unroll
   for (int j = 0; j < TN; ++j) bias[j] = *(const f32x4*)(kept_bias + wn + j * 16 + quad * 4);
-  __syncthreads();  // (every wavefront has read its last operands)
   store_tile<O, TM, TN>((O*)a.out + (n0 + wm) * a.out_ld + p0 + wn, a.out_ld, a.N - n0 - wm, a.P - p0 - wn, lds + wave * kStoreBytes<O, TN>,
                         [&](int i, int j, int e) { return acc[i][j][e] + bias[j][e]; }, a.stream);
 }
