@@ -471,9 +471,10 @@ typedef struct {
   int64_t weight_ld;
   const float* bias;       /* [P]; NULL: 0 */
   const int32_t* target;   /* [N] */
-  float* loss;             /* wd_cross_entropy writes [N]; NULL: not wanted */
+  float* loss;             /* wd_cross_entropy (and wd_cross_entropy_grads without stats) writes [N]; NULL: not wanted */
   float* stats;            /* [N][2], 8-byte aligned: a row's largest logit, and the sum of exp(z - largest).
-                              wd_cross_entropy writes them (NULL: not wanted), wd_cross_entropy_grads reads them */
+                              wd_cross_entropy writes them (NULL: not wanted), wd_cross_entropy_grads reads them
+                              (NULL: it forms them itself, and writes `loss`) */
   const float* grad;       /* g [N]; NULL: 1 */
   void* dx;                /* [N][dx_ld], dx_ld >= D; NULL: not wanted */
   int64_t dx_ld;
@@ -481,8 +482,10 @@ typedef struct {
   int64_t dweight_ld;
   float* dbias;            /* [P]; NULL: not wanted */
 } wd_loss_args;
-/* wd_cross_entropy_grads: after wd_cross_entropy of the same x, weight, bias and target;
- * at least one gradient is wanted, and they overlap nothing else.  N = 0: dweight and
+/* wd_cross_entropy_grads: after wd_cross_entropy of the same x, weight, bias and target (`stats`), or
+ * by itself (`stats` NULL), which takes less time and more workspace: 2.6 bytes of each
+ * logit, up to 5.3 GB, for its exponential in 20 bits (off by 2^-18 of it).
+ * At least one gradient is wanted, and they overlap nothing else.  N = 0: dweight and
  * dbias are zeros.  At most 2^19 rows or labels (one of the two may be more).
  * ws as for wd_project (the sizes depend on which gradients are wanted). */
 wd_status wd_cross_entropy_workspace_bytes(const wd_loss_args* a, size_t* bytes);

@@ -1,17 +1,21 @@
 // Cross entropy of hidden rows against their labels, straight from the rows and the
-// output layer's weights, and its gradients; the logits are never in memory.
+// output layer's weights, and its gradients.
 //
 //   z = W x[n] + b      loss[n] = log sum_p exp z_p - z_t, t = target[n]
 //   dz = g[n] (softmax z - 1 at t)      dx[n] = dz W      dW = sum_n dz x[n]      db = sum_n dz
 //
 // Loss: the product W x in tiles of matrix instructions; a tile leaves its largest
 // logit and its sum of exponentials for each of its rows (8 bytes per 256 logits), and
-// the logit of the row's label.  A second kernel joins the row's tiles.
+// the logit of the row's label.  A second kernel joins the row's tiles.  The logits are never in
+// memory.
 //
-// Gradients: the same tiles are formed again and turned into dz, rounded to the
-// inputs' 16-bit type (below) in a workspace that holds a piece of the rows or of the
-// labels; two more products, dz W and dz^T x, read it from there.  Forming the logits
-// twice costs 2 N D P operations of 8, keeping them would cost N P values of memory.
+// Gradients: dz, rounded to the inputs' 16-bit type (below), in the workspace; two
+// more products, dz W and dz^T x, read it from there.  It comes about in one of two ways.
+// A call that forms the losses too (cross_entropy_grads without stats) has their tiles leave the
+// exponentials as well, in 20 bits (Upper, 2.5 bytes each), and a pass over these makes dz
+// of them in their place.  Elsewhere (the losses' call came before, and kept 8 bytes of a row;
+// more than kKeptBytes; narrow layers, kKeptWidth) the same tiles are formed again, a piece of the
+// rows or of the labels at a time: 2 N D P operations of 8 more, instead of 7 N P bytes.
 //
 // What is rounded: dz to 16 bits, as matrix instructions take it; half a step of the
 // type, relative to each value, as large as the rounding of the gradients themselves (over
@@ -21,6 +25,7 @@
 // times smaller than the largest keeps its bits.  db sums the 32-bit values.
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "wd_host.h"
 #include "wd_tile.h"
@@ -36,6 +41,7 @@ struct RowInfo {
   int32_t label;
 };
 
+struct Upper;
 struct LossArgs {
   const void* x;      // rows of the launch, x_ld bytes apart
   const void* w;      // outputs of the launch
@@ -46,11 +52,14 @@ struct LossArgs {
   const int32_t* target;  // of the launch's rows
   float2* part;       // loss: [column tile][N] largest logit, sum of exponentials
   float* label_z;     // loss: [N] logit of the row's label
+  Upper* shares;      // loss: [N][dz_ld] exponentials over those of the largest of 64 outputs; NULL: not kept
+  uint16_t* lower;    // loss: [N][dz_ld / 64][4][4] their lower bits, of outputs 4 q + 16 j at [q][j]
+  float* tops;        // loss: [N][dz_ld / 64] those largest logits
   const RowInfo* info;    // gradients: of the launch's rows
   int32_t p_first;    // gradients: the first output's label
   void* dz;           // gradients: [N][dz_ld], zeros from P on
   void* rest;         // gradients: dz's second term, what the rounding left, as dz
-  int64_t dz_ld;      // in elements, a multiple of 64
+  int64_t dz_ld;      // in elements, a multiple of 64 (shares too)
   float* db_part;     // gradients: [row tile][P]; NULL: not wanted
 };
 
@@ -78,7 +87,25 @@ __device__ __forceinline__ void read_bias(const float* kept, float (&bias)[TN][4
   }
 }
 
-template <class T, int BM, int BN, int WM, int WN, bool EXACT>
+// A value in [0, 1] in 20 bits, four of exponent and sixteen of mantissa: bits 7 to 26 of kShare
+// times it in 32 bits, cut off, and read in the middle of what they stand for.  So 1 is exact,
+// 0 stays 0, and others are off by 2^-18 of them, and by 2^-32 below 2^-15.  The upper 16
+// bits stand where dz will, the lower four of four outputs together.
+constexpr float kShare = (1 - 0x1p-18f) * 0x1p-111f;
+struct Upper {  // of a value that is times kShare
+  uint16_t u;
+  static __device__ __forceinline__ Upper of(float x) { return {(uint16_t)(__float_as_uint(x) >> 11)}; }
+};
+__device__ __forceinline__ uint32_t lower_of(float x) { return __float_as_uint(x) >> 7 & 15; }
+__device__ __forceinline__ float share_of(Upper upper, uint32_t lower) {
+  const uint32_t bits = (uint32_t)upper.u << 11 | lower << 7;
+  return bits ? __uint_as_float(bits | 0x40) * (1 / kShare) : 0.0f;
+}
+
+// KEEP: the exponentials are left as well, each over that of the largest of its 64 outputs, which are a
+// wavefront's (4096 rows of 1024 to 100000: 738 us without them, 1000 with, of which the stores'
+// bytes are 200).
+template <class T, int BM, int BN, int WM, int WN, bool EXACT, bool KEEP>
 __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2) k_loss(LossArgs a, uint32_t row_tiles, uint32_t col_tiles) {
   using Tl = Tile<T, BM, BN, WM, WN, false, false, EXACT>;
   constexpr int TM = Tl::TM, TN = Tl::TN;
@@ -103,7 +130,7 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
   __syncthreads();  // (every wavefront has read its last operands)
   float bias[TN][4];
   read_bias<TN>(kept_bias + wn, bias);
-  float2* sums = (float2*)lds;  // [WN][BM]
+  float2* sums = (float2*)(lds + (KEEP ? kStoreBytes<Upper, TN> * WM * WN : 0));  // [WN][BM]
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
     const int64_t n = n0 + wm + i * 16 + col;
@@ -118,15 +145,6 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
       }
     top = fmaxf(top, __shfl_xor(top, 16));
     top = fmaxf(top, __shfl_xor(top, 32));
-    const float at = top > -INFINITY ? top : 0.0f;
-    float sum = 0.0f;
-#pragma unroll
-    for (int j = 0; j < TN; ++j)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) sum += __builtin_amdgcn_exp2f((acc[i][j][e] - at) * kLog2e);
-    sum += __shfl_xor(sum, 16);
-    sum += __shfl_xor(sum, 32);
-    if (quad == 0) sums[(wave % WN) * BM + wm + i * 16 + col] = make_float2(top, sum);
     if (__any(t >= 0 && t < TN * 16)) {  // (few blocks hold a label)
 #pragma unroll
       for (int j = 0; j < TN; ++j)
@@ -134,6 +152,31 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
         for (int e = 0; e < 4; ++e)
           if (t == j * 16 + quad * 4 + e && t + p0 + wn < a.P) a.label_z[n] = acc[i][j][e];
     }
+    const float at = top > -INFINITY ? top : 0.0f;
+    float sum = 0.0f;
+#pragma unroll
+    for (int j = 0; j < TN; ++j)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const float v = __builtin_amdgcn_exp2f((acc[i][j][e] - at) * kLog2e);
+        sum += v;
+        if (KEEP) acc[i][j][e] = v * kShare;
+      }
+    sum += __shfl_xor(sum, 16);
+    sum += __shfl_xor(sum, 32);
+    if (quad == 0) sums[(wave % WN) * BM + wm + i * 16 + col] = make_float2(top, sum);
+    if constexpr (KEEP) {
+      Few<uint16_t, 4> few;
+#pragma unroll
+      for (int j = 0; j < TN; ++j)
+        few.v[j] = (uint16_t)(lower_of(acc[i][j][0]) | lower_of(acc[i][j][1]) << 4 | lower_of(acc[i][j][2]) << 8 | lower_of(acc[i][j][3]) << 12);
+      if (n < a.N && p0 + wn < a.dz_ld) *(uint2*)(a.lower + (n * (a.dz_ld / 64) + (p0 + wn) / 64) * 16 + quad * 4) = __builtin_bit_cast(uint2, few);
+    }
+  }
+  if constexpr (KEEP) {
+    static_assert(TN == 4 && kStoreBytes<Upper, TN> * WM * WN + WN * BM * 8 <= Tl::kBytes, "");
+    store_tile<Upper, TM, TN>(a.shares + (n0 + wm) * a.dz_ld + p0 + wn, a.dz_ld, a.N - n0 - wm, a.dz_ld - p0 - wn,
+                              lds + wave * kStoreBytes<Upper, TN>, [&](int i, int j, int e) { return acc[i][j][e]; });
   }
   __syncthreads();
   for (int r = threadIdx.x; r < BM; r += 64 * WM * WN) {
@@ -141,28 +184,53 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
 #pragma unroll
     for (int k = 1; k < WN; ++k) v = join(v, sums[k * BM + r]);
     if (n0 + r < a.N) a.part[(int64_t)col_tile * a.N + n0 + r] = v;
+    if constexpr (KEEP) {
+#pragma unroll
+      for (int k = 0; k < WN; ++k)
+        if (n0 + r < a.N && p0 + k * 64 < a.dz_ld) a.tops[(n0 + r) * (a.dz_ld / 64) + p0 / 64 + k] = sums[k * BM + r].x;
+    }
   }
 }
 
-// A row's tiles: LANES lanes each take every LANES-th, then join theirs.
+struct JoinArgs {
+  const float2* part;  // [tiles][N]
+  int32_t tiles, P;
+  int64_t N;
+  const float* label_z;
+  const int32_t* target;
+  float* loss;    // NULL: not wanted
+  float2* stats;  // NULL: not wanted
+};
+// A row's tiles: LANES lanes each take every LANES-th, four of them under way, then join theirs.
+// The row's first lane has its statistics (and writes them and the loss).
 template <int LANES>
-__global__ void __launch_bounds__(256) k_loss_join(const float2* part, int tiles, const float* label_z, const int32_t* target, int32_t P,
-                                                   int64_t N, float* loss, float2* stats) {
+__device__ __forceinline__ float2 join_tiles(const JoinArgs& a, float2 (*sums)[256 / LANES]) {
   constexpr int kRows = 256 / LANES;
-  __shared__ float2 sums[LANES][kRows];
   const int r = threadIdx.x % kRows, l = threadIdx.x / kRows;
-  const int64_t n = (int64_t)blockIdx.x * kRows + r;
+  const int64_t n = (int64_t)blockIdx.x * kRows + r, at = min<int64_t>(n, a.N - 1);
   float2 v = make_float2(-INFINITY, 0.0f);
-  if (n < N)
-    for (int t = l; t < tiles; t += LANES) v = join(v, part[(int64_t)t * N + n]);
-  sums[l][r] = v;
-  __syncthreads();
-  if (l != 0 || n >= N) return;
+  for (int t0 = l; t0 < a.tiles; t0 += 4 * LANES) {
+    float2 of[4];
 #pragma unroll
-  for (int k = 1; k < LANES; ++k) v = join(v, sums[k][r]);
-  const int t = target[n];
-  if (stats) stats[n] = v;
-  if (loss) loss[n] = t < 0 || t >= P ? 0.0f : v.y == 0.0f ? INFINITY : (v.x - label_z[n]) + logf(v.y);
+    for (int k = 0; k < 4; ++k) of[k] = t0 + k * LANES < a.tiles ? a.part[(int64_t)(t0 + k * LANES) * a.N + at] : make_float2(-INFINITY, 0.0f);
+    v = join(v, join(join(of[0], of[1]), join(of[2], of[3])));
+  }
+#pragma unroll
+  for (int o = kRows; o < 64; o *= 2) v = join(v, make_float2(__shfl_xor(v.x, o), __shfl_xor(v.y, o)));
+  if ((threadIdx.x & 63) < kRows) sums[threadIdx.x >> 6][r] = v;
+  __syncthreads();
+  if (l != 0 || n >= a.N) return v;
+#pragma unroll
+  for (int k = 1; k < 4; ++k) v = join(v, sums[k][r]);
+  const int t = a.target[n];
+  if (a.stats) a.stats[n] = v;
+  if (a.loss) a.loss[n] = t < 0 || t >= a.P ? 0.0f : v.y == 0.0f ? INFINITY : (v.x - a.label_z[n]) + logf(v.y);
+  return v;
+}
+template <int LANES>
+__global__ void __launch_bounds__(256) k_loss_join(JoinArgs a) {
+  __shared__ float2 sums[4][256 / LANES];
+  join_tiles<LANES>(a, sums);
 }
 
 // The power of two of the gradients (half precision) by THREADS threads, in each of them.
@@ -189,8 +257,7 @@ __global__ void __launch_bounds__(1024) k_power(const float* g, int64_t N, float
 }
 
 // What the gradients need of a row.
-__device__ __forceinline__ RowInfo row_info(const float2* stats, const float* g, const int32_t* target, int32_t P, float power, int64_t n) {
-  const float2 s = stats[n];
+__device__ __forceinline__ RowInfo row_info(float2 s, const float* g, const int32_t* target, int32_t P, float power, int64_t n) {
   const int t = target[n];
   const float gn = (g ? g[n] : 1.0f) * power;
   // (a row without a finite logit has no softmax)
@@ -238,26 +305,51 @@ struct PrepareArgs {
   void* again;         // the rows once more; NULL: not wanted
   int64_t to_ld;
 };
+__device__ __forceinline__ float prepared_power(const PrepareArgs& a, float* tops) {
+  if (!a.all_N) return a.power ? a.power[0] : 1.0f;
+  const float power = power_of<256>(a.all_g, a.all_N, tops);
+  if (blockIdx.x == 0 && threadIdx.x == 0) a.power[0] = power, a.power[1] = 1.0f / power;
+  return power;
+}
 template <class T>
 __global__ void __launch_bounds__(256) k_loss_prepare(PrepareArgs a) {
   __shared__ float tops[4];
-  float power = 1.0f;
-  if (a.all_N) {
-    power = power_of<256>(a.all_g, a.all_N, tops);
-    if (blockIdx.x == 0 && threadIdx.x == 0) a.power[0] = power, a.power[1] = 1.0f / power;
-  } else if (a.power) {
-    power = a.power[0];
-  }
+  const float power = prepared_power(a, tops);
   const uint32_t per = (uint32_t)(a.to_ld / 8);
   for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < a.N * per; i += gridDim.x * 256) {
     const int64_t n = i / per;
     const int k = (int)(i % per) * 8;
-    const RowInfo r = row_info(a.stats, a.g, a.target, a.P, power, n);
+    const RowInfo r = row_info(a.stats[n], a.g, a.target, a.P, power, n);
     const Few<T, 8> v = load_few((const T*)a.x + n * a.x_ld, k, a.D);
     if (k == 0) a.info[n] = r;
     const uint4 w = r.label >= 0 ? __builtin_bit_cast(uint4, v) : make_uint4(0, 0, 0, 0);
     *(uint4*)((T*)a.to + n * a.to_ld + k) = w;
     if (a.again) *(uint4*)((T*)a.again + n * a.to_ld + k) = w;
+  }
+}
+// Both in one launch, where the losses are formed for the gradients of all their rows.
+template <class T, int LANES>
+__global__ void __launch_bounds__(256) k_loss_ready(JoinArgs j, PrepareArgs a) {
+  constexpr int kRows = 256 / LANES;
+  __shared__ float2 sums[4][kRows];
+  __shared__ float tops[4];
+  __shared__ int in[kRows];
+  const float power = prepared_power(a, tops);
+  const float2 s = join_tiles<LANES>(j, sums);
+  const int64_t n0 = (int64_t)blockIdx.x * kRows;
+  const int rows = (int)min<int64_t>(kRows, j.N - n0), r = threadIdx.x;
+  if (r < rows) {  // (a row's first lane)
+    const RowInfo info = row_info(s, a.g, a.target, a.P, power, n0 + r);
+    a.info[n0 + r] = info;
+    in[r] = info.label >= 0;
+  }
+  __syncthreads();
+  const uint32_t per = (uint32_t)(a.to_ld / 8);
+  for (uint32_t i = threadIdx.x; i < rows * per; i += 256) {
+    const int64_t n = n0 + i / per;
+    const int k = (int)(i % per) * 8;
+    const Few<T, 8> v = load_few((const T*)a.x + n * a.x_ld, k, a.D);
+    *(uint4*)((T*)a.to + n * a.to_ld + k) = in[i / per] ? __builtin_bit_cast(uint4, v) : make_uint4(0, 0, 0, 0);
   }
 }
 
@@ -326,6 +418,68 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
 #pragma unroll
     for (int k = 1; k < WM; ++k) s += sums[k * BN + p];
     if (p0 + p < a.P) a.db_part[(int64_t)row_tile * a.P + p0 + p] = s;
+  }
+}
+
+// dz from the exponentials that the loss has kept, in their place.  The label's own value, which
+// what is left of 1 hangs on, comes from its logit.  A workgroup takes `rows` rows of 512 outputs, a wavefront
+// every fourth of them, a lane eight outputs, four rows' loads under way.  Bound by memory: 4.5 bytes of each
+// output, 4096 rows to 100000 411 us, 4.6 TB/s.
+struct SharesArgs {
+  uint16_t* dz;       // [N][ld]
+  const uint16_t* lower;
+  int64_t ld, N;
+  int32_t P, rows;    // (rows: a multiple of 16)
+  const float *tops, *label_z;
+  const RowInfo* info;
+  float* db_part;     // [row tile][P]; NULL: not wanted
+};
+template <class T>
+__global__ void __launch_bounds__(256) k_loss_shares(SharesArgs a, uint32_t cols) {
+  __shared__ float sums[4][64][9];
+  const int wave = wave_number(), lane = threadIdx.x & 63;
+  const int64_t tile = blockIdx.x / cols, n0 = tile * a.rows + wave;
+  const int p = ((int)(blockIdx.x % cols) * 64 + lane) * 8, left = (int)min<int64_t>(a.N - tile * a.rows, a.rows);
+  const bool in = p < a.ld;
+  float db[8] = {};
+  for (int r0 = 0; r0 + wave < left; r0 += 16) {
+    uint4 v[4];
+    uint32_t lower[4][2];
+    float top[4];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int64_t n = n0 + min(r0 + k * 4, (left - 1 - wave) / 4 * 4);
+      v[k] = in ? *(const uint4*)(a.dz + n * a.ld + p) : make_uint4(0, 0, 0, 0);
+      const int64_t of64 = n * (a.ld / 64) + p / 64;  // (the lane's outputs are columns 16 j + 4 q and 4 q + 4 of them)
+      top[k] = in ? a.tops[of64] : 0.0f;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) lower[k][h] = in ? a.lower[of64 * 16 + ((p / 4 + h) % 4) * 4 + p / 16 % 4] : 0;
+    }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (r0 + k * 4 + wave >= left) break;
+      const int64_t n = n0 + r0 + k * 4;
+      const RowInfo r = a.info[n];
+      const float by = r.gs * __builtin_amdgcn_exp2f((top[k] - r.top) * kLog2e);
+      const Few<Upper, 8> s = __builtin_bit_cast(Few<Upper, 8>, v[k]);
+      Few<T, 8> out;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        float z = r.label >= 0 ? share_of(s.v[e], lower[k][e / 4] >> (e % 4 * 4) & 15) * by : 0.0f;
+        if (r.label == p + e) z = r.gs * __builtin_amdgcn_exp2f((a.label_z[n] - r.top) * kLog2e) - r.g;
+        db[e] += z;
+        out.v[e] = T::of(z);
+      }
+      if (in) *(uint4*)(a.dz + n * a.ld + p) = __builtin_bit_cast(uint4, out);
+    }
+  }
+  if (!a.db_part) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) sums[wave][lane][e] = db[e];
+  __syncthreads();
+  for (int i = threadIdx.x; i < 512; i += 256) {
+    const int at = (int)(blockIdx.x % cols) * 512 + i;
+    if (at < a.P) a.db_part[tile * a.P + at] = sums[0][i / 8][i % 8] + sums[1][i / 8][i % 8] + sums[2][i / 8][i % 8] + sums[3][i / 8][i % 8];
   }
 }
 
@@ -476,14 +630,23 @@ template <class T>
 static void launch_loss(const LossArgs& a, int size, bool careful, hipStream_t s) {
   if (careful) {
     static std::atomic<uint64_t> done{0};
-    launch_tile(k_loss<T, 64, 64, 2, 2, true>, Tile<T, 64, 64, 2, 2, false, false>::kBytes + 64 * 8, done, 256, 64, a.N, a.P, 1, s, a);
+    launch_tile(k_loss<T, 64, 64, 2, 2, true, false>, Tile<T, 64, 64, 2, 2, false, false>::kBytes + 64 * 8, done, 256, 64, a.N, a.P, 1, s, a);
     return;
   }
-#define WD_CALL(B, WM, WN)                                                                                                      \
-  static std::atomic<uint64_t> done{0};                                                                                         \
-  launch_tile(k_loss<T, B, B, WM, WN, false>, Tile<T, B, B, WM, WN, false, false>::kBytes + B * 8, done, 64 * WM * WN, B, a.N, a.P, 1, s, a)
-  WD_TILES(size, WD_CALL)
-#undef WD_CALL
+  const auto of = [&](auto keep) {
+    constexpr bool KEEP = keep.value;
+    if (size == kLarge) {
+      static std::atomic<uint64_t> done{0};
+      launch_tile(k_loss<T, 256, 256, 2, 4, false, KEEP>, Tile<T, 256, 256, 2, 4, false, false>::kBytes + 256 * 8, done, 512, 256, a.N, a.P, 1, s, a);
+    } else if (size == kMiddle) {
+      static std::atomic<uint64_t> done{0};
+      launch_tile(k_loss<T, 128, 128, 2, 2, false, KEEP>, Tile<T, 128, 128, 2, 2, false, false>::kBytes + 128 * 8, done, 256, 128, a.N, a.P, 1, s, a);
+    } else {
+      static std::atomic<uint64_t> done{0};
+      launch_tile(k_loss<T, 64, 64, 4, 1, false, KEEP>, Tile<T, 64, 64, 4, 1, false, false>::kBytes + 64 * 8, done, 256, 64, a.N, a.P, 1, s, a);
+    }
+  };
+  a.shares ? of(std::true_type{}) : of(std::false_type{});
 }
 template <class T>
 static void launch_dz(const LossArgs& a, int size, hipStream_t s) {
@@ -581,7 +744,8 @@ struct LossPlan {
   int64_t block;             // loss: rows of a launch
   int64_t rows, cols;        // gradients: rows and labels of a piece
   int64_t terms;             // gradients: of dz
-  size_t w, x, part, label_z, info, power, dz, db, sum, split, end;
+  bool keep;                 // gradients: the loss, formed in the call, keeps its exponentials
+  size_t w, x, part, label_z, info, power, dz, db, sum, split, stats, tops, lower, loss, end;
 };
 
 // Bytes of dz at a time.  (4096 rows to 100000 labels: 128 and 256 MB 3300 us, 512 3170, 1024
@@ -597,7 +761,24 @@ static uint64_t split_bytes(const LossPlan& p, const Cut& cut, int i, int64_t M,
   return cut.splits[i] > 1 || (cut.splits[i] && pieces) ? (uint64_t)cut.splits[i] * M * p.Dp * 4 : 0;
 }
 
-static LossPlan plan_loss(const wd_loss_args* a, bool grads) {
+// Exponentials are kept up to 4 GB of dz (and 1 GB of their lower bits), and of layers whose
+// product takes longer than the way through memory.  Gradients with their losses, tiles formed
+// again and exponentials kept, 4096 rows to 100000 labels: of 1024 columns 3145 and 2785 us, 512 1888 and 1839,
+// 256 (in 16 bits, without the lower ones) 1273 and 1310; 32000 rows of 512 to 6000 884 and 876; 16384 of 1024 to
+// 100000 (3.3 GB) 12150 and 11340.
+constexpr int64_t kKeptBytes = 4ll << 30;
+constexpr int kKeptWidth = 512;
+static bool keeps(const wd_loss_args* a) {
+  return !a->stats && a->D >= kKeptWidth && a->N > kCarefulRows && (uint64_t)a->N * align_up(a->P, 64) <= (uint64_t)kKeptBytes / 2;
+}
+// Rows of a workgroup of k_loss_shares: fewer where the chip would not be full, more where the
+// workgroups' sums of db (four bytes of an output each) would be many.
+static int shares_rows(int64_t N, int64_t ld) {
+  const int64_t cols = (ld + 511) / 512;
+  return (N + 127) / 128 * cols >= 1024 ? 128 : (N + 63) / 64 * cols >= 1024 ? 64 : (N + 31) / 32 * cols >= 512 ? 32 : 16;
+}
+
+static LossPlan plan_loss(const wd_loss_args* a, bool grads, bool own_w = true) {
   LossPlan p{};
   const int64_t N = a->N, D = a->D, P = a->P;
   p.Dp = align_up(D, 8);
@@ -609,7 +790,7 @@ static LossPlan plan_loss(const wd_loss_args* a, bool grads) {
     at += align_up(bytes, 256);
     return here;
   };
-  if (p.copy_w) p.w = take((uint64_t)P * p.Dp * 2);
+  if (p.copy_w && own_w) p.w = take((uint64_t)P * p.Dp * 2);
   if (!grads) {
     const int64_t cols = (P + 255) / 256;
     p.block = std::min(N, std::max<int64_t>(16, 8192 / cols) * 256);
@@ -622,8 +803,9 @@ static LossPlan plan_loss(const wd_loss_args* a, bool grads) {
     p.rows = N;
     p.cols = P;
     p.terms = N <= kCarefulRows ? 2 : 1;
+    p.keep = keeps(a);
     const int64_t most = kPieceBytes / 2;
-    if ((uint64_t)N * align_up(P, 64) > (uint64_t)most) {
+    if (!p.keep && (uint64_t)N * align_up(P, 64) > (uint64_t)most) {
       if (N > P)
         p.rows = std::max<int64_t>(1, most / (int64_t)align_up(P, 64) / 256) * 256;
       else
@@ -642,12 +824,20 @@ static LossPlan plan_loss(const wd_loss_args* a, bool grads) {
     for (int64_t n : {p.rows, (N - 1) % p.rows + 1})
       for (int64_t c : {p.cols, (P - 1) % p.cols + 1}) {
         const int size = tile_size(n, align_up(c, 64));
-        db = std::max(db, (uint64_t)((n + size - 1) / size) * c * 4);
+        const int64_t each = p.keep ? shares_rows(n, align_up(c, 64)) : size;
+        db = std::max(db, (uint64_t)((n + each - 1) / each) * c * 4);
         const Cut cut = cut_products(n * p.terms, c, D, a->dweight, a->dx);
         split = std::max(split, split_bytes(p, cut, 0, c, N) + split_bytes(p, cut, 1, n * p.terms, P));
       }
     p.db = take(db);
     p.split = take(split);
+    if (!a->stats) {
+      if (p.keep)
+        p.label_z = take((uint64_t)N * 4), p.tops = take((uint64_t)N * (align_up(P, 64) / 64) * 4), p.lower = take((uint64_t)N * align_up(P, 64) / 2);
+      else
+        p.stats = take((uint64_t)N * sizeof(float2));
+      p.loss = take(plan_loss(a, false, false).end);
+    }
   }
   p.end = at;
   return p;
@@ -670,14 +860,25 @@ static void lay(const void* from, int64_t ld, int64_t N, int D, void* to, int64_
   });
 }
 
+// The weights as the product takes them.
 template <class T>
-static void run_loss(const wd_loss_args* a, const LossPlan& p, char* ws, hipStream_t s) {
-  const void* w = a->weight;
-  int64_t w_ld = a->weight_ld * 2;
-  if (p.copy_w) {
-    lay<T>(a->weight, a->weight_ld, a->P, a->D, ws + p.w, p.Dp, s);
-    w = ws + p.w, w_ld = p.Dp * 2;
-  }
+static const void* laid_weights(const wd_loss_args* a, const LossPlan& p, char* ws, int64_t& w_ld, hipStream_t s) {
+  w_ld = a->weight_ld * 2;
+  if (!p.copy_w) return a->weight;
+  lay<T>(a->weight, a->weight_ld, a->P, a->D, ws + p.w, p.Dp, s);
+  w_ld = p.Dp * 2;
+  return ws + p.w;
+}
+
+// What a call of the gradients that forms the losses itself has of them: its plan and workspace.
+struct Kept {
+  const LossPlan* plan;
+  char* ws;
+  PrepareArgs prepare;  // of all rows, where the plan keeps exponentials
+};
+template <class T>
+static void run_loss(const wd_loss_args* a, const LossPlan& p, char* ws, const void* w, int64_t w_ld, float* out_stats, const Kept* kept, hipStream_t s) {
+  const bool keep = kept && kept->plan->keep;
   for (int64_t n0 = 0; n0 < a->N; n0 += p.block) {
     const int64_t n = std::min(p.block, a->N - n0);
     const int size = tile_size(n, a->P), tiles = (a->P + size - 1) / size;
@@ -690,23 +891,39 @@ static void run_loss(const wd_loss_args* a, const LossPlan& p, char* ws, hipStre
     LossArgs l{};
     l.x = x, l.w = w, l.x_ld = x_ld, l.w_ld = w_ld, l.N = n, l.P = a->P, l.K = (int)p.Dp, l.bias = a->bias;
     l.target = a->target + n0, l.part = (float2*)(ws + p.part), l.label_z = (float*)(ws + p.label_z);
+    if (keep) {
+      l.dz_ld = align_up(a->P, 64), l.label_z = (float*)(kept->ws + kept->plan->label_z) + n0;
+      l.shares = (Upper*)(kept->ws + kept->plan->dz) + n0 * l.dz_ld, l.tops = (float*)(kept->ws + kept->plan->tops) + n0 * (l.dz_ld / 64);
+      l.lower = (uint16_t*)(kept->ws + kept->plan->lower) + n0 * (l.dz_ld / 4);
+    }
     launch_loss<T>(l, size, a->N <= kCarefulRows, s);
-    float* loss = a->loss ? a->loss + n0 : nullptr;
-    float2* stats = a->stats ? (float2*)a->stats + n0 : nullptr;
-    if (tiles <= 8 || (tiles <= 64 && n >= 16384))
-      hipLaunchKernelGGL((k_loss_join<4>), dim3((uint32_t)((n + 63) / 64)), dim3(256), 0, s, l.part, tiles, l.label_z, l.target, l.P, n, loss, stats);
-    else if (tiles <= 64)
-      hipLaunchKernelGGL((k_loss_join<16>), dim3((uint32_t)((n + 15) / 16)), dim3(256), 0, s, l.part, tiles, l.label_z, l.target, l.P, n, loss, stats);
+    const JoinArgs j{l.part, tiles, l.P, n, l.label_z, l.target, a->loss ? a->loss + n0 : nullptr, out_stats ? (float2*)out_stats + n0 : nullptr};
+    PrepareArgs q{};
+    if (keep) {
+      q = kept->prepare;
+      q.x = (const T*)q.x + n0 * q.x_ld, q.target += n0, q.info += n0, q.to = (T*)q.to + n0 * q.to_ld;
+      if (q.g) q.g += n0;
+    }
+    const auto launch = [&](auto lanes) {
+      constexpr int L = lanes.value, kRows = 256 / L;
+      const dim3 grid((uint32_t)((n + kRows - 1) / kRows));
+      if (keep)
+        hipLaunchKernelGGL((k_loss_ready<T, L>), grid, dim3(256), 0, s, j, q);
+      else
+        hipLaunchKernelGGL((k_loss_join<L>), grid, dim3(256), 0, s, j);
+    };
+    // (300 rows of 391 tiles with 16 lanes 69.7 us in all, with 64 67.7; 32000 rows of 24 198.5 and
+    // 203.4; four lanes are a little better only for the fewest tiles, 8192 rows of 4 11.9 and 12.2)
+    if (tiles <= 64)
+      launch(std::integral_constant<int, 16>{});
     else
-      hipLaunchKernelGGL((k_loss_join<64>), dim3((uint32_t)((n + 3) / 4)), dim3(256), 0, s, l.part, tiles, l.label_z, l.target, l.P, n, loss, stats);
+      launch(std::integral_constant<int, 64>{});
   }
 }
 
 template <class T>
 static void run_grads(const wd_loss_args* a, const LossPlan& p, char* ws, hipStream_t s) {
   const int64_t N = a->N, P = a->P, D = a->D;
-  const void* w = a->weight;
-  int64_t w_ld = a->weight_ld * 2;
   float* power = nullptr;
   RowInfo* info = (RowInfo*)(ws + p.info);
   const auto join = [&](ProductArgs q, int splits, const float* before, float* sum) {
@@ -720,34 +937,47 @@ static void run_grads(const wd_loss_args* a, const LossPlan& p, char* ws, hipStr
     if (a->dbias) hipLaunchKernelGGL(k_loss_db, dim3((uint32_t)((P + 255) / 256)), dim3(256), 0, s, DbArgs{nullptr, 0, (int)P, nullptr, false, a->dbias});
     return;
   }
-  if (p.copy_w) {
-    lay<T>(a->weight, a->weight_ld, P, (int)D, ws + p.w, p.Dp, s);
-    w = ws + p.w, w_ld = p.Dp * 2;
-  }
+  int64_t w_ld;
+  const void* w = laid_weights<T>(a, p, ws, w_ld, s);
   const bool own_power = __is_same(T, Half) && N <= kFewPowers;
   if (__is_same(T, Half)) {
     power = (float*)(ws + p.power);
     if (!own_power) hipLaunchKernelGGL(k_power, dim3(1), dim3(1024), 0, s, a->grad, N, power);
   }
+  const auto prepare_of = [&](int64_t at, int64_t r0, int64_t rows, const float* stats, void* again) {
+    return PrepareArgs{(const T*)a->x + at * a->x_ld, a->x_ld, (uint32_t)rows, (int)D, (int)P, (const float2*)stats + at,
+                       a->grad ? a->grad + at : nullptr, a->target + at, power, a->grad, own_power ? N : 0, info + at, (T*)(ws + p.x) + r0 * p.Dp, again, p.Dp};
+  };
+  const float* stats = a->stats;
+  if (!stats) {
+    stats = (float*)(ws + p.stats);
+    const Kept kept{&p, ws, prepare_of(0, 0, N, stats, nullptr)};
+    run_loss<T>(a, plan_loss(a, false, false), ws + p.loss, w, w_ld, p.keep ? nullptr : (float*)(ws + p.stats), &kept, s);
+  }
   float* sum = (float*)(ws + p.sum);
   for (int64_t n0 = 0; n0 < N; n0 += p.rows) {
     const int64_t n = std::min(p.rows, N - n0);
-    in_rows(n, p.Dp / 8, [&](int64_t r0, int64_t rows, dim3 grid) {
-      const int64_t at = n0 + r0;
-      const PrepareArgs prepare{(const T*)a->x + at * a->x_ld, a->x_ld, (uint32_t)rows, (int)D, (int)P, (const float2*)a->stats + at,
-                                a->grad ? a->grad + at : nullptr, a->target + at, power, a->grad, own_power ? N : 0, info + at, (T*)(ws + p.x) + r0 * p.Dp,
-                                p.terms > 1 ? (T*)(ws + p.x) + (n + r0) * p.Dp : nullptr, p.Dp};
-      hipLaunchKernelGGL((k_loss_prepare<T>), grid, dim3(256), 0, s, prepare);
-    });
+    if (!p.keep)
+      in_rows(n, p.Dp / 8, [&](int64_t r0, int64_t rows, dim3 grid) {
+        hipLaunchKernelGGL((k_loss_prepare<T>), grid, dim3(256), 0, s,
+                           prepare_of(n0 + r0, r0, rows, stats, p.terms > 1 ? (T*)(ws + p.x) + (n + r0) * p.Dp : nullptr));
+      });
     for (int64_t c0 = 0; c0 < P; c0 += p.cols) {
       const int64_t c = std::min(p.cols, P - c0);
       LossArgs l{};
       l.x = ws + p.x, l.w = (const char*)w + c0 * w_ld, l.x_ld = p.Dp * 2, l.w_ld = w_ld, l.N = n, l.P = (int)c, l.K = (int)p.Dp;
       l.bias = a->bias ? a->bias + c0 : nullptr, l.info = info + n0, l.p_first = (int)c0, l.dz = ws + p.dz, l.dz_ld = align_up(c, 64);
       l.db_part = a->dbias ? (float*)(ws + p.db) : nullptr, l.rest = p.terms > 1 ? (T*)l.dz + n * l.dz_ld : nullptr;
-      const int size = tile_size(n, l.dz_ld);
-      launch_dz<T>(l, size, s);
-      const DbArgs db{l.db_part, (int)((n + size - 1) / size), (int)c, power, n0 > 0, a->dbias + c0};
+      int tile = tile_size(n, l.dz_ld);  // rows of a sum of db
+      if (p.keep) {
+        tile = shares_rows(n, l.dz_ld);
+        const uint32_t cols = (uint32_t)((l.dz_ld + 511) / 512);
+        hipLaunchKernelGGL((k_loss_shares<T>), dim3((uint32_t)((n + tile - 1) / tile) * cols), dim3(256), 0, s,
+                           SharesArgs{(uint16_t*)l.dz, (const uint16_t*)(ws + p.lower), l.dz_ld, n, (int32_t)c, tile, (const float*)(ws + p.tops), (const float*)(ws + p.label_z), info, l.db_part}, cols);
+      } else {
+        launch_dz<T>(l, tile, s);
+      }
+      const DbArgs db{l.db_part, (int)((n + tile - 1) / tile), (int)c, power, n0 > 0, a->dbias + c0};
       if (a->dbias && !a->dweight) hipLaunchKernelGGL(k_loss_db, dim3((uint32_t)((c + 255) / 256)), dim3(256), 0, s, db);
       if (!a->dweight && !a->dx) continue;
       const Cut cut = cut_products(n * p.terms, c, D, a->dweight, a->dx);
@@ -797,7 +1027,6 @@ static wd_status check_loss(const wd_loss_args* a, bool grads) {
     if (a->N > 0 && !a->loss && !a->stats) return fail(WD_EINVAL, "cross_entropy: null loss and stats");
     return WD_OK;
   }
-  if (a->N > 0 && !a->stats) return fail(WD_EINVAL, "cross_entropy: the gradients need stats");
   if (!a->dx && !a->dweight && !a->dbias) return fail(WD_EINVAL, "cross_entropy: no gradient wanted");
   if ((uintptr_t)a->grad & 3 || (uintptr_t)a->dx & 1 || (uintptr_t)a->dweight & 1 || (uintptr_t)a->dbias & 3)
     return fail(WD_EINVAL, "cross_entropy: misaligned gradient");
@@ -823,10 +1052,17 @@ static wd_status loss_call(const wd_loss_args* a, bool grads, void* ws, size_t w
   }
   const LossPlan p = plan_loss(a, grads);
   if (!ws || ws_bytes < p.end || (uintptr_t)ws & 255) return fail(WD_EINVAL, "cross_entropy: workspace missing, too small or not 256-byte aligned");
-  if (grads)
-    a->type == WD_F16 ? run_grads<Half>(a, p, (char*)ws, s) : run_grads<Bf16>(a, p, (char*)ws, s);
-  else
-    a->type == WD_F16 ? run_loss<Half>(a, p, (char*)ws, s) : run_loss<Bf16>(a, p, (char*)ws, s);
+  const auto run = [&](auto type) {
+    using T = decltype(type);
+    if (grads) {
+      run_grads<T>(a, p, (char*)ws, s);
+      return;
+    }
+    int64_t w_ld;
+    const void* w = laid_weights<T>(a, p, (char*)ws, w_ld, s);
+    run_loss<T>(a, p, (char*)ws, w, w_ld, a->stats, nullptr, s);
+  };
+  a->type == WD_F16 ? run(Half{}) : run(Bf16{});
   return hip_check(hipGetLastError(), "cross_entropy");
 }
 

@@ -29,7 +29,7 @@ def loss(**kw):
 BAD = [dict(N=-1), dict(N=1 << 31), dict(D=0), dict(D=1 << 22), dict(P=0), dict(P=1 << 24), dict(type=wf.WD_F32), dict(type=9), dict(x_ld=63),
        dict(weight_ld=63), dict(weight=None), dict(x=None), dict(target=None), dict(x=P + 1), dict(weight=P + 1), dict(bias=P + 2),
        dict(target=P + 2), dict(loss=P + 2), dict(stats=P + 4)]
-BAD_GRADS = [dict(dx_ld=63), dict(dweight_ld=63), dict(stats=None), dict(dx=None, dweight=None, dbias=None), dict(grad=P + 2), dict(dx=P + 1),
+BAD_GRADS = [dict(dx_ld=63), dict(dweight_ld=63), dict(dx=None, dweight=None, dbias=None), dict(grad=P + 2), dict(dx=P + 1),
              dict(dweight=P + 1), dict(dbias=P + 2), dict(N=(1 << 19) + 1, P=(1 << 19) + 1)]
 
 
@@ -59,6 +59,10 @@ def test_loss_workspaces():
     sizes = [wf.wd_cross_entropy_grads_workspace_bytes(loss(N=n, P=p)) for n, p in ((1 << 16, 1 << 14), (1 << 20, 1 << 14), (1 << 14, 1 << 20))]
     assert all(s < (1 << 31) for s in sizes)
     assert wf.wd_cross_entropy_workspace_bytes(loss(N=1 << 20, P=1 << 17)) < 1 << 26
+    # (without stats the gradients may keep 2.6 bytes of each logit, up to 5.3 GB)
+    need = lambda **kw: wf.wd_cross_entropy_grads_workspace_bytes(loss(stats=None, D=512, x_ld=512, weight_ld=512, dx_ld=512, dweight_ld=512, **kw))  # noqa: E731
+    assert 1 << 31 < need(N=1 << 15, P=1 << 15) < 2.7 * 2 ** 30 + (1 << 30)
+    assert all(need(N=n, P=p) < 7 * 2 ** 30 for n, p in ((1 << 16, 1 << 15), (1 << 17, 1 << 15), (1 << 14, 1 << 18), (1 << 19, 1 << 14)))
 
 
 def clip(tensors, n=None, max_norm=1.0, norm=P, ws=P, ws_bytes=1 << 30):
