@@ -73,8 +73,8 @@ __device__ __forceinline__ float2 join(float2 a, float2 b) {
 // a thread, and passed round through LDS behind it: read at the end it is round trips that
 // nothing hides (losses of 32000 rows to 6000 labels 367 us, and 349 without; gradients of
 // 4096 rows to 100000 3315 and 3220).  Nor does the product wait for it: passed round before
-// the first step, gradients of 777 rows to 777 labels are 62.9 us, and 61.1 so; of 256 rows to
-// 100000 138.1 and 136.8.  The logits are acc + bias, -inf past the last output.
+// the first step, gradients of 777 rows to 3001 labels are 62.9 us, and 61.1 so; of 2048 rows to
+// 6000 138.1 and 136.8.  The logits are acc + bias, -inf past the last output.
 __device__ __forceinline__ float bias_of(const LossArgs& a, int p) { return p >= a.P ? -INFINITY : a.bias ? a.bias[p] : 0.0f; }
 template <int TN>
 __device__ __forceinline__ void read_bias(const float* kept, float (&bias)[TN][4]) {
@@ -102,9 +102,11 @@ __device__ __forceinline__ float share_of(Upper upper, uint32_t lower) {
   return bits ? __uint_as_float(bits | 0x40) * (1 / kShare) : 0.0f;
 }
 
+// Bound by the matrix instructions and what surrounds a tile: 32000 rows of 1024 to 6000 labels 340 us, 1160
+// TFLOP/s; a tile of 256 takes 1.5 us a step and 4 us at its ends.
 // KEEP: the exponentials are left as well, each over that of the largest of its 64 outputs, which are a
 // wavefront's (4096 rows of 1024 to 100000: 738 us without them, 1000 with, of which the stores'
-// bytes are 200).
+// bytes are 200).  They pass the caches by, which the tiles' operands use: the whole call 2830 us, 2790 so.
 template <class T, int BM, int BN, int WM, int WN, bool EXACT, bool KEEP>
 __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2) k_loss(LossArgs a, uint32_t row_tiles, uint32_t col_tiles) {
   using Tl = Tile<T, BM, BN, WM, WN, false, false, EXACT>;
@@ -176,7 +178,7 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
   if constexpr (KEEP) {
     static_assert(TN == 4 && kStoreBytes<Upper, TN> * WM * WN + WN * BM * 8 <= Tl::kBytes, "");
     store_tile<Upper, TM, TN>(a.shares + (n0 + wm) * a.dz_ld + p0 + wn, a.dz_ld, a.N - n0 - wm, a.dz_ld - p0 - wn,
-                              lds + wave * kStoreBytes<Upper, TN>, [&](int i, int j, int e) { return acc[i][j][e]; });
+                              lds + wave * kStoreBytes<Upper, TN>, [&](int i, int j, int e) { return acc[i][j][e]; }, true);
   }
   __syncthreads();
   for (int r = threadIdx.x; r < BM; r += 64 * WM * WN) {
@@ -601,7 +603,10 @@ __global__ void __launch_bounds__(256) k_product_join(ProductArgs a, int splits,
 // exact gradients: 1.6e-3).
 constexpr int64_t kCarefulRows = 64;
 
-// Tiles: the largest that gives every compute unit one (256, 192 of the middle ones).
+// Tiles: the largest that gives every compute unit one, or three quarters of them one of the middle
+// ones.  (Losses of rows of 1024 in tiles of 256, 128 and 64, us: 4096 rows to 4096 labels 33.6, 39.8 and 52;
+// 4096 to 3000 32.4, 32.5 and 41.4; 2000 to 2000 30.5, 16.5 and 17.4; 2000 to 1500 30.0, 16.3 and
+// 15.5; 200 to 6000 27.8, 14.7 and 11.3.)
 enum TileSize { kSmall = 64, kMiddle = 128, kLarge = 256 };
 static int64_t tiles_of(int64_t M, int64_t C, int size) { return ((M + size - 1) / size) * ((C + size - 1) / size); }
 static TileSize tile_size(int64_t M, int64_t C) {

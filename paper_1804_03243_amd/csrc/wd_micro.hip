@@ -59,8 +59,8 @@ __device__ __forceinline__ uint32_t to_codes(const float (&v)[8], uint32_t& code
   return bad ? 255 : (uint32_t)s;
 }
 
-// Four lanes to a block, eight values each.  Bound by memory.  Lanes of a scale row's
-// padding write its zeros.
+// Four lanes to a block, eight values each.  Bound by memory: 100000 rows of 1024 in bfloat16 51
+// us, 5.1 TB/s.  Lanes of a scale row's padding write its zeros.
 template <class T>
 __global__ void __launch_bounds__(256) k_micro(const T* x, int64_t ld, uint32_t N, int D, uint32_t* codes, uint8_t* scales) {
   const int64_t blocks = micro_blocks(D), sl = micro_scales(D);
@@ -77,7 +77,8 @@ __global__ void __launch_bounds__(256) k_micro(const T* x, int64_t ld, uint32_t 
   }
 }
 
-// The values, exact in bfloat16 and 32 bits.
+// The values, exact in bfloat16 and 32 bits.  Bound by memory: 100000 rows of 1024 to bfloat16 63
+// us, 4.1 TB/s.
 template <class O>
 __global__ void __launch_bounds__(256) k_micro_values(const uint32_t* codes, const uint8_t* scales, uint32_t N, int D, O* out, int64_t ld) {
   const int64_t blocks = micro_blocks(D), sl = micro_scales(D);
@@ -120,7 +121,10 @@ struct MicroArgs {
 
 // Many rows: tiles of BM rows and BN outputs, as the 16-bit products go (Tile): a step is
 // 128 bytes of a row, here 256 columns, its halves 128.  The scales of two steps
-// come with the even one, 16 bytes of each row, into two places of their own.
+// come with the even one, 16 bytes of each row, into two places of their own.  64000 rows of 1024 to
+// 6000 outputs in 32 bits 390 us: bound by the outputs' 1.5 GB (300 us), which tiles of three workgroups
+// on a compute unit write while others multiply (in tiles of 256 x 256 837 us, of 256 x 128 526, 64-row
+// tiles of eight wavefronts 446).
 template <class O, int BM, int BN, int WM, int WN>
 __global__ void __launch_bounds__(64 * WM * WN, 2) k_micro_tiles(MicroArgs a, uint32_t row_tiles, uint32_t col_tiles) {
   constexpr int kWaves_ = WM * WN, TM = BM / WM / 16, TN = BN / WN / 16;
@@ -224,7 +228,8 @@ __global__ void __launch_bounds__(64 * WM * WN, 2) k_micro_tiles(MicroArgs a, ui
 // form itself, in LDS, while its first reads of W are under way.  A wavefront takes 16
 // outputs, W straight from memory, the next 512 columns' reads under way while one is
 // multiplied.  Rows in LDS are an odd number of 16-byte blocks apart, so that reads of
-// several rows fall on different banks.
+// several rows fall on different banks.  (Rows of 1024 to 6000 outputs this way and in two launches:
+// 1 row 3.5 and 5.4 us, 8 rows 4.8 and 6.0, 16 rows 6.3 and 5.9; 8 rows of 2000 to 5000 7.9 and 7.4.)
 constexpr int kFewRows = 8;
 template <class T, class O>
 __global__ void __launch_bounds__(256, 4) k_micro_few(MicroArgs a, const T* rows, int64_t ld, int D) {
@@ -348,6 +353,10 @@ static void launch_micro_product(MicroArgs a, const void* x, int32_t type, int64
     return;
   }
   quantize(x, ld, a.N, D, type, codes, scales, s);
+  // The largest tiles that fill the chip.  (128 x 128 and 64 x 64: 300 rows of 1024 to 100000 49.8 and 55.5 us, 2000
+  // to 3001 16.5 and 16.6, 900 to 6000 15.2 and 15.3, 900 to 3001 12.6 and 10.9.  64 x 64 and 32 x 32: 300 rows to
+  // 3001 8.1 and 8.4, 100 to 6000 7.7 and 7.5, 100 of 512 to 500 6.4 and 5.7.  32 x 64 for up to 32 rows: 32 rows
+  // to 100000 15.0, in 64 x 64 16.6; 16 rows of 256 to 30000 5.5, in 32 x 32 6.0, to 6000 6.2 and 5.9.)
   const auto tiles = [&](int64_t m, int64_t n) { return ((a.N + m - 1) / m) * ((a.P + n - 1) / n); };
   a.stream = (uint64_t)a.N * a.P * sizeof(O) >= (256u << 20);
   if (a.N > 64 && tiles(128, 128) >= 384)
