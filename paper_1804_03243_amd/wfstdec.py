@@ -1243,6 +1243,9 @@ class Micro:
             if t.dtype != torch.uint8 or t.dim() != 2 or t.shape[0] != rows or t.numel() != n or not t.is_contiguous() \
                     or t.device != codes.device:
                 raise ValueError(f"{what} must be a contiguous uint8 tensor of {rows} rows, {n} bytes in all, on {codes.device}")
+        self._hold(codes, scales, rows, D)
+
+    def _hold(self, codes, scales, rows, D):
         self.codes, self.scales, self.rows, self.D, self.device = codes, scales, rows, D, codes.device
         # (tensors of our own on the same memory)
         self._kept = (codes.detach(), scales.detach())
@@ -1269,10 +1272,10 @@ def micro(x):
     _matrix(x, types, x.device, "x")
     _no_gradient(torch, "micro", x)
     rows, D = x.shape
-    n_codes, n_scales = wd_micro_bytes(rows, D)
+    wd_micro_bytes(rows, D)  # the library's checks of the sizes
     each = ((D + 31) // 32 * 16, (D + 511) // 512 * 16)
-    m = Micro(torch.empty((rows, each[0]), dtype=torch.uint8, device=x.device),
-              torch.empty((rows, each[1]), dtype=torch.uint8, device=x.device), D)
+    m = Micro.__new__(Micro)
+    m._hold(*(torch.empty((rows, n), dtype=torch.uint8, device=x.device) for n in each), rows, D)
     _enqueue(x.device, lambda stream: wd_micro_quantize(x.data_ptr(), types[x.dtype], _ld(x), m.desc, stream))
     return m
 
