@@ -485,10 +485,10 @@ typedef struct {
 } wd_loss_args;
 /* wd_cross_entropy_grads: after wd_cross_entropy of the same x, weight, bias and target (`stats`), or
  * by itself (`stats` NULL), which takes less time and more workspace: 2.6 bytes of each
- * logit, up to 5.3 GB, for its exponential in 20 bits (off by 2^-18 of it).
+ * logit, up to 5.3 GB, for its exponential in 20 bits (off by 2^-18 of it), and a copy of x up to 4 GB.
  * At least one gradient is wanted, and they overlap nothing else.  N = 0: dweight and
  * dbias are zeros.  At most 2^19 rows or labels (one of the two may be more).
- * ws as for wd_project (the sizes depend on which gradients are wanted). */
+ * ws as for wd_project (the sizes depend on which gradients are wanted, and on whether there are stats). */
 wd_status wd_cross_entropy_workspace_bytes(const wd_loss_args* a, size_t* bytes);
 wd_status wd_cross_entropy(const wd_loss_args* a, void* ws, size_t ws_bytes, void* stream);
 wd_status wd_cross_entropy_grads_workspace_bytes(const wd_loss_args* a, size_t* bytes);

@@ -766,15 +766,16 @@ static uint64_t split_bytes(const LossPlan& p, const Cut& cut, int i, int64_t M,
   return cut.splits[i] > 1 || (cut.splits[i] && pieces) ? (uint64_t)cut.splits[i] * M * p.Dp * 4 : 0;
 }
 
-// Exponentials are kept up to 4 GB of dz (and 1 GB of their lower bits), and of layers whose
-// product takes longer than the way through memory.  Gradients with their losses, tiles formed
+// Exponentials are kept up to 4 GB of dz (and 1 GB of their lower bits; the rows' copy is of all rows
+// then, 4 GB too), and of layers whose product takes longer than the way through memory.  Gradients with their losses, tiles formed
 // again and exponentials kept, 4096 rows to 100000 labels: of 1024 columns 3145 and 2785 us, 512 1888 and 1839,
 // 256 (in 16 bits, without the lower ones) 1273 and 1310; 32000 rows of 512 to 6000 884 and 876; 16384 of 1024 to
 // 100000 (3.3 GB) 12150 and 11340.
 constexpr int64_t kKeptBytes = 4ll << 30;
 constexpr int kKeptWidth = 512;
 static bool keeps(const wd_loss_args* a) {
-  return !a->stats && a->D >= kKeptWidth && a->N > kCarefulRows && (uint64_t)a->N * align_up(a->P, 64) <= (uint64_t)kKeptBytes / 2;
+  return !a->stats && a->D >= kKeptWidth && a->N > kCarefulRows && a->P < (1 << 22) &&  // (a tile's rows of dz within 31 bits)
+         (uint64_t)a->N * std::max(align_up(a->P, 64), align_up(a->D, 8)) <= (uint64_t)kKeptBytes / 2;
 }
 // Rows of a workgroup of k_loss_shares: fewer where the chip would not be full, more where the
 // workgroups' sums of db (four bytes of an output each) would be many.

@@ -63,6 +63,9 @@ def test_loss_workspaces():
     need = lambda **kw: wf.wd_cross_entropy_grads_workspace_bytes(loss(stats=None, D=512, x_ld=512, weight_ld=512, dx_ld=512, dweight_ld=512, **kw))  # noqa: E731
     assert 1 << 31 < need(N=1 << 15, P=1 << 15) < 2.7 * 2 ** 30 + (1 << 30)
     assert all(need(N=n, P=p) < 7 * 2 ** 30 for n, p in ((1 << 16, 1 << 15), (1 << 17, 1 << 15), (1 << 14, 1 << 18), (1 << 19, 1 << 14)))
+    # nothing is kept of outputs that a tile's offsets would not reach, or of very many rows
+    assert need(N=500, P=(1 << 22) - 64) > 1 << 32 > need(N=500, P=1 << 22)
+    assert need(N=1 << 24, P=64) < need(N=1 << 22, P=64) * 4
 
 
 def clip(tensors, n=None, max_norm=1.0, norm=P, ws=P, ws_bytes=1 << 30):

@@ -179,3 +179,21 @@ def test_parts_of_the_gradients(wf):  # noqa: F811
                 assert float((g.float() - w.float()).norm()) <= 2.0 ** -7 * float(w.float().norm())
             else:
                 assert g is None
+
+
+@pytest.mark.parametrize("N,P", [(300, 4_194_000), (300_000, 5000)])
+def test_as_far_as_is_kept(wf, N, P):  # noqa: F811
+    """Close to the most that is kept: as with the logits formed again, but for the roundings."""
+    gen = torch.Generator(DEV).manual_seed(5)
+    rnd = lambda *s: torch.randn(s, generator=gen, device=DEV)  # noqa: E731
+    w, x = (rnd(P, 512) / 10).to(BF16), rnd(N, 512).to(BF16)
+    t, g = torch.randint(-1, P, (N,), generator=gen, device=DEV, dtype=torch.int32), torch.rand(N, device=DEV) / N
+    loss, dx, dw, db = wf.cross_entropy_grads(x, w, t, None, g)
+    a = wf._loss_args(x, w, t, None)
+    stats = torch.empty((N, 2), device=DEV)
+    assert torch.equal(wf._loss(a, x.device, stats), loss)
+    ex, ew, _ = wf._loss_grads(a, x, w, None, stats, None, g, (True, True, True))
+    for v, e in ((dx, ex), (dw, ew)):
+        assert bool(torch.isfinite(v).all())
+        # (each within two roundings, of dz and its own, of the same values)
+        assert float((v.float() - e.float()).norm()) <= 4 * 2.0 ** -8 * float(e.float().norm())
