@@ -1158,7 +1158,7 @@ def cross_entropy(hidden, weight, target, bias=None):
     cross_entropy_grads: a backward pass under capture is refused, since autograd
     would wait on streams that the capture does not hold."""
     torch = _torch()
-    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in (hidden, weight, bias)):
+    if (hidden.requires_grad or weight.requires_grad or bias is not None and bias.requires_grad) and torch.is_grad_enabled():
         if weight.is_cuda and torch.cuda.is_current_stream_capturing():
             raise ValueError("cross_entropy of tensors that require a gradient cannot be captured: use cross_entropy_grads")
         return _cross_entropy_function().apply(hidden, weight, target, bias)
