@@ -60,13 +60,14 @@ constexpr int kStepK = 64;  // columns of a step: 128 bytes of a row
 __device__ __forceinline__ int swizzle(int row) { return (row >> 1) & 7; }
 
 // The tile of a workgroup by its number.  Workgroups go round the eight XCDs, each with an
-// L2 of its own: an XCD takes a run of tiles, in groups of kGroup rows of tiles
+// L2 of its own: an XCD takes a run of tiles, in groups of kGroup (or group_rows) rows of tiles
 // column by column, so that its workgroups share rows of x and of W.
 constexpr uint32_t kGroup = 8;
-__device__ __forceinline__ void tile_at(uint32_t number, uint32_t rows, uint32_t cols, uint32_t& row, uint32_t& col) {
+__device__ __forceinline__ void tile_at(uint32_t number, uint32_t rows, uint32_t cols, uint32_t& row, uint32_t& col,
+                                        uint32_t group_rows = kGroup) {
   const uint32_t all = rows * cols, xcd = number % 8, q = all / 8, r = all % 8;
   const uint32_t at = xcd * q + min(xcd, r) + number / 8;
-  const uint32_t group = at / (kGroup * cols), first = group * kGroup, height = min(kGroup, rows - first);
+  const uint32_t group = at / (group_rows * cols), first = group * group_rows, height = min(group_rows, rows - first);
   const uint32_t in = at - first * cols;
   col = in / height;
   row = first + in % height;
