@@ -113,7 +113,9 @@ __global__ void __launch_bounds__(64 * WM * WN, BM * BN / WM / WN > 8192 ? 1 : 2
   constexpr int TM = Tl::TM, TN = Tl::TN;
   extern __shared__ __attribute__((aligned(1024))) char lds[];
   uint32_t row_tile, col_tile;
-  my_tile(row_tiles, col_tiles, row_tile, col_tile);
+  // (Groups of 4, 8 and 16 rows of tiles: gradients of 777 rows to 3001, in the smallest tiles, 55.6, 54.0 and 52.8 us;
+  // losses of 32000 to 6000 341, 344 and 350, gradients of 4096 to 100000 2738, 2733 and 2772.)
+  tile_at(blockIdx.x, row_tiles, col_tiles, row_tile, col_tile, BM > 64 ? kGroup : 16);
   const int64_t n0 = (int64_t)row_tile * BM;
   const int p0 = (int)col_tile * BN;
   float* kept_bias = (float*)(lds + Tl::kBytes);  // [BN]
